@@ -271,6 +271,62 @@ int gptaq_pack_codes(const uint8_t* codes, int64_t m, int64_t n, int64_t ldc, in
                      uint32_t* packed, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Running layers that the solve has quantised: products with the codes, scales and zeros of gptaq_quantize_layer, and
+ * what lies between the products of a decoder layer.  Activations are token-major bf16, or 8-bit codes with one scale
+ * per token: x[t][j] = scales[t] * codes[t][j], codes -127 .. 127 (symmetric).  Rows may have any leading dimension and
+ * any alignment of the element; calls with tokens = 0 do nothing.
+ *
+ * gptaq_linear_pack lays the weights of an m x n layer out for the products, once per layer:
+ *   codes, scales, zeros : as gptaq_quantize_layer returns them, solved with bits <= 4 (codes have leading dimension ldc,
+ *            scales and zeros G = max(1, n / group)).  Zeros are integers 0 .. 15.
+ *   group  : 32, 64 or 128 with n % group == 0, or <= 0 for one group per row.
+ *   weights: gptaq_linear_weights_bytes(m, n, group) bytes (0 for sizes that are out of range), 256-byte aligned;
+ *            about m n / 2 + 5 m G bytes.
+ *   info   : int32, out: 0, or 1 + the last row with a code above 15 or a zero that is no integer in 0 .. 15 (the
+ *            weights are then garbage).
+ * gptaq_linear, gptaq_linear_i8: Y[t][r] = sum_j scale[r][j / group] (code[r][j] - zero[r][j / group]) x[t][p(j)] + bias[r].
+ *   perm   : n x int32 or NULL: p(j) = perm[j], for codes in the order of gptaq_act_order (Wp = W[:, perm], the order in
+ *            which the solve returns them); NULL: p(j) = j.  An entry outside 0 .. n - 1 stands for an activation of 0.
+ *   bias   : m x fp32 or NULL.
+ *   Y      : (tokens x m), leading dimension ldy, fp32 where y_f32 != 0, else bf16.  Must not overlap the inputs.
+ *   ws     : >= gptaq_linear_workspace_bytes(tokens, m, n) bytes, 256-byte aligned; the size for more tokens serves fewer.
+ *   m, n   : at most 2^20; tokens at most 2^23.
+ * Weights enter the products exactly; sums are taken in fp32 (bf16 activations) or, inside a group, in int32 (8 bits),
+ * group sums are scaled and added in fp32, and the result is rounded once.
+ */
+size_t gptaq_linear_weights_bytes(int64_t m, int64_t n, int group);
+int gptaq_linear_pack(const uint8_t* codes, int64_t ldc, const float* scales, const float* zeros, int64_t m, int64_t n,
+                      int group, void* weights, size_t weights_bytes, int32_t* info, void* stream);
+size_t gptaq_linear_workspace_bytes(int64_t tokens, int64_t m, int64_t n);
+int gptaq_linear(const uint16_t* X, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights, int64_t m,
+                 int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes,
+                 void* stream);
+int gptaq_linear_i8(const int8_t* X, const float* x_scales, int64_t tokens, int64_t ldx, const int32_t* perm,
+                    const void* weights, int64_t m, int64_t n, int group, const float* bias, void* Y, int64_t ldy,
+                    int y_f32, void* ws, size_t ws_bytes, void* stream);
+
+/* gptaq_rms_norm: h = X + residual (X alone if residual is NULL), Y = h * weight / sqrt(mean(h^2) + eps) over each row's n
+ *   columns; weight: n x bf16 or NULL for ones (rotated models have theirs in the next layer's weights).  sum, if not
+ *   NULL, receives h (the next residual).  h is not rounded on its way to Y.
+ * gptaq_silu_mul: Y = gate / (1 + exp(-gate)) * up; gate and up may be the two halves of one product's rows.
+ * _i8: the same Y, in fp32, as codes on a symmetric 8-bit grid: scales[t] = clip * max|Y[t][:]| / 127,
+ *   code = clamp(rint(Y / scale), -127, 127), with Y / scale taken as Y * (1 / scale) (a code within 2^-15 of a
+ *   rounding boundary may go either way).  clip in (0, 1].  A row of zeros has scale 0; a row with a value that is not
+ *   finite has scale NaN.
+ * All sums and products in fp32, each output rounded once.  An output may be an input's own memory (same pointer and
+ * leading dimension); otherwise they must not overlap. */
+int gptaq_rms_norm(const uint16_t* X, const uint16_t* residual, const uint16_t* weight, int64_t tokens, int64_t n,
+                   int64_t ldx, int64_t ldr, float eps, uint16_t* sum, int64_t lds, uint16_t* Y, int64_t ldy,
+                   void* stream);
+int gptaq_rms_norm_i8(const uint16_t* X, const uint16_t* residual, const uint16_t* weight, int64_t tokens, int64_t n,
+                      int64_t ldx, int64_t ldr, float eps, uint16_t* sum, int64_t lds, float clip, int8_t* codes,
+                      int64_t ldc, float* scales, void* stream);
+int gptaq_silu_mul(const uint16_t* gate, const uint16_t* up, int64_t tokens, int64_t n, int64_t ldg, int64_t ldu,
+                   uint16_t* Y, int64_t ldy, void* stream);
+int gptaq_silu_mul_i8(const uint16_t* gate, const uint16_t* up, int64_t tokens, int64_t n, int64_t ldg, int64_t ldu,
+                      float clip, int8_t* codes, int64_t ldc, float* scales, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Measurement aid (not part of the method).  While enabled, the library brackets its kernels
  * with HIP events on the caller's stream, grouped by tag:
  *   0 accumulate MFMA GEMM (H and dXXT, one launch per pass)   1 accumulate split/transpose pass

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -67,6 +67,22 @@ _SIGS = {
                                                 _c.c_int, _c.c_float, _c.c_void_p]),
     "gptaq_packed_words_per_row": (_c.c_int64, [_c.c_int64, _c.c_int]),
     "gptaq_pack_codes": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_void_p]),
+    "gptaq_linear_weights_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int64, _c.c_int]),
+    "gptaq_linear_pack": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int, _c.c_void_p,
+                                     _c.c_size_t, _c.c_void_p, _c.c_void_p]),
+    "gptaq_linear_workspace_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int64, _c.c_int64]),
+    "gptaq_linear": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int, _c.c_void_p,
+                                _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "gptaq_linear_i8": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64,
+                                   _c.c_int, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "gptaq_rms_norm": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float,
+                                  _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p]),
+    "gptaq_rms_norm_i8": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float,
+                                     _c.c_void_p, _c.c_int64, _c.c_float, _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p]),
+    "gptaq_silu_mul": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                  _c.c_void_p]),
+    "gptaq_silu_mul_i8": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float, _c.c_void_p,
+                                     _c.c_int64, _c.c_void_p, _c.c_void_p]),
     "gptaq_profile_enable": (_c.c_int, [_c.c_int]),
     "gptaq_profile_read": (_c.c_int, [_c.c_int, _c.POINTER(_c.c_int64), _c.POINTER(_c.c_double)]),
     "gptaq_measure_mfma_peak": (_c.c_int, [_c.c_int, _c.c_int, _c.c_void_p, _c.c_size_t, _c.POINTER(_c.c_double),
@@ -390,3 +406,163 @@ def gptaq_pack_codes(codes: torch.Tensor, bits: int) -> torch.Tensor:
     _check(load().gptaq_pack_codes(_ptr(codes), m, n, codes.stride(0), int(bits), _ptr(out), _stream()),
            "gptaq_pack_codes")
     return out
+
+
+# ---- running quantised layers
+
+class LinearWeights(NamedTuple):
+    """A layer's weights as gptaq_linear and gptaq_linear_i8 read them."""
+    data: torch.Tensor
+    m: int
+    n: int
+    group: int                                   # 0: one group per row
+    perm: Optional[torch.Tensor]
+    bias: Optional[torch.Tensor]
+    info: torch.Tensor                           # int32 of 1, on the GPU: 0, or 1 + a row whose codes or zeros do not fit in 4 bits
+
+
+def gptaq_linear_weights_bytes(m: int, n: int, group: int) -> int:
+    return load().gptaq_linear_weights_bytes(m, n, group)
+
+
+def gptaq_linear_pack(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, group: int,
+                      perm: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None) -> LinearWeights:
+    """Lays out what gptaq_quantize_layer returned (bits <= 4; group 32, 64, 128, or <= 0 for one per row).  perm: the columns'
+    order where the layer was solved with act_order; bias: fp32."""
+    _need(codes, torch.uint8, "codes")
+    m, n = codes.shape
+    G = max(1, n // group) if group > 0 else 1
+    for t, name in ((scales, "scales"), (zeros, "zeros")):
+        if not t.is_cuda or t.dtype != torch.float32 or t.shape != (m, G) or not t.is_contiguous():
+            raise GptaqError(f"gptaq_linear_pack: {name}: expected a contiguous {m} x {G} float32 CUDA tensor")
+    if perm is not None:
+        _need_vec(perm, torch.int32, "perm")
+        if perm.numel() != n:
+            raise GptaqError("gptaq_linear_pack: perm: expected one entry per column")
+    if bias is not None:
+        _need_vec(bias, torch.float32, "bias")
+        if bias.numel() != m:
+            raise GptaqError("gptaq_linear_pack: bias: expected one entry per row")
+    data = workspace(gptaq_linear_weights_bytes(m, n, group), codes.device)
+    info = torch.empty(1, dtype=torch.int32, device=codes.device)
+    _check(load().gptaq_linear_pack(_ptr(codes), codes.stride(0), _ptr(scales), _ptr(zeros), m, n, int(group), _ptr(data), data.numel(),
+                                    _ptr(info), _stream()), "gptaq_linear_pack")
+    return LinearWeights(data, m, n, max(0, int(group)), perm, bias, info)
+
+
+def gptaq_linear_workspace_bytes(tokens: int, m: int, n: int) -> int:
+    return load().gptaq_linear_workspace_bytes(tokens, m, n)
+
+
+def _linear_out(X: torch.Tensor, w: LinearWeights, dtype, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
+    if X.shape[1] != w.n:
+        raise GptaqError(f"{name}: X has {X.shape[1]} columns, the weights {w.n}")
+    if out is None:
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise GptaqError(f"{name}: the output is bfloat16 or float32")
+        return torch.empty((X.shape[0], w.m), dtype=dtype, device=X.device)
+    _need(out, out.dtype if out.dtype == torch.float32 else torch.bfloat16, "out")
+    if out.shape != (X.shape[0], w.m):
+        raise GptaqError(f"{name}: out: shape mismatch")
+    return out
+
+
+def gptaq_linear(X: torch.Tensor, weights: LinearWeights, ws: torch.Tensor, out: Optional[torch.Tensor] = None,
+                 dtype=torch.bfloat16) -> torch.Tensor:
+    """X W^T + bias for token-major bf16 X; returns (tokens x m), bf16 or fp32 (`dtype`, or the type of `out`)."""
+    _need(X, torch.bfloat16, "X")
+    Y = _linear_out(X, weights, dtype, out, "gptaq_linear")
+    _check(load().gptaq_linear(_ptr(X), X.shape[0], X.stride(0), _ptr(weights.perm), _ptr(weights.data), weights.m, weights.n, weights.group,
+                               _ptr(weights.bias), _ptr(Y), Y.stride(0), int(Y.dtype == torch.float32), _ptr(ws),
+                               ws.numel() * ws.element_size(), _stream()), "gptaq_linear")
+    return Y
+
+
+def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWeights, ws: torch.Tensor,
+                    out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
+    """gptaq_linear for 8-bit activations scales[t] * codes[t][:]."""
+    _need(codes, torch.int8, "codes"); _need_vec(scales, torch.float32, "scales")
+    if scales.numel() != codes.shape[0]:
+        raise GptaqError("gptaq_linear_i8: scales: expected one per token")
+    Y = _linear_out(codes, weights, dtype, out, "gptaq_linear_i8")
+    _check(load().gptaq_linear_i8(_ptr(codes), _ptr(scales), codes.shape[0], codes.stride(0), _ptr(weights.perm), _ptr(weights.data),
+                                  weights.m, weights.n, weights.group, _ptr(weights.bias), _ptr(Y), Y.stride(0),
+                                  int(Y.dtype == torch.float32), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "gptaq_linear_i8")
+    return Y
+
+
+def _norm_args(X: torch.Tensor, weight: Optional[torch.Tensor], residual: Optional[torch.Tensor], total: Optional[torch.Tensor], name: str):
+    _need(X, torch.bfloat16, "X")
+    if weight is not None:
+        _need_vec(weight, torch.bfloat16, "weight")
+        if weight.numel() != X.shape[1]:
+            raise GptaqError(f"{name}: weight: expected one entry per column")
+    if residual is not None:
+        _need(residual, torch.bfloat16, "residual")
+        if residual.shape != X.shape:
+            raise GptaqError(f"{name}: residual: shape mismatch")
+        if total is None:
+            total = torch.empty(X.shape, dtype=torch.bfloat16, device=X.device)
+    if total is not None:
+        _need(total, torch.bfloat16, "total")
+        if total.shape != X.shape:
+            raise GptaqError(f"{name}: total: shape mismatch")
+    return total
+
+
+def gptaq_rms_norm(X: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None,
+                   total: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None):
+    """(Y, total): total = X + residual, Y = its root-mean-square norm times weight (None: ones).  Without a residual and without
+    `total`, total is None.  `total` may be the residual itself (in place)."""
+    total = _norm_args(X, weight, residual, total, "gptaq_rms_norm")
+    tokens, n = X.shape
+    Y = torch.empty(X.shape, dtype=torch.bfloat16, device=X.device) if out is None else out
+    _need(Y, torch.bfloat16, "out")
+    if Y.shape != X.shape:
+        raise GptaqError("gptaq_rms_norm: out: shape mismatch")
+    _check(load().gptaq_rms_norm(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, X.stride(0), residual.stride(0) if residual is not None else 0,
+                                 float(eps), _ptr(total), total.stride(0) if total is not None else 0, _ptr(Y), Y.stride(0), _stream()),
+           "gptaq_rms_norm")
+    return Y, total
+
+
+def gptaq_rms_norm_i8(X: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None,
+                      total: Optional[torch.Tensor] = None, clip: float = 1.0):
+    """(codes, scales, total): gptaq_rms_norm with its output as 8-bit codes and a scale per token."""
+    total = _norm_args(X, weight, residual, total, "gptaq_rms_norm_i8")
+    tokens, n = X.shape
+    codes = torch.empty((tokens, n), dtype=torch.int8, device=X.device)
+    scales = torch.empty(tokens, dtype=torch.float32, device=X.device)
+    _check(load().gptaq_rms_norm_i8(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, X.stride(0), residual.stride(0) if residual is not None else 0,
+                                    float(eps), _ptr(total), total.stride(0) if total is not None else 0, float(clip), _ptr(codes), n,
+                                    _ptr(scales), _stream()), "gptaq_rms_norm_i8")
+    return codes, scales, total
+
+
+def _gated_args(gate: torch.Tensor, up: torch.Tensor, name: str) -> None:
+    _need(gate, torch.bfloat16, "gate"); _need(up, torch.bfloat16, "up")
+    if gate.shape != up.shape:
+        raise GptaqError(f"{name}: shape mismatch")
+
+
+def gptaq_silu_mul(gate: torch.Tensor, up: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """silu(gate) * up in bf16; gate and up may be the two halves of one product's output."""
+    _gated_args(gate, up, "gptaq_silu_mul")
+    tokens, n = gate.shape
+    Y = torch.empty((tokens, n), dtype=torch.bfloat16, device=gate.device) if out is None else out
+    _need(Y, torch.bfloat16, "out")
+    if Y.shape != gate.shape:
+        raise GptaqError("gptaq_silu_mul: out: shape mismatch")
+    _check(load().gptaq_silu_mul(_ptr(gate), _ptr(up), tokens, n, gate.stride(0), up.stride(0), _ptr(Y), Y.stride(0), _stream()), "gptaq_silu_mul")
+    return Y
+
+
+def gptaq_silu_mul_i8(gate: torch.Tensor, up: torch.Tensor, clip: float = 1.0):
+    """(codes, scales): silu(gate) * up as 8-bit codes and a scale per token."""
+    _gated_args(gate, up, "gptaq_silu_mul_i8")
+    tokens, n = gate.shape
+    codes = torch.empty((tokens, n), dtype=torch.int8, device=gate.device)
+    scales = torch.empty(tokens, dtype=torch.float32, device=gate.device)
+    _check(load().gptaq_silu_mul_i8(_ptr(gate), _ptr(up), tokens, n, gate.stride(0), up.stride(0), float(clip), _ptr(codes), n, _ptr(scales),
+                                    _stream()), "gptaq_silu_mul_i8")
+    return codes, scales

@@ -1,0 +1,59 @@
+// Layout of a quantised layer's weights as the products read them (gptaq_linear_pack).
+#pragma once
+#include "common.h"
+
+namespace gptaq {
+
+// Codes lie in tiles of 16 rows by 128 columns, 1 KB each, the tiles of 16 rows one after the other.  A tile is four words for each
+// of 64 lanes: word i of lane l holds row l % 16, columns 32 i + 8 (l / 16) .. + 7, which is what the lane feeds to the i-th matrix
+// instruction of 32 columns; columns 0 .. 3 of the eight in the even nibbles, 4 .. 7 in the odd ones.  So a wavefront reads a tile
+// as one run of 16 bytes a lane.  Behind the codes: scales [tile row][group][16] in fp32, then zeros likewise, one byte each.
+// Rows are padded to 16 and columns to 128 with codes, scales and zeros of 0, so padding adds nothing.
+struct LinearLayout {
+  int64_t mt, kt, groups;              // tiles of rows, tiles of columns, groups (padded to whole column tiles; 1: one per row)
+  size_t scales, zeros, bytes;         // offsets of the scales and zeros, total size
+};
+// group: 32, 64, 128, or 0 for one group per row.
+inline LinearLayout linear_layout(int64_t m, int64_t n, int group) {
+  LinearLayout l;
+  l.mt = (m + 15) / 16;
+  l.kt = (n + 127) / 128;
+  l.groups = group > 0 ? l.kt * (128 / group) : 1;
+  l.scales = (size_t)(l.mt * l.kt) * 1024;
+  l.zeros = l.scales + (size_t)(l.mt * l.groups) * 64;
+  l.bytes = (l.zeros + (size_t)(l.mt * l.groups) * 16 + 255) / 256 * 256;
+  return l;
+}
+
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+// code - zero of the eight codes of a word as signed bytes: columns 0 .. 3, then 4 .. 7.  `z4` is the zero in all four bytes.
+// (Bit 7 keeps a byte's borrow from the next; flipping it makes the difference a signed byte.)
+__device__ __forceinline__ u32x2 linear_bytes(uint32_t w, uint32_t z4) {
+  u32x2 b;
+  b[0] = (((w & 0x0f0f0f0fu) | 0x80808080u) - z4) ^ 0x80808080u;
+  b[1] = ((((w >> 4) & 0x0f0f0f0fu) | 0x80808080u) - z4) ^ 0x80808080u;
+  return b;
+}
+// The same as bfloat16: integers of at most four bits and a sign, so the conversion is exact.
+__device__ __forceinline__ bf16x8 linear_bf16(uint32_t w, uint32_t z4) {
+  const u32x2 b = linear_bytes(w, z4);
+  bf16x8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (__bf16)(float)(int8_t)(b[i >> 2] >> (8 * (i & 3)));
+  return v;
+}
+
+struct LinearArgs {
+  const void* x;                       // tokens x n bf16, or int8 codes
+  const float* xs;                     // int8: a scale per token
+  int64_t ldx;
+  const uint8_t* codes; const float* scales; const uint8_t* zeros;
+  const float* bias;
+  void* y; int64_t ldy;
+  int32_t y_f32;
+  int32_t tokens, m, n;
+  int32_t mt, kt, groups;
+};
+
+}  // namespace gptaq
