@@ -56,4 +56,7 @@ struct LinearArgs {
   int32_t mt, kt, groups;
 };
 
+// linear_many.hip: rows of activations start at 16 bytes and have a multiple of 128 columns.
+hipError_t launch_linear_many(const LinearArgs& p, int gs, bool i8, hipStream_t s);
+
 }  // namespace gptaq

@@ -195,6 +195,7 @@ static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
 }
 
 static hipError_t launch_linear(const LinearArgs& p, int gs, bool i8, hipStream_t s) {
+  if (p.tokens > 128) return launch_linear_many(p, gs, i8, s);
   if (p.tokens <= 16) return i8 ? launch_few<true, 1, 1>(p, gs, s) : launch_few<false, 1, 1>(p, gs, s);
   return i8 ? launch_few<true, 4, 2>(p, gs, s) : launch_few<false, 4, 2>(p, gs, s);
 }
@@ -229,8 +230,8 @@ static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, i
   p.bias = bias; p.y = Y; p.ldy = ldy; p.y_f32 = y_f32 ? 1 : 0;
   p.tokens = (int32_t)tokens; p.m = (int32_t)m; p.n = (int32_t)n;
   p.mt = (int32_t)l.mt; p.kt = (int32_t)l.kt; p.groups = (int32_t)l.groups;
-  const int piece = i8 ? 16 : 8;
-  if (perm || n % piece || ldx % piece || ((uintptr_t)X & 15)) {
+  const int piece = tokens > 128 ? 128 : i8 ? 16 : 8;
+  if (perm || n % piece || ldx % (i8 ? 16 : 8) || ((uintptr_t)X & 15)) {
     const int64_t ld = padded_columns(n);
     if (i8) hipLaunchKernelGGL(linear_gather_kernel<int8_t>, dim3((unsigned)tokens), dim3(256), 0, s, (const int8_t*)X, ldx, perm, (int)n, (int8_t*)ws, ld);
     else hipLaunchKernelGGL(linear_gather_kernel<uint16_t>, dim3((unsigned)tokens), dim3(256), 0, s, (const uint16_t*)X, ldx, perm, (int)n, (uint16_t*)ws, ld);
