@@ -27,17 +27,18 @@ inline LinearLayout linear_layout(int64_t m, int64_t n, int group) {
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
-// code - zero of the eight codes of a word as signed bytes: columns 0 .. 3, then 4 .. 7.  `z4` is the zero in all four bytes.
-// (Bit 7 keeps a byte's borrow from the next; flipping it makes the difference a signed byte.)
-__device__ __forceinline__ u32x2 linear_bytes(uint32_t w, uint32_t z4) {
+// code - zero of the eight codes of a word as signed bytes: columns 0 .. 3, then 4 .. 7.  `off` is linear_offset(zero): the differences
+// are taken with 128 more in every byte, which keeps a byte's borrow from the next, and flipping bit 7 makes them signed.
+__device__ __forceinline__ uint32_t linear_offset(uint32_t zero) { return __builtin_amdgcn_perm(zero, zero, 0u) - 0x80808080u; }
+__device__ __forceinline__ u32x2 linear_bytes(uint32_t w, uint32_t off) {
   u32x2 b;
-  b[0] = (((w & 0x0f0f0f0fu) | 0x80808080u) - z4) ^ 0x80808080u;
-  b[1] = ((((w >> 4) & 0x0f0f0f0fu) | 0x80808080u) - z4) ^ 0x80808080u;
+  b[0] = ((w & 0x0f0f0f0fu) - off) ^ 0x80808080u;
+  b[1] = (((w >> 4) & 0x0f0f0f0fu) - off) ^ 0x80808080u;
   return b;
 }
 // The same as bfloat16: integers of at most four bits and a sign, so the conversion is exact.
-__device__ __forceinline__ bf16x8 linear_bf16(uint32_t w, uint32_t z4) {
-  const u32x2 b = linear_bytes(w, z4);
+__device__ __forceinline__ bf16x8 linear_bf16(uint32_t w, uint32_t off) {
+  const u32x2 b = linear_bytes(w, off);
   bf16x8 v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (__bf16)(float)(int8_t)(b[i >> 2] >> (8 * (i & 3)));
@@ -56,7 +57,41 @@ struct LinearArgs {
   int32_t mt, kt, groups;
 };
 
-// linear_many.hip: rows of activations start at 16 bytes and have a multiple of 128 columns.
+// Outputs row .. row + 7 of a token, as far as there are so many.  Rows of Y start at any element: global memory takes wide accesses at any address.
+typedef u32x4 __attribute__((aligned(2))) u32x4_at2;
+typedef u32x4 __attribute__((aligned(4))) u32x4_at4;
+__device__ __forceinline__ void linear_store(const LinearArgs& p, int tok, int row, const float (&v)[8]) {
+  const int64_t o = (int64_t)tok * p.ldy + row;
+  if (p.y_f32) {
+    float* y = (float*)p.y + o;
+    if (row + 8 <= p.m) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<u32x4_at4*>(y + 4 * h) = u32x4{__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]), __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (row + e < p.m) y[e] = v[e];
+    }
+  } else {
+    uint16_t* y = (uint16_t*)p.y + o;
+    u32x4 a;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      a[e] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * e]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * e + 1]) << 16;
+    if (row + 8 <= p.m) {
+      *reinterpret_cast<u32x4_at2*>(y) = a;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (row + e < p.m) y[e] = (uint16_t)(a[e >> 1] >> (16 * (e & 1)));
+    }
+  }
+}
+
+// linear_many.hip: rows of activations start at 16 bytes, have a multiple of 128 columns, and lie at most kManyMaxRow bytes apart (its
+// loads take 31 bits of offset inside 128 rows).
+constexpr int64_t kManyMaxRow = ((int64_t)1 << 24) - 16;
 hipError_t launch_linear_many(const LinearArgs& p, int gs, bool i8, hipStream_t s);
 
 }  // namespace gptaq

@@ -103,7 +103,7 @@ __global__ __launch_bounds__(512) void linear_few_kernel(LinearArgs p) {
   for (int k = wave; k < p.kt; k += waves) {
     u32x4 w[RT];
     float s[RT][G];
-    uint32_t z4[RT][G];
+    uint32_t off[RT][G];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       w[r] = *reinterpret_cast<const u32x4*>(p.codes + (tile_row[r] * p.kt + k) * 1024 + lane * 16);
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(512) void linear_few_kernel(LinearArgs p) {
       for (int g = 0; g < G; ++g) {
         const int64_t at = (tile_row[r] * p.groups + (GS ? k * GS + g : 0)) * 16 + l16;
         s[r][g] = p.scales[at];
-        z4[r][g] = p.zeros[at] * 0x01010101u;
+        off[r][g] = linear_offset(p.zeros[at]);
       }
     }
 #pragma unroll
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(512) void linear_few_kernel(LinearArgs p) {
       }
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const uint32_t z = z4[r][GS ? i * GS / 4 : 0];
+        const uint32_t z = off[r][GS ? i * GS / 4 : 0];
         if (I8) {
           const u32x2 b = linear_bytes(w[r][i], z);
 #pragma unroll
@@ -231,7 +231,7 @@ static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, i
   p.tokens = (int32_t)tokens; p.m = (int32_t)m; p.n = (int32_t)n;
   p.mt = (int32_t)l.mt; p.kt = (int32_t)l.kt; p.groups = (int32_t)l.groups;
   const int piece = tokens > 128 ? 128 : i8 ? 16 : 8;
-  if (perm || n % piece || ldx % (i8 ? 16 : 8) || ((uintptr_t)X & 15)) {
+  if (perm || n % piece || ldx % (i8 ? 16 : 8) || ((uintptr_t)X & 15) || (tokens > 128 && ldx * (i8 ? 1 : 2) > kManyMaxRow)) {
     const int64_t ld = padded_columns(n);
     if (i8) hipLaunchKernelGGL(linear_gather_kernel<int8_t>, dim3((unsigned)tokens), dim3(256), 0, s, (const int8_t*)X, ldx, perm, (int)n, (int8_t*)ws, ld);
     else hipLaunchKernelGGL(linear_gather_kernel<uint16_t>, dim3((unsigned)tokens), dim3(256), 0, s, (const uint16_t*)X, ldx, perm, (int)n, (uint16_t*)ws, ld);

@@ -6,16 +6,17 @@ namespace gptaq {
 typedef __attribute__((ext_vector_type(4))) int32_t i32x4;
 typedef __attribute__((ext_vector_type(16))) int32_t i32x16;
 
-// A workgroup of eight wavefronts takes 128 tokens x 256 rows of W; a wavefront 64 x 64 of it as 2 x 2 results of
+// A workgroup of eight wavefronts takes 128 tokens x 256 rows of W; a wavefront all the tokens and 32 rows, as four results of
 // v_mfma 32x32, twice: the sum of the current group of columns and the fp32 total it is scaled into.  These 128 registers a lane
-// are what limits the tile.  A byte of W feeds four times the products that a byte of bf16 activations does, so the tile is
-// taller in W: 24 KB come in for every 64 columns of bf16.
-// A stage is 128 bytes of each row (64 columns of bf16, 128 of int8): activations go from memory straight to LDS, codes to
-// registers, code - zero from there to LDS, once per workgroup.  Rings of three stages, one barrier a stage, in its middle: it
-// publishes the next stage (whose first fragments are read before the stage ends) and retires the one before.
-constexpr int kManyTokens = 128, kManyRows = 256;
-constexpr int kXStage = kManyTokens * 128, kWStage = kManyRows * 128, kRing = 3;
-constexpr int kManyLds = kRing * (kXStage + kWStage);
+// are what limits the tile.  The right operand of a matrix instruction is made of codes in the registers of the lanes that feed it:
+// the rows of W belong to one wavefront each, so every code is unpacked once per workgroup and W never passes through LDS.
+// A byte of W feeds four times the products that a byte of bf16 activations does, so the tile is taller in W.
+// Activations go from memory straight to LDS, 128 columns (a stage) at a time, in a ring of four stages with one barrier a stage, in
+// its middle: it publishes the next stage (whose first fragments are read before the stage ends) and retires the one before.
+constexpr int kManyTokens = 128, kManyRows = 256, kXRing = 4;
+constexpr int kOutRow = kManyRows + 4;                    // results in LDS: fp32, and 16 bytes so that tokens start at different banks
+constexpr int kManyLds = kManyTokens * kOutRow * 4;
+static_assert(kXRing * kManyTokens * 256 <= kManyLds, "the ring of bf16 stages");
 
 __device__ __forceinline__ void many_barrier() {          // no memory fence: loads stay in flight across it
   asm volatile("" ::: "memory");
@@ -27,225 +28,213 @@ template <int N> __device__ __forceinline__ void many_wait() {      // vmcnt <= 
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
+// 16 bytes a lane from base + lane offset + scalar offset to 1 KB of LDS
+struct LdsLoader {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ LdsLoader(const unsigned char* base) : rsrc(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00020000)) {}
+  __device__ __forceinline__ void load(unsigned char* to, int lane, int scalar) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, lane, scalar, 0, 0);
+  }
+};
+
 template <bool I8, int GS>
 __global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int token_tiles, int row_tiles) {
-  extern __shared__ __attribute__((aligned(128))) unsigned char smem[];
-  constexpr int NST = I8 ? 1 : 2;                       // stages per 128 columns
-  constexpr int WPS = I8 ? 4 : 2;                       // words of a tile per stage
-  constexpr int SPG = GS ? 4 * NST / GS : 0;            // steps (four a stage) per group
+  extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
+  constexpr int ST = I8 ? 4 : 8;                        // steps (matrix instructions along the columns) per stage
+  constexpr int SPG = GS ? ST / GS : ST;                // steps per group
   constexpr int NG = GS ? GS : 1;
+  constexpr int XROW = I8 ? 128 : 256, XSTAGE = kManyTokens * XROW, CHUNKS = XROW / 16;
+  constexpr int NL = XSTAGE / 8192;                     // loads of 1 KB per wavefront and stage
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15, q = lane >> 4;
-  const int tile_t = blockIdx.x % token_tiles, tile_r = blockIdx.x / token_tiles;
+  const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
+  // Workgroups go to the eight XCDs in turn: each gets one run of the list of tiles, and the list takes eight tiles of tokens against
+  // one tile of rows after the other, so that what an XCD works on at a time shares both operands in its L2.
+  const int total_tiles = token_tiles * row_tiles, xcd = blockIdx.x & 7;
+  const int at = xcd * (total_tiles >> 3) + min(xcd, total_tiles & 7) + (int)(blockIdx.x >> 3);
+  const int band = at / (8 * row_tiles), in_band = at - band * 8 * row_tiles, wide = min(8, token_tiles - band * 8);
+  const int tile_t = band * 8 + in_band % wide, tile_r = in_band / wide;
   const int tok0 = tile_t * kManyTokens, row0 = tile_r * kManyRows;
-  const int wt = (wave & 1) * 64, wr = (wave >> 1) * 64;
-  unsigned char* const xs_lds = smem + kRing * kWStage;
 
-  // ---- activations: the wavefront's 16 rows of a stage in two loads of 1 KB.  LDS rows are 128 bytes, their 16-byte chunks
-  // permuted so that 16 consecutive rows of one chunk lie in 16 different places of two rows' 256 bytes (all banks once).
-  const unsigned char* xsrc[2];
+  // ---- activations: the wavefront's 16 rows of a stage in NL loads.  The 16-byte chunks of a row are permuted so that 16
+  // consecutive rows of one chunk lie in 16 different places of 256 bytes (all banks once).
+  auto swizzle = [](int row) { return I8 ? (row >> 1) & 7 : row & 15; };
+  // (Buffer loads: behind a global load to LDS the compiler takes LDS reads to return in any order, and waits for all of them each time.)
+  const LdsLoader xfrom((const unsigned char*)p.x + (int64_t)tok0 * p.ldx * (I8 ? 1 : 2));
+  int xsrc[NL];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int row = wave * 16 + j * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
-    const int tok = tok0 + row < p.tokens ? tok0 + row : p.tokens - 1;         // (their results are not stored)
-    xsrc[j] = (const unsigned char*)p.x + (int64_t)tok * p.ldx * (I8 ? 1 : 2) + chunk * 16;
+  for (int j = 0; j < NL; ++j) {
+    const int row = wave * 16 + j * (1024 / XROW) + lane / CHUNKS, chunk = lane % CHUNKS ^ swizzle(row);
+    const int tok = tok0 + row < p.tokens ? row : p.tokens - 1 - tok0;         // (their results are not stored)
+    xsrc[j] = tok * (int)p.ldx * (I8 ? 1 : 2) + chunk * 16;
   }
-  const int nstage = p.kt * NST;
-  int xload = 0, xslot = 0;                             // next stage to load, its place
+  int xload = 0;                                        // next stage to load
   auto load_x = [&]() {
+    const int from = (xload < p.kt ? xload : p.kt - 1) * XROW;                 // (behind the last stage that again: the counts stay the same)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)xsrc[j],
-                                       (__attribute__((address_space(3))) void*)(xs_lds + xslot * kXStage + wave * 2048 + j * 1024), 16, 0, 0);
+    for (int j = 0; j < NL; ++j)
+      xfrom.load(smem + xload % kXRing * XSTAGE + wave * (16 * XROW) + j * 1024, xsrc[j], from);
     ++xload;
-    xslot = xslot == kRing - 1 ? 0 : xslot + 1;
-    const int step = xload < nstage ? 128 : 0;          // (behind the last stage it is loaded again, so that the counts stay the same)
-    xsrc[0] += step;
-    xsrc[1] += step;
+  };
+  const int foff = l32 * XROW + ((half ^ swizzle(l32)) << 4);
+  u32x4 xf[2][4];                                       // [step & 1][tile of 32 tokens]
+  auto read_x = [&](int stage, int s, int i) {
+    xf[s & 1][i] = *reinterpret_cast<const u32x4*>(smem + ((stage % kXRing * XSTAGE + foff) ^ (s << 5)) + i * 32 * XROW);
   };
 
-  // ---- weights: the wavefront unpacks two tiles of 16 rows
-  const uint8_t* csrc[2];
-  int64_t zat[2], sat[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    int tr = row0 / 16 + wave * 2 + j;
-    tr = tr < p.mt ? tr : p.mt - 1;
-    csrc[j] = p.codes + (int64_t)tr * p.kt * 1024 + lane * 16;
-    zat[j] = (int64_t)tr * p.groups * 16 + l16;
-    int sr = (row0 + wr + j * 32 + l32) / 16;           // the results' rows
-    sr = sr < p.mt ? sr : p.mt - 1;
-    sat[j] = (int64_t)sr * p.groups * 16 + l16;
-  }
-  struct Codes { u32x4 w[2]; uint32_t z[2][NG]; };
+  // ---- weights: lane l has row l % 32 of the wavefront's; of a tile's columns the pieces that its steps need (linear.h): bf16: word s / 2
+  // of piece s % 2 in step s; int8: word s of both
+  int tr = row0 / 16 + wave * 2 + (l32 >> 4);
+  tr = tr < p.mt ? tr : p.mt - 1;
+  const uint8_t* const codes = p.codes + (int64_t)tr * p.kt * 1024 + l16 * 16;
+  const int piece0 = (I8 ? 2 * half : half) * 256, piece1 = (I8 ? 2 * half + 1 : half + 2) * 256;
+  const int64_t group0 = (int64_t)tr * p.groups * 16 + l16;
+  struct Codes { u32x4 w[2]; uint32_t zero[NG]; float scale[NG]; };
   auto load_codes = [&](Codes& c, int k) {
     k = k < p.kt ? k : p.kt - 1;
+    c.w[0] = *reinterpret_cast<const u32x4*>(codes + (int64_t)k * 1024 + piece0);
+    c.w[1] = *reinterpret_cast<const u32x4*>(codes + (int64_t)k * 1024 + piece1);
+    if (GS) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      c.w[j] = *reinterpret_cast<const u32x4*>(csrc[j] + (int64_t)k * 1024);
-#pragma unroll
-      for (int g = 0; g < NG; ++g) c.z[j][g] = p.zeros[zat[j] + (GS ? (int64_t)(k * GS + g) * 16 : 0)];
+      for (int g = 0; g < NG; ++g) {
+        c.zero[g] = p.zeros[group0 + (int64_t)(k * GS + g) * 16];
+        c.scale[g] = p.scales[group0 + (int64_t)(k * GS + g) * 16];
+      }
     }
   };
-  const int wrow = wave * 32 + l16;                     // of the first tile; the second is 16 rows on
-  const int wswz = (l16 >> 1) & 7;
-  // word i of tile j to the stage at `slot`
-  auto unpack = [&](const Codes& c, int j, int i, int slot) {
-    const uint32_t z = c.z[j][GS ? i * GS / 4 : 0], z4 = __builtin_amdgcn_perm(z, z, 0u);
-    unsigned char* row = smem + slot * kWStage + (wrow + j * 16) * 128;
-    if (I8) {
-      *reinterpret_cast<u32x2*>(row + (((2 * i + (q >> 1)) ^ wswz) << 4) + (q & 1) * 8) = linear_bytes(c.w[j][i], z4);
+  uint32_t off = GS ? 0u : linear_offset(p.zeros[group0]);       // of the group being unpacked
+  u32x4 wf[2];                                          // [step & 1]
+  u32x2 bytes;
+  // Bytes 0, 1 or 2, 3 as bf16.  (Left to itself the compiler shifts the odd bytes down first.)
+  auto pair = [](uint32_t b, bool high) {
+    float f0, f1;
+    if (high) {
+      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f0) : "v"(b));
+      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f1) : "v"(b));
     } else {
-      *reinterpret_cast<u32x4*>(row + (((4 * (i & 1) + q) ^ wswz) << 4)) = __builtin_bit_cast(u32x4, linear_bf16(c.w[j][i], z4));
+      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f0) : "v"(b));
+      asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f1) : "v"(b));
+    }
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)f0, (__bf16)f1});
+  };
+  // step s's operand, in four parts
+  auto unpack = [&](const Codes& c, int s, int part) {
+    if (GS && s % SPG == 0 && part == 0) {
+      uint32_t z = c.zero[s / SPG];
+      asm volatile("" : "+v"(z));                       // (here, not right behind its load)
+      off = linear_offset(z);
+    }
+    if (I8) {
+      if (part < 2) {
+        const u32x2 b = linear_bytes(c.w[part][s], off);
+        wf[s & 1][2 * part] = b[0];
+        wf[s & 1][2 * part + 1] = b[1];
+      }
+    } else {
+      if (part == 0) bytes = linear_bytes(c.w[s & 1][s >> 1], off);
+      if (part == 1) { wf[s & 1][0] = pair(bytes[0], false); wf[s & 1][1] = pair(bytes[0], true); }
+      if (part == 2) { wf[s & 1][2] = pair(bytes[1], false); wf[s & 1][3] = pair(bytes[1], true); }
     }
   };
 
   // ---- products
-  f32x16 acc[2][2], total[2][2];                        // I8: acc holds the bits of int32
+  f32x16 acc[4], total[4];                              // I8: acc holds the bits of int32
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) { acc[i][j][e] = 0.f; total[i][j][e] = 0.f; }
-  int off[4];
-#pragma unroll
-  for (int s = 0; s < 4; ++s) off[s] = l32 * 128 + (((2 * s + half) ^ ((l32 >> 1) & 7)) << 4);
-  u32x4 xf[2][2], wf[2][2];                             // [set][tile]
-  auto read_frags = [&](int set, int s, int slot) {
-    const unsigned char* xb = xs_lds + slot * kXStage + wt * 128 + off[s];
-    const unsigned char* wb = smem + slot * kWStage + wr * 128 + off[s];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      xf[set][i] = *reinterpret_cast<const u32x4*>(xb + i * 4096);
-      wf[set][i] = *reinterpret_cast<const u32x4*>(wb + i * 4096);
-    }
-  };
-  auto add_scaled = [&](int i, int j, float s) {
+    for (int e = 0; e < 16; ++e) { acc[i][e] = 0.f; total[i][e] = 0.f; }
+  auto add_scaled = [&](int i, float s) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float v = I8 ? (float)__float_as_int(acc[i][j][e]) : acc[i][j][e];
-      total[i][j][e] = fmaf(s, v, total[i][j][e]);
+      const float v = I8 ? (float)__float_as_int(acc[i][e]) : acc[i][e];
+      total[i][e] = fmaf(s, v, total[i][e]);
     }
   };
-  auto product = [&](int set, int i, int j, bool first) {
+  auto product = [&](int s, int i, bool first) {
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const f32x16 c = first ? zero : acc[i][j];
+    const f32x16 c = first ? zero : acc[i];
     if (I8)
-      acc[i][j] = __builtin_bit_cast(f32x16, __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, xf[set][i]),
-                                     __builtin_bit_cast(i32x4, wf[set][j]), __builtin_bit_cast(i32x16, c), 0, 0, 0));
+      acc[i] = __builtin_bit_cast(f32x16, __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, xf[s & 1][i]),
+                                  __builtin_bit_cast(i32x4, wf[s & 1]), __builtin_bit_cast(i32x16, c), 0, 0, 0));
     else
-      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, xf[set][i]), __builtin_bit_cast(bf16x8, wf[set][j]), c, 0, 0, 0);
-  };
-  float s_old[2] = {0.f, 0.f}, s_cur[2][NG], s_next[2][NG];
-  auto load_scales = [&](float (&s)[2][NG], int k) {
-    k = k < p.kt ? k : p.kt - 1;
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int g = 0; g < NG; ++g) s[j][g] = p.scales[sat[j] + (GS ? (int64_t)(k * GS + g) * 16 : 0)];
+      acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, xf[s & 1][i]), __builtin_bit_cast(bf16x8, wf[s & 1]), c, 0, 0, 0);
   };
 
-  // ---- start: stages 0 and 1 unpacked and on their way
-  Codes cur, next;
-  load_codes(cur, 0);
-  load_codes(next, 1);
-  load_scales(s_cur, 0);
-  load_scales(s_next, 1);
+  // Behind each of a step's four matrix instructions: one fragment of the next step's activations, a part of its weights.  A group's sum goes
+  // to the total just before the first instruction of the next group replaces it.
+  float last_scale = 0.f;
+  auto stage = [&](Codes& c, Codes& next, int k) {
+#pragma unroll
+    for (int s = 0; s < ST; ++s) {
+      const bool first = GS && s % SPG == 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (first) add_scaled(i, s == 0 ? last_scale : c.scale[s == 0 ? 0 : s / SPG - 1]);
+        product(s, i, first);
+        __builtin_amdgcn_sched_barrier(0);
+        if (s + 1 < ST) { read_x(k, s + 1, i); unpack(c, s + 1, i); }
+        else { read_x(k + 1, 0, i); unpack(next, 0, i); }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (s == ST / 2 - 1) {
+        many_wait<NL>();                                // stage k + 1 is there: all but the youngest loads, those of stage k + 2
+        many_barrier();
+        load_x();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (GS) {
+      last_scale = c.scale[NG - 1];
+      asm volatile("" : "+v"(last_scale));              // (here, not behind the loads that replace it)
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_codes(c, k + 2);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  Codes ca, cb;
+  load_codes(ca, 0);
+  load_codes(cb, 1);
   __builtin_amdgcn_sched_barrier(0);
   load_x();
   load_x();
-  constexpr int kWords = 2 * WPS;                       // per stage: tile w / WPS, word w % WPS
+  load_x();
 #pragma unroll
-  for (int w = 0; w < kWords; ++w) unpack(cur, w / WPS, w % WPS, 0);
-  if (NST == 2) {
-#pragma unroll
-    for (int w = 0; w < kWords; ++w) unpack(cur, w / WPS, WPS * (NST - 1) + w % WPS, 1);
-  } else {
-#pragma unroll
-    for (int w = 0; w < kWords; ++w) unpack(next, w / WPS, w % WPS, 1);
-    load_codes(next, 2);
-  }
-  many_wait<0>();
+  for (int part = 0; part < 3; ++part) unpack(ca, 0, part);
+  many_wait<2 * NL>();
   many_barrier();
-  int slot = 0;
-  read_frags(0, 0, 0);
-  // Stage t = k * NST + h; behind its barrier stage t + 2 is unpacked (words 0 .. half of them in this stage, the rest in the next).
-  for (int k = 0; k < p.kt; ++k) {
 #pragma unroll
-    for (int h = 0; h < NST; ++h) {
-      const int slot1 = slot == kRing - 1 ? 0 : slot + 1, slot2 = slot1 == kRing - 1 ? 0 : slot1 + 1;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int set = s & 1;
-        const int gstep = h * 4 + s;                    // step in the 128 columns
-        if (s < 3) read_frags(set ^ 1, s + 1, slot);
-        else read_frags(set ^ 1, 0, slot1);
-        const bool first = GS ? gstep % (SPG ? SPG : 1) == 0 : false;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            if (first) add_scaled(i, j, gstep == 0 ? s_old[j] : s_cur[j][GS ? (gstep - 1) / (SPG ? SPG : 1) : 0]);
-            product(set, i, j, first);
-          }
-        // unpacking: steps 2, 3 the first half of stage t + 2, steps 0, 1 the second half of stage t + 1
-        constexpr int PER = kWords / 4;
-        if (s == 2) {
-          if (h == 0) { cur = next; load_codes(next, k + (I8 ? 3 : 2)); }
-        }
-        if (s >= 2) {
-#pragma unroll
-          for (int w = (s - 2) * PER; w < (s - 1) * PER; ++w) unpack(cur, w / WPS, (I8 ? 0 : WPS * h) + w % WPS, slot2);
-        } else {
-          // (the stage before this one began it, from the same registers)
-          const int hw = NST == 2 ? 1 - h : 0;
-          if (h != 0 || k != 0) {
-#pragma unroll
-            for (int w = (s + 2) * PER; w < (s + 3) * PER; ++w) unpack(cur, w / WPS, (I8 ? 0 : WPS * hw) + w % WPS, slot1);
-          }
-        }
-        if (s == 1) {
-          many_wait<0>();
-          many_barrier();
-          load_x();
-        }
-      }
-      slot = slot1;
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      s_old[j] = s_cur[j][NG - 1];
-#pragma unroll
-      for (int g = 0; g < NG; ++g) s_cur[j][g] = s_next[j][g];
-    }
-    load_scales(s_next, k + 2);
+  for (int i = 0; i < 4; ++i) read_x(0, 0, i);
+  int k = 0;
+  for (; k + 1 < p.kt; k += 2) {
+    stage(ca, cb, k);
+    stage(cb, ca, k + 1);
   }
+  if (k < p.kt) stage(ca, cb, k);
+  if (!GS) last_scale = p.scales[group0];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) add_scaled(i, j, GS ? s_old[j] : s_cur[j][0]);
+  for (int i = 0; i < 4; ++i) add_scaled(i, last_scale);
 
-  many_wait<0>();                                       // (nothing writes to LDS behind the workgroup's end)
-
-  // ---- results: the lane has row l32 of a tile, tokens 8 (e / 4) + 4 half + e % 4
+  // ---- results: through LDS, so that a token's outputs leave in runs.  The lane has row l32 of a tile, tokens 8 (e / 4) + 4 half + e % 4.
+  many_wait<0>();                                       // (no load writes to LDS from here on)
+  many_barrier();
+  float* out = reinterpret_cast<float*>(smem);
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int row = row0 + wr + j * 32 + l32;
-    const float b = p.bias && row < p.m ? p.bias[row] : 0.f;
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int e = 0; e < 16; ++e) out[(i * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * kOutRow + wave * 32 + l32] = total[i][e];
+  __syncthreads();
+  const int col = (tid & 31) * 8, row = row0 + col;
+  float b[8];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int tok = tok0 + wt + i * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-        if (row >= p.m || tok >= p.tokens) continue;
-        float v = total[i][j][e];
-        if (I8) v *= p.xs[tok];
-        v += b;
-        const int64_t o = (int64_t)tok * p.ldy + row;
-        if (p.y_f32) ((float*)p.y)[o] = v;
-        else ((uint16_t*)p.y)[o] = __builtin_bit_cast(uint16_t, (__bf16)v);
-      }
+  for (int e = 0; e < 8; ++e) b[e] = p.bias && row + e < p.m ? p.bias[row + e] : 0.f;
+  for (int t = tid >> 5; t < kManyTokens; t += 16) {
+    const int tok = tok0 + t;
+    if (tok >= p.tokens || row >= p.m) break;
+    const float sx = I8 ? p.xs[tok] : 1.f;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = I8 ? fmaf(out[t * kOutRow + col + e], sx, b[e]) : out[t * kOutRow + col + e] + b[e];
+    linear_store(p, tok, row, v);
   }
 }
 
