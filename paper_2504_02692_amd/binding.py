@@ -124,7 +124,13 @@ def _check(status: int, what: str) -> None:
         raise GptaqError(f"{what}: {msg} (status {status}, hip error {lib.gptaq_last_hip_error()})")
 
 
+# The handle alone: a stream object costs 3 us, as much as the launch of a kernel.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -491,6 +497,15 @@ def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWe
     return Y
 
 
+def _like(X: torch.Tensor, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
+    if out is None:
+        return torch.empty_like(X, memory_format=torch.contiguous_format)
+    _need(out, torch.bfloat16, "out")
+    if out.shape != X.shape:
+        raise GptaqError(f"{name}: out: shape mismatch")
+    return out
+
+
 def _norm_args(X: torch.Tensor, weight: Optional[torch.Tensor], residual: Optional[torch.Tensor], total: Optional[torch.Tensor], name: str):
     _need(X, torch.bfloat16, "X")
     if weight is not None:
@@ -502,7 +517,7 @@ def _norm_args(X: torch.Tensor, weight: Optional[torch.Tensor], residual: Option
         if residual.shape != X.shape:
             raise GptaqError(f"{name}: residual: shape mismatch")
         if total is None:
-            total = torch.empty(X.shape, dtype=torch.bfloat16, device=X.device)
+            return torch.empty_like(X, memory_format=torch.contiguous_format)
     if total is not None:
         _need(total, torch.bfloat16, "total")
         if total.shape != X.shape:
@@ -516,10 +531,7 @@ def gptaq_rms_norm(X: torch.Tensor, weight: Optional[torch.Tensor], eps: float, 
     `total`, total is None.  `total` may be the residual itself (in place)."""
     total = _norm_args(X, weight, residual, total, "gptaq_rms_norm")
     tokens, n = X.shape
-    Y = torch.empty(X.shape, dtype=torch.bfloat16, device=X.device) if out is None else out
-    _need(Y, torch.bfloat16, "out")
-    if Y.shape != X.shape:
-        raise GptaqError("gptaq_rms_norm: out: shape mismatch")
+    Y = _like(X, out, "gptaq_rms_norm")
     _check(load().gptaq_rms_norm(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, X.stride(0), residual.stride(0) if residual is not None else 0,
                                  float(eps), _ptr(total), total.stride(0) if total is not None else 0, _ptr(Y), Y.stride(0), _stream()),
            "gptaq_rms_norm")
@@ -549,10 +561,7 @@ def gptaq_silu_mul(gate: torch.Tensor, up: torch.Tensor, out: Optional[torch.Ten
     """silu(gate) * up in bf16; gate and up may be the two halves of one product's output."""
     _gated_args(gate, up, "gptaq_silu_mul")
     tokens, n = gate.shape
-    Y = torch.empty((tokens, n), dtype=torch.bfloat16, device=gate.device) if out is None else out
-    _need(Y, torch.bfloat16, "out")
-    if Y.shape != gate.shape:
-        raise GptaqError("gptaq_silu_mul: out: shape mismatch")
+    Y = _like(gate, out, "gptaq_silu_mul")
     _check(load().gptaq_silu_mul(_ptr(gate), _ptr(up), tokens, n, gate.stride(0), up.stride(0), _ptr(Y), Y.stride(0), _stream()), "gptaq_silu_mul")
     return Y
 
