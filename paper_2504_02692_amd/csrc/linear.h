@@ -55,6 +55,8 @@ struct LinearArgs {
   int32_t y_f32;
   int32_t tokens, m, n;
   int32_t mt, kt, groups;
+  int32_t parts;                       // linear_many.hip: the columns in so many parts, whose sums (more than one) go to
+  float* partial; int64_t ld_partial;  // partial[part][token][row]
 };
 
 // Outputs row .. row + 7 of a token, as far as there are so many.  Rows of Y start at any element: global memory takes wide accesses at any address.
@@ -92,6 +94,7 @@ __device__ __forceinline__ void linear_store(const LinearArgs& p, int tok, int r
 // linear_many.hip: rows of activations start at 16 bytes, have a multiple of 128 columns, and lie at most kManyMaxRow bytes apart (its
 // loads take 31 bits of offset inside 128 rows).
 constexpr int64_t kManyMaxRow = ((int64_t)1 << 24) - 16;
-hipError_t launch_linear_many(const LinearArgs& p, int gs, bool i8, hipStream_t s);
+hipError_t launch_linear_many(LinearArgs p, int gs, bool i8, float* partial, hipStream_t s);
+size_t linear_partial_bytes(int64_t tokens, int64_t m, int64_t n);
 
 }  // namespace gptaq

@@ -66,115 +66,112 @@ __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t 
 
 // ---- few tokens
 //
-// A workgroup takes RT tiles of 16 rows and TT of 16 tokens; its wavefronts share the tiles of 128 columns out among themselves and
-// add their sums through LDS, in the wavefronts' order.  The weights go straight from memory to the lanes that feed the matrix
-// unit: nothing is read twice, and with all of a wavefront's tiles independent many loads are in flight.  v_mfma 16x16: the left
-// operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the result has the row of W in l % 16
-// and tokens 4 (l / 16) .. + 3 in the lane's four values, so one scale per lane serves a result.
+// Up to 16 tokens, one tile of v_mfma 16x16.  A workgroup takes RT tiles of 16 rows; its wavefronts share the tiles of 128 columns out
+// among themselves and add their sums through LDS, in the wavefronts' order.  The weights go straight from memory to the lanes that
+// feed the matrix unit, two tiles of columns ahead: nothing of W is read twice, and with everything of a wavefront independent many
+// loads are in flight.  The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the result has the
+// row of W in l % 16 and tokens 4 (l / 16) .. + 3 in the lane's four values, so one scale per lane serves a result.
 // GS: groups per 128 columns (1, 2, 4), 0: one group per row.
-template <bool I8, int GS, int TT, int RT>
-__global__ __launch_bounds__(512) void linear_few_kernel(LinearArgs p) {
+template <bool I8, int GS, int RT>
+__global__ __launch_bounds__(RT == 1 ? 1024 : 512) void linear_few_kernel(LinearArgs p) {
   extern __shared__ float lds[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int l16 = lane & 15, q = lane >> 4;
-  const int row_blocks = (p.mt + RT - 1) / RT;
-  const int rb = blockIdx.x % row_blocks, tb = blockIdx.x / row_blocks;
-  const int rt0 = rb * RT, tok0 = tb * TT * 16;
-
-  f32x4 total[TT][RT];
-  f32x4 acc[TT][RT];                   // I8: the bits of int32
-#pragma unroll
-  for (int t = 0; t < TT; ++t)
-#pragma unroll
-    for (int r = 0; r < RT; ++r) { total[t][r] = f32x4{0.f, 0.f, 0.f, 0.f}; acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f}; }
-
-  int64_t tile_row[RT];                // (past the last tile of rows: that one again; nothing of it is stored)
-#pragma unroll
-  for (int r = 0; r < RT; ++r) tile_row[r] = rt0 + r < p.mt ? rt0 + r : p.mt - 1;
-  auto add_scaled = [&](int t, int r, float s) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float v = I8 ? (float)__float_as_int(acc[t][r][e]) : acc[t][r][e];
-      total[t][r][e] = fmaf(s, v, total[t][r][e]);
-    }
-    acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-  };
+  const int rt0 = blockIdx.x * RT;
   constexpr int G = GS ? GS : 1;       // groups per tile of 128 columns
-  for (int k = wave; k < p.kt; k += waves) {
-    u32x4 w[RT];
-    float s[RT][G];
-    uint32_t off[RT][G];
+
+  f32x4 total[RT], acc[RT];            // I8: acc holds the bits of int32
+  const uint8_t* codes[RT];
+  int64_t group[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    total[r] = acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int64_t tr = rt0 + r < p.mt ? rt0 + r : p.mt - 1;      // (past the last tile of rows: that one again; nothing of it is stored)
+    codes[r] = p.codes + tr * p.kt * 1024 + lane * 16;
+    group[r] = tr * p.groups * 16 + l16;
+  }
+  const bool here = l16 < p.tokens;
+  const uint8_t* x0 = (const uint8_t*)p.x + ((int64_t)(here ? l16 : 0) * p.ldx + q * 8) * (I8 ? 1 : 2);
+
+  struct Stage { u32x4 w[RT]; uint32_t zero[RT][G]; float scale[RT][G]; u32x4 x[4]; };
+  auto load = [&](Stage& s, int k) {
+    if (k >= p.kt) return;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      w[r] = *reinterpret_cast<const u32x4*>(p.codes + (tile_row[r] * p.kt + k) * 1024 + lane * 16);
+      s.w[r] = *reinterpret_cast<const u32x4*>(codes[r] + (int64_t)k * 1024);
+      if (GS) {
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        const int64_t at = (tile_row[r] * p.groups + (GS ? k * GS + g : 0)) * 16 + l16;
-        s[r][g] = p.scales[at];
-        off[r][g] = linear_offset(p.zeros[at]);
+        for (int g = 0; g < G; ++g) {
+          s.zero[r][g] = p.zeros[group[r] + (int64_t)(k * GS + g) * 16];
+          s.scale[r][g] = p.scales[group[r] + (int64_t)(k * GS + g) * 16];
+        }
       }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int col = k * 128 + i * 32 + q * 8;
-      u32x4 x[TT];                     // I8: two words
-#pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        const int tok = tok0 + t * 16 + l16;
-        x[t] = u32x4{0u, 0u, 0u, 0u};
-        if (tok < p.tokens && col < p.n) {
-          if (I8) {
-            const u32x2 v = *reinterpret_cast<const u32x2*>((const int8_t*)p.x + (int64_t)tok * p.ldx + col);
-            x[t][0] = v[0]; x[t][1] = v[1];
-          } else {
-            x[t] = *reinterpret_cast<const u32x4*>((const uint16_t*)p.x + (int64_t)tok * p.ldx + col);
-          }
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        const uint32_t z = off[r][GS ? i * GS / 4 : 0];
+      const int col = k * 128 + i * 32;
+      s.x[i] = u32x4{0u, 0u, 0u, 0u};
+      if (here && col + q * 8 < p.n) {
         if (I8) {
-          const u32x2 b = linear_bytes(w[r][i], z);
-#pragma unroll
-          for (int t = 0; t < TT; ++t)
-            acc[t][r] = __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x32_i8(
-                __builtin_bit_cast(long, u32x2{x[t][0], x[t][1]}), __builtin_bit_cast(long, b), __builtin_bit_cast(i32x4, acc[t][r]), 0, 0, 0));
+          const u32x2 v = *reinterpret_cast<const u32x2*>(x0 + col);
+          s.x[i][0] = v[0]; s.x[i][1] = v[1];
         } else {
-          const bf16x8 b = linear_bf16(w[r][i], z);
-#pragma unroll
-          for (int t = 0; t < TT; ++t)
-            acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), b, acc[t][r], 0, 0, 0);
-        }
-        if (GS && (i + 1) % (4 / G) == 0) {
-#pragma unroll
-          for (int t = 0; t < TT; ++t) add_scaled(t, r, s[r][i * G / 4]);
+          s.x[i] = *reinterpret_cast<const u32x4*>(x0 + 2 * col);
         }
       }
     }
+  };
+  auto add_scaled = [&](int r, float s) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) total[r][e] = fmaf(s, I8 ? (float)__float_as_int(acc[r][e]) : acc[r][e], total[r][e]);
+  };
+  uint32_t row_off[RT];
+  if (!GS) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) row_off[r] = linear_offset(p.zeros[group[r]]);
+  }
+  auto multiply = [&](const Stage& s) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t off = GS ? linear_offset(s.zero[r][i * G / 4]) : row_off[r];
+        const f32x4 c = GS && i % (4 / G) == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[r];
+        if (I8)
+          acc[r] = __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x32_i8(
+              __builtin_bit_cast(long, u32x2{s.x[i][0], s.x[i][1]}), __builtin_bit_cast(long, linear_bytes(s.w[r][i], off)),
+              __builtin_bit_cast(i32x4, c), 0, 0, 0));
+        else
+          acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, s.x[i]), linear_bf16(s.w[r][i], off), c, 0, 0, 0);
+        if (GS && (i + 1) % (4 / G) == 0) add_scaled(r, s.scale[r][i * G / 4]);
+      }
+    }
+  };
+  Stage a, b;
+  load(a, wave);
+  load(b, wave + waves);
+  for (int k = wave; k < p.kt; k += 2 * waves) {
+    multiply(a);
+    load(a, k + 2 * waves);
+    if (k + waves >= p.kt) break;
+    multiply(b);
+    load(b, k + 3 * waves);
   }
   if (!GS) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const float s = p.scales[tile_row[r] * 16 + l16];
-#pragma unroll
-      for (int t = 0; t < TT; ++t) add_scaled(t, r, s);
-    }
+    for (int r = 0; r < RT; ++r) add_scaled(r, p.scales[group[r]]);
   }
-  // [wave][t][r][lane][4]
+  // [wave][r][lane][4]
 #pragma unroll
-  for (int t = 0; t < TT; ++t)
-#pragma unroll
-    for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(&lds[(((wave * TT + t) * RT + r) * 64 + lane) * 4]) = total[t][r];
+  for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(&lds[((wave * RT + r) * 64 + lane) * 4]) = total[r];
   __syncthreads();
-  for (int at = threadIdx.x; at < TT * RT * 256; at += blockDim.x) {
-    // 16 rows of W in a run of threads, so that a token's outputs are written together
-    const int r = at & 15, rt = at / 16 % RT, tok_in = at / (16 * RT);
-    const int t = tok_in >> 4, row = (rt0 + rt) * 16 + r, tok = tok0 + tok_in;
-    if (rt0 + rt >= p.mt || row >= p.m || tok >= p.tokens) continue;
-    const int slot = ((t * RT + rt) * 64 + (tok_in & 15) / 4 * 16 + r) * 4 + (tok_in & 3);
+  for (int at = threadIdx.x; at < RT * 256; at += blockDim.x) {
+    // 16 RT rows of W in a run of threads, so that a token's outputs are written together
+    const int r = at % (16 * RT), tok = at / (16 * RT), row = rt0 * 16 + r;
+    if (row >= p.m || tok >= p.tokens) continue;
+    const int slot = ((r >> 4) * 64 + (tok >> 2) * 16 + (r & 15)) * 4 + (tok & 3);
     float v = 0.f;
-    for (int w = 0; w < waves; ++w) v += lds[w * TT * RT * 256 + slot];
+    for (int w = 0; w < waves; ++w) v += lds[w * RT * 256 + slot];
     if (I8) v *= p.xs[tok];
     if (p.bias) v += p.bias[row];
     const int64_t o = (int64_t)tok * p.ldy + row;
@@ -183,21 +180,31 @@ __global__ __launch_bounds__(512) void linear_few_kernel(LinearArgs p) {
   }
 }
 
-template <bool I8, int TT, int RT>
-static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
-  int waves = 8;
-  while (waves > 1 && waves > p.kt) waves /= 2;
-  const int64_t blocks = (int64_t)((p.mt + RT - 1) / RT) * ((p.tokens + TT * 16 - 1) / (TT * 16));
-  const auto kernel = gs == 0 ? &linear_few_kernel<I8, 0, TT, RT> : gs == 1 ? &linear_few_kernel<I8, 1, TT, RT>
-                    : gs == 2 ? &linear_few_kernel<I8, 2, TT, RT> : &linear_few_kernel<I8, 4, TT, RT>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * waves), (size_t)waves * TT * RT * 1024, s, p);
+template <bool I8, int RT>
+static hipError_t launch_few_as(const LinearArgs& p, int gs, int waves, hipStream_t s) {
+  const auto kernel = gs == 0 ? &linear_few_kernel<I8, 0, RT> : gs == 1 ? &linear_few_kernel<I8, 1, RT>
+                    : gs == 2 ? &linear_few_kernel<I8, 2, RT> : &linear_few_kernel<I8, RT == 4 ? 2 : 4, RT>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.mt + RT - 1) / RT)), dim3(64 * waves), (size_t)waves * RT * 1024, s, p);
   return hipGetLastError();
 }
+// Tiles of rows per workgroup: the more, the less often the activations are read, the fewer workgroups.  us a call, 1 token, RT 1 / 2 / 4:
+// 4096 x 4096 5.1 / 7.4 / 10.3, 11008 x 4096 10.7 / 11.3 / 11.5, 28672 x 8192 43.2 / 38.3 / 40.9; 16 tokens 6.7 / 8.4 / 11.8, 15.2 / 13.7 / 12.5,
+// 60.8 / 45.7 / 42.3.  (With four groups to 128 columns, four tiles of rows have more scales than registers.)
+// Wavefronts, RT 1, 8 / 16: 4096 x 11008 11.3 / 9.3, 1024 x 8192 7.1 / 6.6, 11008 x 4096 10.7 / 11.7.  RT 4, 4 / 8: 28672 x 8192, 16 tokens 40.2 / 42.3,
+// 11008 x 4096 15.0 / 12.5.
+template <bool I8>
+static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
+  const int rt = p.tokens > 8 ? (p.mt >= 512 ? (gs == 4 ? 2 : 4) : 1) : p.mt >= 1024 ? 2 : 1;
+  int waves = rt == 1 ? (p.mt < 512 ? 16 : 8) : rt == 4 && p.mt >= 1024 ? 4 : 8;
+  while (waves > 1 && waves > p.kt) waves /= 2;
+  if (rt == 4) return launch_few_as<I8, 4>(p, gs, waves, s);
+  if (rt == 2) return launch_few_as<I8, 2>(p, gs, waves, s);
+  return launch_few_as<I8, 1>(p, gs, waves, s);
+}
 
-static hipError_t launch_linear(const LinearArgs& p, int gs, bool i8, hipStream_t s) {
-  if (p.tokens > 128) return launch_linear_many(p, gs, i8, s);
-  if (p.tokens <= 16) return i8 ? launch_few<true, 1, 1>(p, gs, s) : launch_few<false, 1, 1>(p, gs, s);
-  return i8 ? launch_few<true, 4, 2>(p, gs, s) : launch_few<false, 4, 2>(p, gs, s);
+static hipError_t launch_linear(const LinearArgs& p, int gs, bool i8, float* partial, hipStream_t s) {
+  if (p.tokens > 16) return launch_linear_many(p, gs, i8, partial, s);
+  return i8 ? launch_few<true>(p, gs, s) : launch_few<false>(p, gs, s);
 }
 
 // ---- argument checks
@@ -208,6 +215,8 @@ static bool good_group(int64_t n, int group) {
 }
 // Elements of a row of activations in the workspace: whole tiles of columns.
 static int64_t padded_columns(int64_t n) { return (n + 127) / 128 * 128; }
+
+static size_t gather_bytes(int64_t tokens, int64_t n) { return ((size_t)tokens * padded_columns(n) * 2 + 255) / 256 * 256; }
 
 static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights, int64_t m,
                       int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes, void* stream) {
@@ -230,8 +239,8 @@ static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, i
   p.bias = bias; p.y = Y; p.ldy = ldy; p.y_f32 = y_f32 ? 1 : 0;
   p.tokens = (int32_t)tokens; p.m = (int32_t)m; p.n = (int32_t)n;
   p.mt = (int32_t)l.mt; p.kt = (int32_t)l.kt; p.groups = (int32_t)l.groups;
-  const int piece = tokens > 128 ? 128 : i8 ? 16 : 8;
-  if (perm || n % piece || ldx % (i8 ? 16 : 8) || ((uintptr_t)X & 15) || (tokens > 128 && ldx * (i8 ? 1 : 2) > kManyMaxRow)) {
+  const int piece = tokens > 16 ? 128 : i8 ? 16 : 8;
+  if (perm || n % piece || ldx % (i8 ? 16 : 8) || ((uintptr_t)X & 15) || (tokens > 16 && ldx * (i8 ? 1 : 2) > kManyMaxRow)) {
     const int64_t ld = padded_columns(n);
     if (i8) hipLaunchKernelGGL(linear_gather_kernel<int8_t>, dim3((unsigned)tokens), dim3(256), 0, s, (const int8_t*)X, ldx, perm, (int)n, (int8_t*)ws, ld);
     else hipLaunchKernelGGL(linear_gather_kernel<uint16_t>, dim3((unsigned)tokens), dim3(256), 0, s, (const uint16_t*)X, ldx, perm, (int)n, (uint16_t*)ws, ld);
@@ -239,6 +248,7 @@ static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, i
     p.x = ws; p.ldx = ld;
     p.n = (int32_t)ld;                 // (the columns behind n are zeros here)
   }
+  float* const partial = (float*)((uint8_t*)ws + gather_bytes(tokens, n));
   // A grid has less than 2^32 threads: more tokens than that takes are several launches.
   const int64_t most = (((int64_t)1 << 22) / p.mt) * 64;
   for (int64_t first = 0; first < tokens; first += most) {
@@ -247,7 +257,7 @@ static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, i
     part.x = (const uint8_t*)p.x + first * p.ldx * (i8 ? 1 : 2);
     part.y = (uint8_t*)p.y + first * p.ldy * (y_f32 ? 4 : 2);
     if (i8) part.xs = p.xs + first;
-    if (const hipError_t e = launch_linear(part, group ? 128 / group : 0, i8, s); e != hipSuccess) { set_last_hip_error(e); return GPTAQ_ELAUNCH; }
+    if (const hipError_t e = launch_linear(part, group ? 128 / group : 0, i8, partial, s); e != hipSuccess) { set_last_hip_error(e); return GPTAQ_ELAUNCH; }
   }
   return GPTAQ_OK;
 }
@@ -284,7 +294,7 @@ extern "C" int gptaq_linear_pack(const uint8_t* codes, int64_t ldc, const float*
 
 extern "C" size_t gptaq_linear_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
   if (tokens <= 0 || tokens > kMaxTokens || m <= 0 || n <= 0 || m > kMaxSide || n > kMaxSide) return 0;
-  return ((size_t)tokens * padded_columns(n) * 2 + 255) / 256 * 256;
+  return gather_bytes(tokens, n) + (linear_partial_bytes(tokens, m, n) + 255) / 256 * 256;
 }
 
 extern "C" int gptaq_linear(const uint16_t* X, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights, int64_t m, int64_t n,

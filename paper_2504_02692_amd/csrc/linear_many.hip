@@ -13,10 +13,16 @@ typedef __attribute__((ext_vector_type(16))) int32_t i32x16;
 // A byte of W feeds four times the products that a byte of bf16 activations does, so the tile is taller in W.
 // Activations go from memory straight to LDS, 128 columns (a stage) at a time, in a ring of four stages with one barrier a stage, in
 // its middle: it publishes the next stage (whose first fragments are read before the stage ends) and retires the one before.
-constexpr int kManyTokens = 128, kManyRows = 256, kXRing = 4;
-constexpr int kOutRow = kManyRows + 4;                    // results in LDS: fp32, and 16 bytes so that tokens start at different banks
-constexpr int kManyLds = kManyTokens * kOutRow * 4;
-static_assert(kXRing * kManyTokens * 256 <= kManyLds, "the ring of bf16 stages");
+// TT tiles of 32 tokens (4, or 1 and 2 where there are no more tokens) and WV wavefronts; with fewer tokens than 128 several workgroups
+// share a CU.  A result that too few workgroups would share is taken in parts of the columns, each by workgroups of its own: their sums
+// go to p.partial, and linear_join_kernel adds them in order.
+constexpr int kXRing = 4;
+template <int TT, int WV> struct ManyTile {
+  static constexpr int kTokens = 32 * TT, kRows = 32 * WV;
+  static constexpr int kOutRow = kRows + 4;               // results in LDS: fp32, and 16 bytes so that tokens start at different banks
+  static constexpr int kRingBytes = kXRing * kTokens * 256, kOutBytes = kTokens * kOutRow * 4;
+  static constexpr int kLds = kRingBytes > kOutBytes ? kRingBytes : kOutBytes;
+};
 
 __device__ __forceinline__ void many_barrier() {          // no memory fence: loads stay in flight across it
   asm volatile("" ::: "memory");
@@ -37,25 +43,28 @@ struct LdsLoader {
   }
 };
 
-template <bool I8, int GS>
-__global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int token_tiles, int row_tiles) {
+template <bool I8, int GS, int TT, int WV>
+__global__ __launch_bounds__(64 * WV, 2) void linear_many_kernel(LinearArgs p, int token_tiles, int row_tiles) {
+  using Tile = ManyTile<TT, WV>;
   extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
   constexpr int ST = I8 ? 4 : 8;                        // steps (matrix instructions along the columns) per stage
-  constexpr int SPG = GS ? ST / GS : ST;                // steps per group
+  constexpr int SPG = GS ? ST / (GS ? GS : 1) : ST;                // steps per group
   constexpr int NG = GS ? GS : 1;
-  constexpr int XROW = I8 ? 128 : 256, XSTAGE = kManyTokens * XROW, CHUNKS = XROW / 16;
-  constexpr int NL = XSTAGE / 8192;                     // loads of 1 KB per wavefront and stage
+  constexpr int XROW = I8 ? 128 : 256, XSTAGE = Tile::kTokens * XROW, CHUNKS = XROW / 16;
+  constexpr int NL = XSTAGE / (1024 * WV);              // loads of 1 KB per wavefront and stage
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
   // Workgroups go to the eight XCDs in turn: each gets one run of the list of tiles, and the list takes eight tiles of tokens against
   // one tile of rows after the other, so that what an XCD works on at a time shares both operands in its L2.
-  const int total_tiles = token_tiles * row_tiles, xcd = blockIdx.x & 7;
-  const int at = xcd * (total_tiles >> 3) + min(xcd, total_tiles & 7) + (int)(blockIdx.x >> 3);
+  const int grid = gridDim.x, xcd = blockIdx.x & 7, tiles = token_tiles * row_tiles;
+  const int of_list = xcd * (grid >> 3) + min(xcd, grid & 7) + (int)(blockIdx.x >> 3);
+  const int part = of_list / tiles, at = of_list - part * tiles;
   const int band = at / (8 * row_tiles), in_band = at - band * 8 * row_tiles, wide = min(8, token_tiles - band * 8);
   const int tile_t = band * 8 + in_band % wide, tile_r = in_band / wide;
-  const int tok0 = tile_t * kManyTokens, row0 = tile_r * kManyRows;
+  const int tok0 = tile_t * Tile::kTokens, row0 = tile_r * Tile::kRows;
+  const int k_begin = (int)((int64_t)p.kt * part / p.parts), k_end = (int)((int64_t)p.kt * (part + 1) / p.parts);   // stages of this part
 
-  // ---- activations: the wavefront's 16 rows of a stage in NL loads.  The 16-byte chunks of a row are permuted so that 16
+  // ---- activations: the wavefront's share of a stage's rows in NL loads.  The 16-byte chunks of a row are permuted so that 16
   // consecutive rows of one chunk lie in 16 different places of 256 bytes (all banks once).
   auto swizzle = [](int row) { return I8 ? (row >> 1) & 7 : row & 15; };
   // (Buffer loads: behind a global load to LDS the compiler takes LDS reads to return in any order, and waits for all of them each time.)
@@ -63,20 +72,20 @@ __global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int t
   int xsrc[NL];
 #pragma unroll
   for (int j = 0; j < NL; ++j) {
-    const int row = wave * 16 + j * (1024 / XROW) + lane / CHUNKS, chunk = lane % CHUNKS ^ swizzle(row);
+    const int row = (wave * NL + j) * (1024 / XROW) + lane / CHUNKS, chunk = lane % CHUNKS ^ swizzle(row);
     const int tok = tok0 + row < p.tokens ? row : p.tokens - 1 - tok0;         // (their results are not stored)
     xsrc[j] = tok * (int)p.ldx * (I8 ? 1 : 2) + chunk * 16;
   }
-  int xload = 0;                                        // next stage to load
+  int xload = k_begin;                                  // next stage to load
   auto load_x = [&]() {
-    const int from = (xload < p.kt ? xload : p.kt - 1) * XROW;                 // (behind the last stage that again: the counts stay the same)
+    const int from = (xload < k_end ? xload : k_end - 1) * XROW;                 // (behind the last stage that again: the counts stay the same)
 #pragma unroll
     for (int j = 0; j < NL; ++j)
-      xfrom.load(smem + xload % kXRing * XSTAGE + wave * (16 * XROW) + j * 1024, xsrc[j], from);
+      xfrom.load(smem + xload % kXRing * XSTAGE + (wave * NL + j) * 1024, xsrc[j], from);
     ++xload;
   };
   const int foff = l32 * XROW + ((half ^ swizzle(l32)) << 4);
-  u32x4 xf[2][4];                                       // [step & 1][tile of 32 tokens]
+  u32x4 xf[2][TT];                                      // [step & 1][tile of 32 tokens]
   auto read_x = [&](int stage, int s, int i) {
     xf[s & 1][i] = *reinterpret_cast<const u32x4*>(smem + ((stage % kXRing * XSTAGE + foff) ^ (s << 5)) + i * 32 * XROW);
   };
@@ -90,7 +99,7 @@ __global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int t
   const int64_t group0 = (int64_t)tr * p.groups * 16 + l16;
   struct Codes { u32x4 w[2]; uint32_t zero[NG]; float scale[NG]; };
   auto load_codes = [&](Codes& c, int k) {
-    k = k < p.kt ? k : p.kt - 1;
+    k = k < k_end ? k : k_end - 1;
     c.w[0] = *reinterpret_cast<const u32x4*>(codes + (int64_t)k * 1024 + piece0);
     c.w[1] = *reinterpret_cast<const u32x4*>(codes + (int64_t)k * 1024 + piece1);
     if (GS) {
@@ -138,9 +147,9 @@ __global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int t
   };
 
   // ---- products
-  f32x16 acc[4], total[4];                              // I8: acc holds the bits of int32
+  f32x16 acc[TT], total[TT];                            // I8: acc holds the bits of int32
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < TT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) { acc[i][e] = 0.f; total[i][e] = 0.f; }
   auto add_scaled = [&](int i, float s) {
@@ -160,7 +169,7 @@ __global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int t
       acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, xf[s & 1][i]), __builtin_bit_cast(bf16x8, wf[s & 1]), c, 0, 0, 0);
   };
 
-  // Behind each of a step's four matrix instructions: one fragment of the next step's activations, a part of its weights.  A group's sum goes
+  // Behind each of a step's matrix instructions: one fragment of the next step's activations, a share of its weights.  A group's sum goes
   // to the total just before the first instruction of the next group replaces it.
   float last_scale = 0.f;
   auto stage = [&](Codes& c, Codes& next, int k) {
@@ -168,12 +177,17 @@ __global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int t
     for (int s = 0; s < ST; ++s) {
       const bool first = GS && s % SPG == 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < TT; ++i) {
         if (first) add_scaled(i, s == 0 ? last_scale : c.scale[s == 0 ? 0 : s / SPG - 1]);
         product(s, i, first);
         __builtin_amdgcn_sched_barrier(0);
-        if (s + 1 < ST) { read_x(k, s + 1, i); unpack(c, s + 1, i); }
-        else { read_x(k + 1, 0, i); unpack(next, 0, i); }
+        if (s + 1 < ST) read_x(k, s + 1, i);
+        else read_x(k + 1, 0, i);
+#pragma unroll
+        for (int part = i * (4 / TT); part < (i + 1) * (4 / TT); ++part) {
+          if (s + 1 < ST) unpack(c, s + 1, part);
+          else unpack(next, 0, part);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
       if (s == ST / 2 - 1) {
@@ -192,8 +206,8 @@ __global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int t
     __builtin_amdgcn_sched_barrier(0);
   };
   Codes ca, cb;
-  load_codes(ca, 0);
-  load_codes(cb, 1);
+  load_codes(ca, k_begin);
+  load_codes(cb, k_begin + 1);
   __builtin_amdgcn_sched_barrier(0);
   load_x();
   load_x();
@@ -203,56 +217,127 @@ __global__ __launch_bounds__(512, 2) void linear_many_kernel(LinearArgs p, int t
   many_wait<2 * NL>();
   many_barrier();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) read_x(0, 0, i);
-  int k = 0;
-  for (; k + 1 < p.kt; k += 2) {
+  for (int i = 0; i < TT; ++i) read_x(k_begin, 0, i);
+  int k = k_begin;
+  for (; k + 1 < k_end; k += 2) {
     stage(ca, cb, k);
     stage(cb, ca, k + 1);
   }
-  if (k < p.kt) stage(ca, cb, k);
+  if (k < k_end) stage(ca, cb, k);
   if (!GS) last_scale = p.scales[group0];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) add_scaled(i, last_scale);
+  for (int i = 0; i < TT; ++i) add_scaled(i, last_scale);
 
   // ---- results: through LDS, so that a token's outputs leave in runs.  The lane has row l32 of a tile, tokens 8 (e / 4) + 4 half + e % 4.
   many_wait<0>();                                       // (no load writes to LDS from here on)
   many_barrier();
   float* out = reinterpret_cast<float*>(smem);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < TT; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) out[(i * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * kOutRow + wave * 32 + l32] = total[i][e];
+    for (int e = 0; e < 16; ++e) out[(i * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * Tile::kOutRow + wave * 32 + l32] = total[i][e];
   __syncthreads();
-  const int col = (tid & 31) * 8, row = row0 + col;
+  constexpr int RUNS = Tile::kRows / 8;                  // runs of eight rows
+  const int col = tid % RUNS * 8, row = row0 + col;
   float b[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) b[e] = p.bias && row + e < p.m ? p.bias[row + e] : 0.f;
-  for (int t = tid >> 5; t < kManyTokens; t += 16) {
+  for (int e = 0; e < 8; ++e) b[e] = p.bias && p.parts == 1 && row + e < p.m ? p.bias[row + e] : 0.f;
+  for (int t = tid / RUNS; t < Tile::kTokens; t += 64 * WV / RUNS) {
     const int tok = tok0 + t;
     if (tok >= p.tokens || row >= p.m) break;
-    const float sx = I8 ? p.xs[tok] : 1.f;
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = I8 ? fmaf(out[t * kOutRow + col + e], sx, b[e]) : out[t * kOutRow + col + e] + b[e];
-    linear_store(p, tok, row, v);
+    for (int e = 0; e < 8; ++e) v[e] = out[t * Tile::kOutRow + col + e];
+    if (p.parts > 1) {                                   // (whole runs: rows of p.partial have room for them)
+      float* to = p.partial + ((int64_t)part * p.tokens + tok) * p.ld_partial + row;
+      *reinterpret_cast<f32x4*>(to) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4*>(to + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    } else {
+      const float sx = I8 ? p.xs[tok] : 1.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = I8 ? fmaf(v[e], sx, b[e]) : v[e] + b[e];
+      linear_store(p, tok, row, v);
+    }
   }
 }
 
-template <bool I8, int GS> static hipError_t launch_many_as(const LinearArgs& p, hipStream_t s) {
+// The parts' sums of eight outputs of a token, in order.
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs p) {
+  const int runs = (int)(p.ld_partial / 8);
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int tok = (int)(at / runs), row = (int)(at % runs) * 8;
+  if (tok >= p.tokens) return;
+  f32x4 v[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+  for (int k = 0; k < p.parts; ++k) {
+    const float* from = p.partial + ((int64_t)k * p.tokens + tok) * p.ld_partial + row;
+    v[0] += *reinterpret_cast<const f32x4*>(from);
+    v[1] += *reinterpret_cast<const f32x4*>(from + 4);
+  }
+  const float sx = p.xs ? p.xs[tok] : 1.f;
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = fmaf(v[e >> 2][e & 3], sx, p.bias && row + e < p.m ? p.bias[row + e] : 0.f);
+  linear_store(p, tok, row, y);
+}
+
+template <bool I8, int GS, int TT, int WV> static hipError_t launch_many_as(const LinearArgs& p, hipStream_t s) {
+  using Tile = ManyTile<TT, WV>;
   static LdsLimitOnce once;
-  if (const hipError_t e = once.ensure((const void*)&linear_many_kernel<I8, GS>, kManyLds); e != hipSuccess) return e;
-  const int tt = (p.tokens + kManyTokens - 1) / kManyTokens, rt = (p.m + kManyRows - 1) / kManyRows;
-  hipLaunchKernelGGL((linear_many_kernel<I8, GS>), dim3((unsigned)(tt * rt)), dim3(512), kManyLds, s, p, tt, rt);
+  if (const hipError_t e = once.ensure((const void*)&linear_many_kernel<I8, GS, TT, WV>, Tile::kLds); e != hipSuccess) return e;
+  const int tt = (p.tokens + Tile::kTokens - 1) / Tile::kTokens, rt = (p.m + Tile::kRows - 1) / Tile::kRows;
+  hipLaunchKernelGGL((linear_many_kernel<I8, GS, TT, WV>), dim3((unsigned)((int64_t)tt * rt * p.parts)), dim3(64 * WV), Tile::kLds, s, p, tt, rt);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess || p.parts == 1) return e;
+  hipLaunchKernelGGL(linear_join_kernel, dim3((unsigned)((p.tokens * (p.ld_partial / 8) + 255) / 256)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
-
-hipError_t launch_linear_many(const LinearArgs& p, int gs, bool i8, hipStream_t s) {
+template <int TT, int WV> static hipError_t launch_many_of(const LinearArgs& p, int gs, bool i8, hipStream_t s) {
   switch (gs) {
-    case 0: return i8 ? launch_many_as<true, 0>(p, s) : launch_many_as<false, 0>(p, s);
-    case 1: return i8 ? launch_many_as<true, 1>(p, s) : launch_many_as<false, 1>(p, s);
-    case 2: return i8 ? launch_many_as<true, 2>(p, s) : launch_many_as<false, 2>(p, s);
-    default: return i8 ? launch_many_as<true, 4>(p, s) : launch_many_as<false, 4>(p, s);
+    case 0: return i8 ? launch_many_as<true, 0, TT, WV>(p, s) : launch_many_as<false, 0, TT, WV>(p, s);
+    case 1: return i8 ? launch_many_as<true, 1, TT, WV>(p, s) : launch_many_as<false, 1, TT, WV>(p, s);
+    case 2: return i8 ? launch_many_as<true, 2, TT, WV>(p, s) : launch_many_as<false, 2, TT, WV>(p, s);
+    default: return i8 ? launch_many_as<true, 4, TT, WV>(p, s) : launch_many_as<false, 4, TT, WV>(p, s);
   }
+}
+
+// Tile of a call: tiles of 32 tokens, and wavefronts.
+static void many_tile(int64_t tokens, int& tt, int& wv) {
+  tt = tokens <= 32 ? 1 : tokens <= 64 ? 2 : 4;
+  wv = tt == 4 ? 8 : 4;
+}
+// Parts that the columns are taken in: as many as leave room for 512 workgroups of four wavefronts (two a CU) or 256 of eight, of at least
+// four stages each.  On 4096 x 4096, 11008 x 4096, 4096 x 11008, 28672 x 8192 and 1024 x 8192, 17 to 1024 tokens: room for 256 (128) instead takes
+// 1.0 to 1.7 times as long, for 1024 (512) 0.9 to 1.8 times; parts of two stages 1.0 to 1.3 times, of eight 1.0 to 1.15 times.
+constexpr int kMinStages = 4;
+static int64_t many_room(int tt) { return tt == 4 ? 256 : 512; }
+static int64_t many_parts(int64_t tokens, int64_t m, int64_t n) {
+  int tt, wv;
+  many_tile(tokens, tt, wv);
+  const int64_t tiles = (tokens + 32 * tt - 1) / (32 * tt) * ((m + 32 * wv - 1) / (32 * wv)), most = (n + 127) / 128 / kMinStages;
+  const int64_t want = many_room(tt) / tiles;
+  return want < 1 || most < 1 ? 1 : want < most ? want : most;
+}
+// Of a call with at most so many tokens: of each tile, parts * tiles of tokens is at most room / tiles of rows.
+size_t linear_partial_bytes(int64_t tokens, int64_t m, int64_t n) {
+  const int64_t ld = (m + 7) / 8 * 8;
+  size_t most = 0;
+  for (const int64_t t : {17, 33, 65}) {
+    int tt, wv;
+    many_tile(t, tt, wv);
+    const int64_t each = many_room(tt) / ((m + 32 * wv - 1) / (32 * wv));
+    if (tokens < t || many_parts(t, m, n) < 2) continue;
+    const size_t bytes = (size_t)(each * 32 * tt * ld) * 4;
+    most = bytes > most ? bytes : most;
+  }
+  return most;
+}
+
+hipError_t launch_linear_many(LinearArgs p, int gs, bool i8, float* partial, hipStream_t s) {
+  int tt, wv;
+  many_tile(p.tokens, tt, wv);
+  p.parts = (int32_t)many_parts(p.tokens, p.m, (int64_t)p.kt * 128);
+  p.partial = partial;
+  p.ld_partial = (p.m + 7) / 8 * 8;
+  return tt == 1 ? launch_many_of<1, 4>(p, gs, i8, s) : tt == 2 ? launch_many_of<2, 4>(p, gs, i8, s) : launch_many_of<4, 8>(p, gs, i8, s);
 }
 
 }  // namespace gptaq

@@ -98,6 +98,9 @@ SHAPES = [                                             # tokens, m, n, group
     (1, 1, 1, 0), (1, 16, 32, 32), (1, 17, 128, 128), (2, 5, 96, 32), (3, 33, 192, 64), (1, 257, 1000, 0), (16, 48, 640, 128),
     (17, 64, 384, 64), (15, 100, 136, 0), (33, 129, 256, 32), (64, 128, 1024, 128), (65, 80, 520, 0), (130, 272, 512, 64),
     (1, 2048, 11008, 128), (300, 512, 768, 128), (257, 515, 1024, 0), (700, 1040, 384, 32), (520, 256, 2736, 0),
+    # around the lines between kernels and tiles, and sums taken in parts of the columns
+    (16, 8200, 256, 128), (9, 16400, 128, 32), (8, 16390, 256, 64), (17, 30, 2048, 128), (32, 500, 1536, 32), (33, 260, 2176, 64), (64, 129, 4096, 0), (65, 1000, 2944, 128),
+    (128, 60, 8192, 128), (129, 300, 5000, 0), (300, 258, 3968, 128), (18, 1, 16384, 64),
 ]
 
 
