@@ -5,6 +5,7 @@
 // per group of columns the sum of (code - zero) x is taken in fp32 (bf16 activations) or exactly in int32 (8-bit activations),
 // multiplied by the group's fp32 scale, and added to the fp32 total.  No weight is rounded.
 #include "linear.h"
+#include <type_traits>
 
 namespace gptaq {
 
@@ -71,9 +72,15 @@ __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t 
 // feed the matrix unit, two tiles of columns ahead: nothing of W is read twice, and with everything of a wavefront independent many
 // loads are in flight.  The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the result has the
 // row of W in l % 16 and tokens 4 (l / 16) .. + 3 in the lane's four values, so one scale per lane serves a result.
+// A load of 16 bytes a lane costs the same whether its lanes want it or not, and a token fills 4 of 64 lanes: so up to XT = 4 (8) tokens
+// one load brings 4 (2) of the 4 steps of 128 columns, each to XT lanes of 16 of its own; the others are zeros for that step, the result has
+// the steps in different rows, and the join adds them.
 // GS: groups per 128 columns (1, 2, 4), 0: one group per row.
-template <bool I8, int GS, int RT>
-__global__ __launch_bounds__(RT == 1 ? 1024 : 512) void linear_few_kernel(LinearArgs p) {
+// Most wavefronts of a workgroup: 16 leave a lane 128 registers.
+constexpr int few_waves(int gs, int rt, int xt) { return rt > 1 || (gs == 4 && xt == 16) ? 8 : 16; }
+
+template <bool I8, int GS, int RT, int XT>
+__global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(LinearArgs p) {
   extern __shared__ float lds[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int l16 = lane & 15, q = lane >> 4;
@@ -90,10 +97,13 @@ __global__ __launch_bounds__(RT == 1 ? 1024 : 512) void linear_few_kernel(Linear
     codes[r] = p.codes + tr * p.kt * 1024 + lane * 16;
     group[r] = tr * p.groups * 16 + l16;
   }
-  const bool here = l16 < p.tokens;
-  const uint8_t* x0 = (const uint8_t*)p.x + ((int64_t)(here ? l16 : 0) * p.ldx + q * 8) * (I8 ? 1 : 2);
+  constexpr int SP = 16 / XT, NX = 4 / SP;       // steps per load of activations, loads per 128 columns
+  const int sub = l16 / XT, tok_lane = l16 % XT;
+  const bool here = tok_lane < p.tokens;
+  const int x_col = sub * 32 + q * 8;
+  const uint8_t* x0 = (const uint8_t*)p.x + ((int64_t)(here ? tok_lane : 0) * p.ldx + x_col) * (I8 ? 1 : 2);
 
-  struct Stage { u32x4 w[RT]; uint32_t zero[RT][G]; float scale[RT][G]; u32x4 x[4]; };
+  struct Stage { u32x4 w[RT]; uint32_t zero[RT][G]; float scale[RT][G]; u32x4 x[NX]; };
   auto load = [&](Stage& s, int k) {
     if (k >= p.kt) return;
 #pragma unroll
@@ -108,10 +118,10 @@ __global__ __launch_bounds__(RT == 1 ? 1024 : 512) void linear_few_kernel(Linear
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int col = k * 128 + i * 32;
+    for (int i = 0; i < NX; ++i) {
+      const int col = k * 128 + i * SP * 32;
       s.x[i] = u32x4{0u, 0u, 0u, 0u};
-      if (here && col + q * 8 < p.n) {
+      if (here && col + x_col < p.n) {
         if (I8) {
           const u32x2 v = *reinterpret_cast<const u32x2*>(x0 + col);
           s.x[i][0] = v[0]; s.x[i][1] = v[1];
@@ -121,85 +131,147 @@ __global__ __launch_bounds__(RT == 1 ? 1024 : 512) void linear_few_kernel(Linear
       }
     }
   };
-  auto add_scaled = [&](int r, float s) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) total[r][e] = fmaf(s, I8 ? (float)__float_as_int(acc[r][e]) : acc[r][e], total[r][e]);
-  };
-  uint32_t row_off[RT];
+  uint32_t row_zero[RT];
   if (!GS) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r) row_off[r] = linear_offset(p.zeros[group[r]]);
+    for (int r = 0; r < RT; ++r) row_zero[r] = p.zeros[group[r]];
   }
-  auto multiply = [&](const Stage& s) {
+  const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  uint32_t sixteen = 0x41804180u;
+  asm volatile("" : "+v"(sixteen));
+  f32x4 accx;                          // sums of the group's activations (the same in all of a token's lanes)
+  // EXACT: the products are those of code - zero.  Else (bf16 only): of 16 + code, which is two instructions for two codes where the difference
+  // takes five, and (16 + zero) times the activations' sum, one more matrix instruction for all RT, is taken off each group's sum.
+  // Where a result is not finite this subtraction may be why, and the workgroup takes its sums again with EXACT.
+  auto add_scaled = [&](auto exact, int r, float s, uint32_t zero) {
+    const float z = -16.f - (float)zero;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
+    for (int e = 0; e < 4; ++e) {
+      float v = I8 ? (float)__float_as_int(acc[r][e]) : acc[r][e];
+      if (!exact) v = fmaf(z, accx[e], v);
+      total[r][e] = fmaf(s, v, total[r][e]);
+    }
+  };
+  auto multiply = [&](auto exact, const Stage& s) {
+    const f32x4 nothing = {0.f, 0.f, 0.f, 0.f};
+    u32x4 all[NX];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t off = GS ? linear_offset(s.zero[r][i * G / 4]) : row_off[r];
-        const f32x4 c = GS && i % (4 / G) == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[r];
-        if (I8)
+    for (int i = 0; i < NX; ++i) {
+      all[i] = s.x[i];
+      if (!exact)                      // columns 0 2 4 6 1 3 5 7, as the codes come out of a word
+        all[i] = u32x4{__builtin_amdgcn_perm(s.x[i][1], s.x[i][0], 0x05040100u), __builtin_amdgcn_perm(s.x[i][3], s.x[i][2], 0x05040100u),
+                       __builtin_amdgcn_perm(s.x[i][1], s.x[i][0], 0x07060302u), __builtin_amdgcn_perm(s.x[i][3], s.x[i][2], 0x07060302u)};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool first = GS && i % (4 / G) == 0, last = GS && (i + 1) % (4 / G) == 0;
+      u32x4 x = all[i / SP];
+      if (SP > 1) {
+#pragma unroll
+        for (int e = 0; e < (I8 ? 2 : 4); ++e) x[e] = sub == i % SP ? x[e] : 0u;
+      }
+      if (!exact)
+        accx = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, ones), first ? nothing : accx, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const f32x4 c = first ? nothing : acc[r];
+        const uint32_t w = s.w[r][i], zero = GS ? s.zero[r][i * G / 4] : row_zero[r];
+        if (I8) {
           acc[r] = __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x32_i8(
-              __builtin_bit_cast(long, u32x2{s.x[i][0], s.x[i][1]}), __builtin_bit_cast(long, linear_bytes(s.w[r][i], off)),
+              __builtin_bit_cast(long, u32x2{x[0], x[1]}), __builtin_bit_cast(long, linear_bytes(w, linear_offset(zero))),
               __builtin_bit_cast(i32x4, c), 0, 0, 0));
-        else
-          acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, s.x[i]), linear_bf16(s.w[r][i], off), c, 0, 0, 0);
-        if (GS && (i + 1) % (4 / G) == 0) add_scaled(r, s.scale[r][i * G / 4]);
+        } else if (exact) {
+          acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), linear_bf16(w, linear_offset(zero)), c, 0, 0, 0);
+        } else {
+          u32x4 v;                     // the code in the upper bits of the mantissa of 16
+          const uint32_t sh[4] = {w << 3, w >> 1, w >> 5, w >> 9};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(v[e]) : "v"(sh[e]), "s"(0x00780078u), "v"(sixteen));
+          acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, v), c, 0, 0, 0);
+        }
+        if (last) add_scaled(exact, r, s.scale[r][i * G / 4], zero);
       }
     }
   };
-  Stage a, b;
-  load(a, wave);
-  load(b, wave + waves);
-  for (int k = wave; k < p.kt; k += 2 * waves) {
-    multiply(a);
-    load(a, k + 2 * waves);
-    if (k + waves >= p.kt) break;
-    multiply(b);
-    load(b, k + 3 * waves);
-  }
-  if (!GS) {
+  auto sums = [&](auto exact) {
+    accx = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int r = 0; r < RT; ++r) add_scaled(r, p.scales[group[r]]);
-  }
-  // [wave][r][lane][4]
+    for (int r = 0; r < RT; ++r) total[r] = acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    Stage a, b;
+    load(a, wave);
+    load(b, wave + waves);
+    for (int k = wave; k < p.kt; k += 2 * waves) {
+      multiply(exact, a);
+      load(a, k + 2 * waves);
+      if (k + waves >= p.kt) break;
+      multiply(exact, b);
+      load(b, k + 3 * waves);
+    }
+    if (!GS) {
 #pragma unroll
-  for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(&lds[((wave * RT + r) * 64 + lane) * 4]) = total[r];
-  __syncthreads();
-  for (int at = threadIdx.x; at < RT * 256; at += blockDim.x) {
-    // 16 RT rows of W in a run of threads, so that a token's outputs are written together
-    const int r = at % (16 * RT), tok = at / (16 * RT), row = rt0 * 16 + r;
-    if (row >= p.m || tok >= p.tokens) continue;
-    const int slot = ((r >> 4) * 64 + (tok >> 2) * 16 + (r & 15)) * 4 + (tok & 3);
-    float v = 0.f;
-    for (int w = 0; w < waves; ++w) v += lds[w * RT * 256 + slot];
-    if (I8) v *= p.xs[tok];
-    if (p.bias) v += p.bias[row];
-    const int64_t o = (int64_t)tok * p.ldy + row;
-    if (p.y_f32) ((float*)p.y)[o] = v;
-    else ((uint16_t*)p.y)[o] = __builtin_bit_cast(uint16_t, (__bf16)v);
+      for (int r = 0; r < RT; ++r) add_scaled(exact, r, p.scales[group[r]], row_zero[r]);
+    }
+  };
+  // Joins the wavefronts' sums, [wave][r][lane][4], and stores; returns whether a sum of this thread's is not finite.
+  auto finish = [&]() {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(&lds[((wave * RT + r) * 64 + lane) * 4]) = total[r];
+    __syncthreads();
+    bool lost = false;
+    for (int at = threadIdx.x; at < RT * 16 * XT; at += blockDim.x) {
+      // 16 RT rows of W in a run of threads, so that a token's outputs are written together
+      const int r = at % (16 * RT), tok = at / (16 * RT), row = rt0 * 16 + r;
+      if (row >= p.m || tok >= p.tokens) continue;
+      float v = 0.f;
+      for (int w = 0; w < waves; ++w)
+#pragma unroll
+        for (int st = 0; st < SP; ++st) {
+          const int t = st * XT + tok;
+          v += lds[w * RT * 256 + ((r >> 4) * 64 + (t >> 2) * 16 + (r & 15)) * 4 + (t & 3)];
+        }
+      lost |= !(fabsf(v) < __builtin_inff());
+      if (I8) v *= p.xs[tok];
+      if (p.bias) v += p.bias[row];
+      const int64_t o = (int64_t)tok * p.ldy + row;
+      if (p.y_f32) ((float*)p.y)[o] = v;
+      else ((uint16_t*)p.y)[o] = __builtin_bit_cast(uint16_t, (__bf16)v);
+    }
+    return lost;
+  };
+  sums(std::integral_constant<bool, I8>{});
+  const bool lost = finish();
+  if (!I8 && __syncthreads_or(lost)) {
+    sums(std::true_type{});
+    finish();
   }
 }
 
-template <bool I8, int RT>
-static hipError_t launch_few_as(const LinearArgs& p, int gs, int waves, hipStream_t s) {
-  const auto kernel = gs == 0 ? &linear_few_kernel<I8, 0, RT> : gs == 1 ? &linear_few_kernel<I8, 1, RT>
-                    : gs == 2 ? &linear_few_kernel<I8, 2, RT> : &linear_few_kernel<I8, RT == 4 ? 2 : 4, RT>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.mt + RT - 1) / RT)), dim3(64 * waves), (size_t)waves * RT * 1024, s, p);
+template <bool I8, int GS, int RT, int XT>
+static hipError_t launch_few_as(const LinearArgs& p, int waves, hipStream_t s) {
+  if (waves > few_waves(GS, RT, XT)) waves = few_waves(GS, RT, XT);
+  while (waves > 1 && waves > p.kt) waves /= 2;
+  hipLaunchKernelGGL((linear_few_kernel<I8, GS, RT, XT>), dim3((unsigned)((p.mt + RT - 1) / RT)), dim3(64 * waves), (size_t)waves * RT * 1024, s, p);
   return hipGetLastError();
 }
-// Tiles of rows per workgroup: the more, the less often the activations are read, the fewer workgroups.  us a call, 1 token, RT 1 / 2 / 4:
-// 4096 x 4096 5.1 / 7.4 / 10.3, 11008 x 4096 10.7 / 11.3 / 11.5, 28672 x 8192 43.2 / 38.3 / 40.9; 16 tokens 6.7 / 8.4 / 11.8, 15.2 / 13.7 / 12.5,
-// 60.8 / 45.7 / 42.3.  (With four groups to 128 columns, four tiles of rows have more scales than registers.)
-// Wavefronts, RT 1, 8 / 16: 4096 x 11008 11.3 / 9.3, 1024 x 8192 7.1 / 6.6, 11008 x 4096 10.7 / 11.7.  RT 4, 4 / 8: 28672 x 8192, 16 tokens 40.2 / 42.3,
-// 11008 x 4096 15.0 / 12.5.
+// Tiles of rows per workgroup: the more, the less often the activations are read, the fewer workgroups.  us a call, bf16, RT 1 / 2 / 4: 1 token
+// 4096 x 4096 4.5 / 5.8 / 9.5, 28672 x 8192 31.8 / 30.0 / 37; 16 tokens 4096 x 4096 7.1 / 7.9 / 11, 11008 x 4096 15.6 / 14.6 / 10.4, 28672 x 8192
+// 61 / 49 / 34.  (With four groups to 128 columns, four tiles of rows have more scales than registers.)
+// Wavefronts, RT 1, 8 / 16: 4096 x 11008 8.7 / 8.1, 1024 x 8192 5.8 / 5.7, 11008 x 4096 8.9 / 9.5; RT 4, 4 / 8: 28672 x 8192, 16 tokens 34 / 42,
+// 11008 x 4096 14.9 / 10.4.
+template <bool I8, int GS>
+static hipError_t launch_few_of(const LinearArgs& p, hipStream_t s) {
+  if (p.tokens > 8) {
+    if (p.mt < 512) return launch_few_as<I8, GS, 1, 16>(p, 16, s);
+    if (GS == 4) return launch_few_as<I8, GS, 2, 16>(p, 8, s);
+    return launch_few_as<I8, GS, GS == 4 ? 2 : 4, 16>(p, p.mt >= 1024 ? 4 : 8, s);
+  }
+  const int waves = p.mt < 512 ? 16 : 8;
+  if (p.tokens > 4) return p.mt >= 1024 ? launch_few_as<I8, GS, 2, 8>(p, waves, s) : launch_few_as<I8, GS, 1, 8>(p, waves, s);
+  return p.mt >= 1024 ? launch_few_as<I8, GS, 2, 4>(p, waves, s) : launch_few_as<I8, GS, 1, 4>(p, waves, s);
+}
 template <bool I8>
 static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
-  const int rt = p.tokens > 8 ? (p.mt >= 512 ? (gs == 4 ? 2 : 4) : 1) : p.mt >= 1024 ? 2 : 1;
-  int waves = rt == 1 ? (p.mt < 512 ? 16 : 8) : rt == 4 && p.mt >= 1024 ? 4 : 8;
-  while (waves > 1 && waves > p.kt) waves /= 2;
-  if (rt == 4) return launch_few_as<I8, 4>(p, gs, waves, s);
-  if (rt == 2) return launch_few_as<I8, 2>(p, gs, waves, s);
-  return launch_few_as<I8, 1>(p, gs, waves, s);
+  return gs == 0 ? launch_few_of<I8, 0>(p, s) : gs == 1 ? launch_few_of<I8, 1>(p, s) : gs == 2 ? launch_few_of<I8, 2>(p, s) : launch_few_of<I8, 4>(p, s);
 }
 
 static hipError_t launch_linear(const LinearArgs& p, int gs, bool i8, float* partial, hipStream_t s) {
