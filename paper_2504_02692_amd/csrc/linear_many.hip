@@ -299,41 +299,46 @@ template <int TT, int WV> static hipError_t launch_many_of(const LinearArgs& p, 
   }
 }
 
-// Tile of a call: tiles of 32 tokens, and wavefronts.
-static void many_tile(int64_t tokens, int& tt, int& wv) {
-  tt = tokens <= 32 ? 1 : tokens <= 64 ? 2 : 4;
+// Tile of a call: tiles of 32 tokens, and wavefronts.  Small tiles where the large ones are few: us a call with 128 x 256 / 64 x 128, bf16,
+// tiles of the larger kind times 128 columns in brackets: 4096 x 4096, 65 tokens 20.0 / 16.8 (512), 384 31.2 / 30.7 (1536), 768 43.6 / 43.6 (3072), 2048 70 /
+// 96 (8192); 4096 x 11008, 192 tokens 37.6 / 34.7 (2752), 384 49.9 / 61.4 (4128); 11008 x 4096, 128 tokens 30.4 / 31.4 (1376), 512 58.7 / 72.5 (5504);
+// 4096 x 1024, 257 tokens 17.0 / 10.6 (384), 1024 19.2 / 16.4 (1024), 2048 23.2 / 28.5 (2048, 256 tiles); 8-bit activations a little more for the small ones.
+static void many_tile(int64_t tokens, int64_t m, int64_t n, int& tt, int& wv) {
+  const int64_t large = (tokens + 127) / 128 * ((m + 255) / 256), kt = (n + 127) / 128;
+  tt = tokens <= 32 ? 1 : tokens <= 64 || (large <= 128 && large * kt <= 3072) ? 2 : 4;
   wv = tt == 4 ? 8 : 4;
 }
-// Parts that the columns are taken in: as many as leave room for 512 workgroups of four wavefronts (two a CU) or 256 of eight, of at least
-// four stages each.  On 4096 x 4096, 11008 x 4096, 4096 x 11008, 28672 x 8192 and 1024 x 8192, 17 to 1024 tokens: room for 256 (128) instead takes
-// 1.0 to 1.7 times as long, for 1024 (512) 0.9 to 1.8 times; parts of two stages 1.0 to 1.3 times, of eight 1.0 to 1.15 times.
-constexpr int kMinStages = 4;
+// Parts that the columns are taken in: as many as leave room for 512 workgroups of four wavefronts (two a CU) or 256 of eight, of at least eight
+// stages each (four up to 64 tokens, where joining them is cheap).  On 4096 x 4096, 11008 x 4096, 4096 x 11008, 28672 x 8192 and 1024 x 8192, 17 to 1024
+// tokens: room for 256 (128) instead takes 1.0 to 1.7 times as long, for 1024 (512) 0.9 to 1.8 times.  Stages, 8 / 4: 4096 x 4096, 17 tokens 13.7 /
+// 12.3, 4096 x 1024, 512 tokens 12.0 / 19.2, 1024 x 4096, 512 tokens 17.6 / 19.1.
 static int64_t many_room(int tt) { return tt == 4 ? 256 : 512; }
+static int64_t most_parts(int64_t tokens, int64_t n) { return (n + 127) / 128 / (tokens <= 64 ? 4 : 8); }
 static int64_t many_parts(int64_t tokens, int64_t m, int64_t n) {
   int tt, wv;
-  many_tile(tokens, tt, wv);
-  const int64_t tiles = (tokens + 32 * tt - 1) / (32 * tt) * ((m + 32 * wv - 1) / (32 * wv)), most = (n + 127) / 128 / kMinStages;
+  many_tile(tokens, m, n, tt, wv);
+  const int64_t tiles = (tokens + 32 * tt - 1) / (32 * tt) * ((m + 32 * wv - 1) / (32 * wv)), most = most_parts(tokens, n);
   const int64_t want = many_room(tt) / tiles;
   return want < 1 || most < 1 ? 1 : want < most ? want : most;
 }
-// Of a call with at most so many tokens: of each tile, parts * tiles of tokens is at most room / tiles of rows.
+// Room for the partial sums of every call with at most so many tokens: parts times tiles of tokens is at most room / tiles of rows.
 size_t linear_partial_bytes(int64_t tokens, int64_t m, int64_t n) {
   const int64_t ld = (m + 7) / 8 * 8;
-  size_t most = 0;
-  for (const int64_t t : {17, 33, 65}) {
-    int tt, wv;
-    many_tile(t, tt, wv);
-    const int64_t each = many_room(tt) / ((m + 32 * wv - 1) / (32 * wv));
-    if (tokens < t || many_parts(t, m, n) < 2) continue;
-    const size_t bytes = (size_t)(each * 32 * tt * ld) * 4;
-    most = bytes > most ? bytes : most;
+  int64_t rows = 0;                                        // of ld floats
+  for (const int tt : {1, 2, 4}) {
+    const int64_t least = tt == 1 ? 17 : 16 * tt + 1, each = many_room(tt) / ((m + 64 * (tt == 4 ? 4 : 2) - 1) / (64 * (tt == 4 ? 4 : 2)));
+    for (const int64_t t : {tokens < 64 ? tokens : (int64_t)64, tokens}) {
+      if (t < least || each < 2 || most_parts(t, n) < 2) continue;
+      const int64_t need = each * 32 * tt < most_parts(t, n) * t ? each * 32 * tt : most_parts(t, n) * t;
+      rows = need > rows ? need : rows;
+    }
   }
-  return most;
+  return (size_t)(rows * ld) * 4;
 }
 
 hipError_t launch_linear_many(LinearArgs p, int gs, bool i8, float* partial, hipStream_t s) {
   int tt, wv;
-  many_tile(p.tokens, tt, wv);
+  many_tile(p.tokens, p.m, (int64_t)p.kt * 128, tt, wv);
   p.parts = (int32_t)many_parts(p.tokens, p.m, (int64_t)p.kt * 128);
   p.partial = partial;
   p.ld_partial = (p.m + 7) / 8 * 8;
