@@ -138,7 +138,7 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(
   }
   const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
   uint32_t sixteen = 0x41804180u;
-  asm volatile("" : "+v"(sixteen));
+  asm volatile("" : "+v"(sixteen));    // (in a register, where the mask and it are one instruction)
   f32x4 accx;                          // sums of the group's activations (the same in all of a token's lanes)
   // EXACT: the products are those of code - zero.  Else (bf16 only): of 16 + code, which is two instructions for two codes where the difference
   // takes five, and (16 + zero) times the activations' sum, one more matrix instruction for all RT, is taken off each group's sum.
@@ -184,9 +184,9 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(
           acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), linear_bf16(w, linear_offset(zero)), c, 0, 0, 0);
         } else {
           u32x4 v;                     // the code in the upper bits of the mantissa of 16
-          const uint32_t sh[4] = {w << 3, w >> 1, w >> 5, w >> 9};
+          const uint32_t shifted[4] = {w << 3, w >> 1, w >> 5, w >> 9};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(v[e]) : "v"(sh[e]), "s"(0x00780078u), "v"(sixteen));
+          for (int e = 0; e < 4; ++e) v[e] = (shifted[e] & 0x00780078u) | sixteen;
           acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, v), c, 0, 0, 0);
         }
         if (last) add_scaled(exact, r, s.scale[r][i * G / 4], zero);
