@@ -450,3 +450,62 @@ def test_another_stream_and_a_graph(tokens):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, block())), k
         ws.fill_(k)
+
+
+def test_rows_of_many_tokens_far_apart():
+    """The same for the kernels that take more than 16 tokens."""
+    m, n, ld = 40, 256, (1 << 27) + 64
+    codes, scales, zeros = quantised(m, n, 4, 64, False, rng(14))
+    w = pack(codes, scales, zeros, 64)
+    x = rng(15).integers(-8, 9, (20, n)).astype(np.float64)
+    X = torch.empty(19 * ld + n, dtype=torch.bfloat16, device="cuda").as_strided((20, n), (ld, 1))
+    Y = torch.empty(19 * ld + m, dtype=torch.bfloat16, device="cuda").as_strided((20, m), (ld, 1))
+    X.copy_(bf16(x))
+    ws = B.workspace(B.gptaq_linear_workspace_bytes(20, m, n))
+    B.gptaq_linear(X, w, ws, out=Y)
+    assert torch.equal(Y, B.gptaq_linear(bf16(x), w, ws))
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("tokens,m,n,group", [(1, 100, 512, 128), (17, 130, 4096, 32), (40, 500, 2048, 0), (70, 260, 4096, 64), (300, 77, 8192, 128), (140, 8200, 1024, 128)])
+def test_linear_keeps_to_its_memory(tokens, m, n, group, i8):
+    """A workspace of just the size that is asked for, and outputs with a gap behind each row: nothing around them changes."""
+    r = rng(tokens, m, 40)
+    w = pack(*quantised(m, n, 4, group, False, r), group, perm=r.permutation(n).astype(np.int32))
+    size = B.gptaq_linear_workspace_bytes(tokens, m, n)
+    buf = torch.full((size + 65536,), 85, dtype=torch.uint8, device="cuda")
+    out = padded(torch.zeros((tokens, m), device="cuda"), 7, 3)
+    if i8:
+        q = torch.from_numpy(r.integers(-127, 128, (tokens, n)).astype(np.int8)).cuda()
+        xs = torch.full((tokens,), 0.03, device="cuda")
+        call = lambda o, ws: B.gptaq_linear_i8(q, xs, w, ws, out=o)
+    else:
+        x = bf16(r.standard_normal((tokens, n)))
+        call = lambda o, ws: B.gptaq_linear(x, w, ws, out=o)
+    call(out, buf[:size])
+    assert torch.all(buf[size:] == 85)
+    if tokens > 1:
+        assert torch.isnan(out.as_strided((tokens - 1, 7), (out.stride(0), 1), out.storage_offset() + m)).all()
+    plain = torch.empty((tokens, m), device="cuda")
+    call(plain, B.workspace(size + 1024))
+    assert torch.equal(out, plain)                                 # and the same bits from call to call
+
+
+@pytest.mark.parametrize("group,act_order", [(64, False), (128, True), (0, True)])
+def test_mlp_from_solve_to_answers(group, act_order):
+    """The example at small sizes, against the formulas with the solve's dequantised weights in fp32: the outputs pass three roundings to
+    bfloat16 (2^-8 each at most) and, with 8 bits, two to steps of 1/127 of a row's largest value, half a step off and about 4 of its
+    deviations large: 1.6 % of a deviation at most, divided by sqrt(3) on average over a row."""
+    from paper_2504_02692_amd import quantized_mlp as Q
+    hidden, inner = 256, 384
+    mlp, full, quant = Q.calibrate(hidden, inner, 2048, group=group, act_order=act_order)
+    for tokens in (1, 5, 33, 200):
+        x, residual = bf16(rng(tokens, 50).standard_normal((tokens, hidden))), bf16(rng(tokens, 51).standard_normal((tokens, hidden)))
+        want = Q.full_precision(x, residual, mlp.norm, *quant)
+        for eight_bits, most in ((False, 3 * 2.0 ** -8), (True, 3 * 2.0 ** -8 + 2 * 0.016)):
+            y, total = mlp(x, residual, mlp.workspace(tokens), eight_bits)
+            assert torch.equal(total, (x.float() + residual.float()).to(torch.bfloat16))
+            assert (y.float() - want).norm().item() <= most * want.norm().item()
+        # 4-bit weights keep most of the signal
+        ref = Q.full_precision(x, residual, mlp.norm, *full)
+        assert (y.float() - ref).norm().item() <= 0.35 * ref.norm().item()
