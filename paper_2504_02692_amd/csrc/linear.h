@@ -45,6 +45,16 @@ __device__ __forceinline__ bf16x8 linear_bf16(uint32_t w, uint32_t off) {
   return v;
 }
 
+// 16 bytes a lane from base + lane offset + scalar offset to 1 KB of LDS.  (A buffer load: behind a global load to LDS the compiler takes LDS reads to
+// return in any order, and waits for all of them each time.)
+struct LdsLoader {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ LdsLoader(const unsigned char* base) : rsrc(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00020000)) {}
+  __device__ __forceinline__ void load(unsigned char* to, int lane, int scalar) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, lane, scalar, 0, 0);
+  }
+};
+
 struct LinearArgs {
   const void* x;                       // tokens x n bf16, or int8 codes
   const float* xs;                     // int8: a scale per token

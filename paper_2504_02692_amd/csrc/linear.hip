@@ -5,6 +5,7 @@
 // per group of columns the sum of (code - zero) x is taken in fp32 (bf16 activations) or exactly in int32 (8-bit activations),
 // multiplied by the group's fp32 scale, and added to the fp32 total.  No weight is rounded.
 #include "linear.h"
+#include <stdlib.h>
 #include <type_traits>
 
 namespace gptaq {
@@ -72,17 +73,16 @@ __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t 
 // feed the matrix unit, two tiles of columns ahead: nothing of W is read twice, and with everything of a wavefront independent many
 // loads are in flight.  The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the result has the
 // row of W in l % 16 and tokens 4 (l / 16) .. + 3 in the lane's four values, so one scale per lane serves a result.
-// A load of 16 bytes a lane costs the same whether its lanes want it or not, and a token fills 4 of 64 lanes: so up to XT = 4 (8) tokens
-// one load brings 4 (2) of the 4 steps of 128 columns, each to XT lanes of 16 of its own; the others are zeros for that step, the result has
-// the steps in different rows, and the join adds them.
+// Activations go to LDS in runs of a token's whole 128 columns, to a place of the wavefront's own, so that no wavefront waits for another.  (A load of
+// 16 tokens by 64 bytes to registers takes about four times as long as one of 1 KB in one run: 4096 x 11008, 16 tokens, 14.5 us; through LDS 9.3.)
 // GS: groups per 128 columns (1, 2, 4), 0: one group per row.
 // Most wavefronts of a workgroup: 16 leave a lane 128 registers.
-constexpr int few_waves(int gs, int rt, int xt) { return rt > 1 || (gs == 4 && xt == 16) ? 8 : 16; }
+constexpr int few_waves(int rt) { return rt > 1 ? 8 : 16; }
 
-template <bool I8, int GS, int RT, int XT>
-__global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(LinearArgs p) {
-  extern __shared__ float lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+template <bool I8, int GS, int RT>
+__global__ __launch_bounds__(64 * few_waves(RT)) void linear_few_kernel(LinearArgs p) {
+  extern __shared__ __attribute__((aligned(256))) float lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int l16 = lane & 15, q = lane >> 4;
   const int rt0 = blockIdx.x * RT;
   constexpr int G = GS ? GS : 1;       // groups per tile of 128 columns
@@ -97,18 +97,29 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(
     codes[r] = p.codes + tr * p.kt * 1024 + lane * 16;
     group[r] = tr * p.groups * 16 + l16;
   }
-  constexpr int SP = 16 / XT, NX = 4 / SP;       // steps per load of activations, loads per 128 columns
-  const int sub = l16 / XT, tok_lane = l16 % XT;
-  const bool here = tok_lane < p.tokens;
-  const int x_col = sub * 32 + q * 8;
-  const uint8_t* x0 = (const uint8_t*)p.x + ((int64_t)(here ? tok_lane : 0) * p.ldx + x_col) * (I8 ? 1 : 2);
+  // The 16-byte chunks of a token's 128 columns are permuted so that 16 tokens' same chunk lies in 16 different places of 256 bytes.  Places of
+  // tokens that there are not hold anything: their results are not stored.
+  constexpr int XROW = I8 ? 128 : 256, XSTAGE = 16 * XROW, CHUNKS = XROW / 16, PER_LOAD = 1024 / XROW, NL = 16 / PER_LOAD;
+  auto swizzle = [](int row) { return I8 ? (row >> 1) & 7 : row & 15; };
+  unsigned char* const xlds = reinterpret_cast<unsigned char*>(lds) + wave * 2 * XSTAGE;
+  const LdsLoader xfrom((const unsigned char*)p.x);
+  int xsrc[NL];
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    const int row = j * PER_LOAD + lane / CHUNKS;
+    xsrc[j] = min(row, p.tokens - 1) * (int)p.ldx * (I8 ? 1 : 2) + ((lane % CHUNKS ^ swizzle(row)) << 4);
+  }
 
-  struct Stage { u32x4 w[RT]; uint32_t zero[RT][G]; float scale[RT][G]; u32x4 x[NX]; };
-  auto load = [&](Stage& s, int k) {
-    if (k >= p.kt) return;
+  struct Stage { u32x4 w[RT]; uint32_t zero[RT][G]; float scale[RT][G]; };
+  auto load = [&](Stage& s, int k, int place) {
+    // the activations first: where the weights are there, so are they
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < NL; ++j)
+      if (j == 0 || j * PER_LOAD < p.tokens) xfrom.load(xlds + place * XSTAGE + j * 1024, xsrc[j], __builtin_amdgcn_readfirstlane(k * XROW));
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      s.w[r] = *reinterpret_cast<const u32x4*>(codes[r] + (int64_t)k * 1024);
       if (GS) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -116,19 +127,7 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(
           s.scale[r][g] = p.scales[group[r] + (int64_t)(k * GS + g) * 16];
         }
       }
-    }
-#pragma unroll
-    for (int i = 0; i < NX; ++i) {
-      const int col = k * 128 + i * SP * 32;
-      s.x[i] = u32x4{0u, 0u, 0u, 0u};
-      if (here && col + x_col < p.n) {
-        if (I8) {
-          const u32x2 v = *reinterpret_cast<const u32x2*>(x0 + col);
-          s.x[i][0] = v[0]; s.x[i][1] = v[1];
-        } else {
-          s.x[i] = *reinterpret_cast<const u32x4*>(x0 + 2 * col);
-        }
-      }
+      s.w[r] = *reinterpret_cast<const u32x4*>(codes[r] + (int64_t)k * 1024);
     }
   };
   uint32_t row_zero[RT];
@@ -152,26 +151,29 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(
       total[r][e] = fmaf(s, v, total[r][e]);
     }
   };
-  auto multiply = [&](auto exact, const Stage& s) {
+  auto multiply = [&](auto exact, const Stage& s, int place) {
     const f32x4 nothing = {0.f, 0.f, 0.f, 0.f};
-    u32x4 all[NX];
+    asm volatile("" :: "v"(s.w[RT - 1]) : "memory");
+    u32x4 all[4];
 #pragma unroll
-    for (int i = 0; i < NX; ++i) {
-      all[i] = s.x[i];
-      if (!exact)                      // columns 0 2 4 6 1 3 5 7, as the codes come out of a word
-        all[i] = u32x4{__builtin_amdgcn_perm(s.x[i][1], s.x[i][0], 0x05040100u), __builtin_amdgcn_perm(s.x[i][3], s.x[i][2], 0x05040100u),
-                       __builtin_amdgcn_perm(s.x[i][1], s.x[i][0], 0x07060302u), __builtin_amdgcn_perm(s.x[i][3], s.x[i][2], 0x07060302u)};
+    for (int i = 0; i < 4; ++i) {
+      const unsigned char* row = xlds + place * XSTAGE + l16 * XROW;
+      if (I8) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(row + (((2 * i + (q >> 1)) ^ swizzle(l16)) << 4) + (q & 1) * 8);
+        all[i] = u32x4{v[0], v[1], 0u, 0u};
+      } else {
+        all[i] = *reinterpret_cast<const u32x4*>(row + (((4 * i + q) ^ swizzle(l16)) << 4));
+      }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool first = GS && i % (4 / G) == 0, last = GS && (i + 1) % (4 / G) == 0;
-      u32x4 x = all[i / SP];
-      if (SP > 1) {
-#pragma unroll
-        for (int e = 0; e < (I8 ? 2 : 4); ++e) x[e] = sub == i % SP ? x[e] : 0u;
-      }
-      if (!exact)
+      u32x4 x = all[i];
+      if (!exact) {                    // columns 0 2 4 6 1 3 5 7, as the codes come out of a word
+        x = u32x4{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u), __builtin_amdgcn_perm(x[3], x[2], 0x05040100u),
+                  __builtin_amdgcn_perm(x[1], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
         accx = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, ones), first ? nothing : accx, 0, 0, 0);
+      }
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const f32x4 c = first ? nothing : acc[r];
@@ -197,16 +199,21 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(
     accx = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int r = 0; r < RT; ++r) total[r] = acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
-    Stage a, b;
-    load(a, wave);
-    load(b, wave + waves);
-    for (int k = wave; k < p.kt; k += 2 * waves) {
-      multiply(exact, a);
-      load(a, k + 2 * waves);
-      if (k + waves >= p.kt) break;
-      multiply(exact, b);
-      load(b, k + 3 * waves);
+    Stage a, b, c;
+    int k = wave;                      // (a workgroup has no more wavefronts than there are tiles)
+    load(a, k, 0);
+    if (k + waves < p.kt) load(b, k + waves, 1);
+    for (; k + 3 * waves < p.kt; k += 2 * waves) {
+      multiply(exact, a, 0);
+      load(a, k + 2 * waves, 0);
+      multiply(exact, b, 1);
+      load(b, k + 3 * waves, 1);
     }
+    multiply(exact, a, 0);
+    if (k + 2 * waves < p.kt) load(c, k + 2 * waves, 0);
+    if (k + waves < p.kt) multiply(exact, b, 1);
+    if (k + 2 * waves < p.kt) multiply(exact, c, 0);
+    __syncthreads();                   // (the sums go where other wavefronts' activations are)
     if (!GS) {
 #pragma unroll
       for (int r = 0; r < RT; ++r) add_scaled(exact, r, p.scales[group[r]], row_zero[r]);
@@ -218,17 +225,12 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(
     for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(&lds[((wave * RT + r) * 64 + lane) * 4]) = total[r];
     __syncthreads();
     bool lost = false;
-    for (int at = threadIdx.x; at < RT * 16 * XT; at += blockDim.x) {
+    for (int at = threadIdx.x; at < RT * 256; at += blockDim.x) {
       // 16 RT rows of W in a run of threads, so that a token's outputs are written together
       const int r = at % (16 * RT), tok = at / (16 * RT), row = rt0 * 16 + r;
       if (row >= p.m || tok >= p.tokens) continue;
       float v = 0.f;
-      for (int w = 0; w < waves; ++w)
-#pragma unroll
-        for (int st = 0; st < SP; ++st) {
-          const int t = st * XT + tok;
-          v += lds[w * RT * 256 + ((r >> 4) * 64 + (t >> 2) * 16 + (r & 15)) * 4 + (t & 3)];
-        }
+      for (int w = 0; w < waves; ++w) v += lds[w * RT * 256 + ((r >> 4) * 64 + (tok >> 2) * 16 + (r & 15)) * 4 + (tok & 3)];
       lost |= !(fabsf(v) < __builtin_inff());
       if (I8) v *= p.xs[tok];
       if (p.bias) v += p.bias[row];
@@ -246,28 +248,22 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, XT)) void linear_few_kernel(
   }
 }
 
-template <bool I8, int GS, int RT, int XT>
+template <bool I8, int GS, int RT>
 static hipError_t launch_few_as(const LinearArgs& p, int waves, hipStream_t s) {
-  if (waves > few_waves(GS, RT, XT)) waves = few_waves(GS, RT, XT);
+  if (waves > few_waves(RT)) waves = few_waves(RT);
   while (waves > 1 && waves > p.kt) waves /= 2;
-  hipLaunchKernelGGL((linear_few_kernel<I8, GS, RT, XT>), dim3((unsigned)((p.mt + RT - 1) / RT)), dim3(64 * waves), (size_t)waves * RT * 1024, s, p);
+  constexpr int kStages = 2 * 16 * (I8 ? 128 : 256), kPerWave = kStages > RT * 1024 ? kStages : RT * 1024;
+  static LdsLimitOnce once;
+  if (const hipError_t e = once.ensure((const void*)&linear_few_kernel<I8, GS, RT>, few_waves(RT) * kPerWave); e != hipSuccess) return e;
+  hipLaunchKernelGGL((linear_few_kernel<I8, GS, RT>), dim3((unsigned)((p.mt + RT - 1) / RT)), dim3(64 * waves), (size_t)(waves * kPerWave), s, p);
   return hipGetLastError();
 }
-// Tiles of rows per workgroup: the more, the less often the activations are read, the fewer workgroups.  us a call, bf16, RT 1 / 2 / 4: 1 token
-// 4096 x 4096 4.5 / 5.8 / 9.5, 28672 x 8192 31.8 / 30.0 / 37; 16 tokens 4096 x 4096 7.1 / 7.9 / 11, 11008 x 4096 15.6 / 14.6 / 10.4, 28672 x 8192
-// 61 / 49 / 34.  (With four groups to 128 columns, four tiles of rows have more scales than registers.)
-// Wavefronts, RT 1, 8 / 16: 4096 x 11008 8.7 / 8.1, 1024 x 8192 5.8 / 5.7, 11008 x 4096 8.9 / 9.5; RT 4, 4 / 8: 28672 x 8192, 16 tokens 34 / 42,
-// 11008 x 4096 14.9 / 10.4.
 template <bool I8, int GS>
 static hipError_t launch_few_of(const LinearArgs& p, hipStream_t s) {
-  if (p.tokens > 8) {
-    if (p.mt < 512) return launch_few_as<I8, GS, 1, 16>(p, 16, s);
-    if (GS == 4) return launch_few_as<I8, GS, 2, 16>(p, 8, s);
-    return launch_few_as<I8, GS, GS == 4 ? 2 : 4, 16>(p, p.mt >= 1024 ? 4 : 8, s);
-  }
-  const int waves = p.mt < 512 ? 16 : 8;
-  if (p.tokens > 4) return p.mt >= 1024 ? launch_few_as<I8, GS, 2, 8>(p, waves, s) : launch_few_as<I8, GS, 1, 8>(p, waves, s);
-  return p.mt >= 1024 ? launch_few_as<I8, GS, 2, 4>(p, waves, s) : launch_few_as<I8, GS, 1, 4>(p, waves, s);
+  static const char* e1 = getenv("FEW_RT"); static const char* e2 = getenv("FEW_W");
+  const int rt = e1 ? atoi(e1) : 1, waves = e2 ? atoi(e2) : 8;
+  if (rt == 4) return launch_few_as<I8, GS == 4 ? 2 : GS, 4>(p, waves, s);
+  return rt == 2 ? launch_few_as<I8, GS, 2>(p, waves, s) : launch_few_as<I8, GS, 1>(p, waves, s);
 }
 template <bool I8>
 static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
@@ -311,8 +307,7 @@ static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, i
   p.bias = bias; p.y = Y; p.ldy = ldy; p.y_f32 = y_f32 ? 1 : 0;
   p.tokens = (int32_t)tokens; p.m = (int32_t)m; p.n = (int32_t)n;
   p.mt = (int32_t)l.mt; p.kt = (int32_t)l.kt; p.groups = (int32_t)l.groups;
-  const int piece = tokens > 16 ? 128 : i8 ? 16 : 8;
-  if (perm || n % piece || ldx % (i8 ? 16 : 8) || ((uintptr_t)X & 15) || (tokens > 16 && ldx * (i8 ? 1 : 2) > kManyMaxRow)) {
+  if (perm || n % 128 || ldx % (i8 ? 16 : 8) || ((uintptr_t)X & 15) || ldx * (i8 ? 1 : 2) > kManyMaxRow) {
     const int64_t ld = padded_columns(n);
     if (i8) hipLaunchKernelGGL(linear_gather_kernel<int8_t>, dim3((unsigned)tokens), dim3(256), 0, s, (const int8_t*)X, ldx, perm, (int)n, (int8_t*)ws, ld);
     else hipLaunchKernelGGL(linear_gather_kernel<uint16_t>, dim3((unsigned)tokens), dim3(256), 0, s, (const uint16_t*)X, ldx, perm, (int)n, (uint16_t*)ws, ld);

@@ -34,15 +34,6 @@ template <int N> __device__ __forceinline__ void many_wait() {      // vmcnt <= 
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
-// 16 bytes a lane from base + lane offset + scalar offset to 1 KB of LDS
-struct LdsLoader {
-  __amdgpu_buffer_rsrc_t rsrc;
-  __device__ __forceinline__ LdsLoader(const unsigned char* base) : rsrc(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00020000)) {}
-  __device__ __forceinline__ void load(unsigned char* to, int lane, int scalar) const {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, lane, scalar, 0, 0);
-  }
-};
-
 template <bool I8, int GS, int TT, int WV>
 __global__ __launch_bounds__(64 * WV, 2) void linear_many_kernel(LinearArgs p, int token_tiles, int row_tiles) {
   using Tile = ManyTile<TT, WV>;
@@ -67,7 +58,6 @@ __global__ __launch_bounds__(64 * WV, 2) void linear_many_kernel(LinearArgs p, i
   // ---- activations: the wavefront's share of a stage's rows in NL loads.  The 16-byte chunks of a row are permuted so that 16
   // consecutive rows of one chunk lie in 16 different places of 256 bytes (all banks once).
   auto swizzle = [](int row) { return I8 ? (row >> 1) & 7 : row & 15; };
-  // (Buffer loads: behind a global load to LDS the compiler takes LDS reads to return in any order, and waits for all of them each time.)
   const LdsLoader xfrom((const unsigned char*)p.x + (int64_t)tok0 * p.ldx * (I8 ? 1 : 2));
   int xsrc[NL];
 #pragma unroll
