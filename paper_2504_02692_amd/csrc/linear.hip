@@ -5,7 +5,6 @@
 // per group of columns the sum of (code - zero) x is taken in fp32 (bf16 activations) or exactly in int32 (8-bit activations),
 // multiplied by the group's fp32 scale, and added to the fp32 total.  No weight is rounded.
 #include "linear.h"
-#include <stdlib.h>
 #include <type_traits>
 
 namespace gptaq {
@@ -68,38 +67,39 @@ __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t 
 
 // ---- few tokens
 //
-// Up to 16 tokens, one tile of v_mfma 16x16.  A workgroup takes RT tiles of 16 rows; its wavefronts share the tiles of 128 columns out
+// Up to 32 tokens, TT = 1 or 2 tiles of v_mfma 16x16.  A workgroup takes RT tiles of 16 rows; its wavefronts share the tiles of 128 columns out
 // among themselves and add their sums through LDS, in the wavefronts' order.  The weights go straight from memory to the lanes that
-// feed the matrix unit, two tiles of columns ahead: nothing of W is read twice, and with everything of a wavefront independent many
-// loads are in flight.  The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the result has the
-// row of W in l % 16 and tokens 4 (l / 16) .. + 3 in the lane's four values, so one scale per lane serves a result.
+// feed the matrix unit, two tiles of columns ahead (three or four ahead were slower: registers): nothing of W is read twice, and with everything of a
+// wavefront independent many loads are in flight.  The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the
+// result has the row of W in l % 16 and tokens 4 (l / 16) .. + 3 in the lane's four values, so one scale per lane serves a result.
+// Bound by the weights' bytes where there are many: 28672 x 8192, one token, 8-bit activations 23 us, 5.4 TB/s; bf16 28 to 30 us, where unpacking the codes
+// takes most of the time that the bytes leave.  4096 x 4096 4.2 us, 2.2 TB/s: the launch, one trip to memory and the join.
 // Activations go to LDS in runs of a token's whole 128 columns, to a place of the wavefront's own, so that no wavefront waits for another.  (A load of
 // 16 tokens by 64 bytes to registers takes about four times as long as one of 1 KB in one run: 4096 x 11008, 16 tokens, 14.5 us; through LDS 9.3.)
 // GS: groups per 128 columns (1, 2, 4), 0: one group per row.
 // Most wavefronts of a workgroup: 16 leave a lane 128 registers.
-constexpr int few_waves(int rt) { return rt > 1 ? 8 : 16; }
+constexpr int few_waves(int gs, int rt, int tt) { return rt > 1 || tt > 1 || gs == 4 ? 8 : 16; }
 
-template <bool I8, int GS, int RT>
-__global__ __launch_bounds__(64 * few_waves(RT)) void linear_few_kernel(LinearArgs p) {
+template <bool I8, int GS, int RT, int TT>
+__global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(LinearArgs p) {
   extern __shared__ __attribute__((aligned(256))) float lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int l16 = lane & 15, q = lane >> 4;
   const int rt0 = blockIdx.x * RT;
   constexpr int G = GS ? GS : 1;       // groups per tile of 128 columns
 
-  f32x4 total[RT], acc[RT];            // I8: acc holds the bits of int32
+  f32x4 total[TT][RT], acc[TT][RT];    // I8: acc holds the bits of int32
   const uint8_t* codes[RT];
   int64_t group[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    total[r] = acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int64_t tr = rt0 + r < p.mt ? rt0 + r : p.mt - 1;      // (past the last tile of rows: that one again; nothing of it is stored)
     codes[r] = p.codes + tr * p.kt * 1024 + lane * 16;
     group[r] = tr * p.groups * 16 + l16;
   }
   // The 16-byte chunks of a token's 128 columns are permuted so that 16 tokens' same chunk lies in 16 different places of 256 bytes.  Places of
   // tokens that there are not hold anything: their results are not stored.
-  constexpr int XROW = I8 ? 128 : 256, XSTAGE = 16 * XROW, CHUNKS = XROW / 16, PER_LOAD = 1024 / XROW, NL = 16 / PER_LOAD;
+  constexpr int XROW = I8 ? 128 : 256, XSTAGE = TT * 16 * XROW, CHUNKS = XROW / 16, PER_LOAD = 1024 / XROW, NL = TT * 16 / PER_LOAD;
   auto swizzle = [](int row) { return I8 ? (row >> 1) & 7 : row & 15; };
   unsigned char* const xlds = reinterpret_cast<unsigned char*>(lds) + wave * 2 * XSTAGE;
   const LdsLoader xfrom((const unsigned char*)p.x);
@@ -138,67 +138,80 @@ __global__ __launch_bounds__(64 * few_waves(RT)) void linear_few_kernel(LinearAr
   const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
   uint32_t sixteen = 0x41804180u;
   asm volatile("" : "+v"(sixteen));    // (in a register, where the mask and it are one instruction)
-  f32x4 accx;                          // sums of the group's activations (the same in all of a token's lanes)
+  f32x4 accx[TT];                      // sums of the group's activations (the same in all of a token's lanes)
   // EXACT: the products are those of code - zero.  Else (bf16 only): of 16 + code, which is two instructions for two codes where the difference
   // takes five, and (16 + zero) times the activations' sum, one more matrix instruction for all RT, is taken off each group's sum.
   // Where a result is not finite this subtraction may be why, and the workgroup takes its sums again with EXACT.
   auto add_scaled = [&](auto exact, int r, float s, uint32_t zero) {
     const float z = -16.f - (float)zero;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float v = I8 ? (float)__float_as_int(acc[r][e]) : acc[r][e];
-      if (!exact) v = fmaf(z, accx[e], v);
-      total[r][e] = fmaf(s, v, total[r][e]);
-    }
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float v = I8 ? (float)__float_as_int(acc[t][r][e]) : acc[t][r][e];
+        if (!exact) v = fmaf(z, accx[t][e], v);
+        total[t][r][e] = fmaf(s, v, total[t][r][e]);
+      }
   };
   auto multiply = [&](auto exact, const Stage& s, int place) {
     const f32x4 nothing = {0.f, 0.f, 0.f, 0.f};
     asm volatile("" :: "v"(s.w[RT - 1]) : "memory");
-    u32x4 all[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned char* row = xlds + place * XSTAGE + l16 * XROW;
-      if (I8) {
-        const u32x2 v = *reinterpret_cast<const u32x2*>(row + (((2 * i + (q >> 1)) ^ swizzle(l16)) << 4) + (q & 1) * 8);
-        all[i] = u32x4{v[0], v[1], 0u, 0u};
-      } else {
-        all[i] = *reinterpret_cast<const u32x4*>(row + (((4 * i + q) ^ swizzle(l16)) << 4));
-      }
-    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool first = GS && i % (4 / G) == 0, last = GS && (i + 1) % (4 / G) == 0;
-      u32x4 x = all[i];
-      if (!exact) {                    // columns 0 2 4 6 1 3 5 7, as the codes come out of a word
-        x = u32x4{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u), __builtin_amdgcn_perm(x[3], x[2], 0x05040100u),
-                  __builtin_amdgcn_perm(x[1], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
-        accx = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, ones), first ? nothing : accx, 0, 0, 0);
+      u32x4 x[TT];
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        const unsigned char* row = xlds + place * XSTAGE + (t * 16 + l16) * XROW;
+        if (I8) {
+          const u32x2 v = *reinterpret_cast<const u32x2*>(row + (((2 * i + (q >> 1)) ^ swizzle(l16)) << 4) + (q & 1) * 8);
+          x[t] = u32x4{v[0], v[1], 0u, 0u};
+        } else {
+          x[t] = *reinterpret_cast<const u32x4*>(row + (((4 * i + q) ^ swizzle(l16)) << 4));
+        }
+      }
+      if (!exact) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {  // columns 0 2 4 6 1 3 5 7, as the codes come out of a word
+          x[t] = u32x4{__builtin_amdgcn_perm(x[t][1], x[t][0], 0x05040100u), __builtin_amdgcn_perm(x[t][3], x[t][2], 0x05040100u),
+                       __builtin_amdgcn_perm(x[t][1], x[t][0], 0x07060302u), __builtin_amdgcn_perm(x[t][3], x[t][2], 0x07060302u)};
+          accx[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), __builtin_bit_cast(bf16x8, ones), first ? nothing : accx[t], 0, 0, 0);
+        }
       }
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const f32x4 c = first ? nothing : acc[r];
         const uint32_t w = s.w[r][i], zero = GS ? s.zero[r][i * G / 4] : row_zero[r];
+        u32x4 v;                         // the right operand (I8: two words)
         if (I8) {
-          acc[r] = __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x32_i8(
-              __builtin_bit_cast(long, u32x2{x[0], x[1]}), __builtin_bit_cast(long, linear_bytes(w, linear_offset(zero))),
-              __builtin_bit_cast(i32x4, c), 0, 0, 0));
+          const u32x2 b = linear_bytes(w, linear_offset(zero));
+          v[0] = b[0]; v[1] = b[1];
         } else if (exact) {
-          acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), linear_bf16(w, linear_offset(zero)), c, 0, 0, 0);
-        } else {
-          u32x4 v;                     // the code in the upper bits of the mantissa of 16
+          v = __builtin_bit_cast(u32x4, linear_bf16(w, linear_offset(zero)));
+        } else {                         // the code in the upper bits of the mantissa of 16
           const uint32_t shifted[4] = {w << 3, w >> 1, w >> 5, w >> 9};
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = (shifted[e] & 0x00780078u) | sixteen;
-          acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, v), c, 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          const f32x4 c = first ? nothing : acc[t][r];
+          if (I8)
+            acc[t][r] = __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, u32x2{x[t][0], x[t][1]}),
+                                                  __builtin_bit_cast(long, u32x2{v[0], v[1]}), __builtin_bit_cast(i32x4, c), 0, 0, 0));
+          else
+            acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), __builtin_bit_cast(bf16x8, v), c, 0, 0, 0);
         }
         if (last) add_scaled(exact, r, s.scale[r][i * G / 4], zero);
       }
     }
   };
   auto sums = [&](auto exact) {
-    accx = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int r = 0; r < RT; ++r) total[r] = acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < TT; ++t) {
+      accx[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < RT; ++r) total[t][r] = acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     Stage a, b, c;
     int k = wave;                      // (a workgroup has no more wavefronts than there are tiles)
     load(a, k, 0);
@@ -219,19 +232,24 @@ __global__ __launch_bounds__(64 * few_waves(RT)) void linear_few_kernel(LinearAr
       for (int r = 0; r < RT; ++r) add_scaled(exact, r, p.scales[group[r]], row_zero[r]);
     }
   };
-  // Joins the wavefronts' sums, [wave][r][lane][4], and stores; returns whether a sum of this thread's is not finite.
-  auto finish = [&]() {
+  // Joins the wavefronts' sums, [wave][t][r][lane][4], and stores those of this thread's results that `wanted` has a bit for; returns which are not
+  // finite.  (A second pass replaces these alone: the other tokens' results do not depend on them.)
+  auto finish = [&](uint64_t wanted) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(&lds[((wave * RT + r) * 64 + lane) * 4]) = total[r];
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) *reinterpret_cast<f32x4*>(&lds[(((wave * TT + t) * RT + r) * 64 + lane) * 4]) = total[t][r];
     __syncthreads();
-    bool lost = false;
-    for (int at = threadIdx.x; at < RT * 256; at += blockDim.x) {
+    uint64_t lost = 0;
+    int bit = 0;
+    for (int at = threadIdx.x; at < TT * RT * 256; at += blockDim.x, ++bit) {
       // 16 RT rows of W in a run of threads, so that a token's outputs are written together
       const int r = at % (16 * RT), tok = at / (16 * RT), row = rt0 * 16 + r;
-      if (row >= p.m || tok >= p.tokens) continue;
+      if (row >= p.m || tok >= p.tokens || !(wanted >> bit & 1)) continue;
+      const int slot = (((tok >> 4) * RT + (r >> 4)) * 64 + (tok & 15) / 4 * 16 + (r & 15)) * 4 + (tok & 3);
       float v = 0.f;
-      for (int w = 0; w < waves; ++w) v += lds[w * RT * 256 + ((r >> 4) * 64 + (tok >> 2) * 16 + (r & 15)) * 4 + (tok & 3)];
-      lost |= !(fabsf(v) < __builtin_inff());
+      for (int w = 0; w < waves; ++w) v += lds[w * TT * RT * 256 + slot];
+      if (!(fabsf(v) < __builtin_inff())) lost |= 1ull << bit;
       if (I8) v *= p.xs[tok];
       if (p.bias) v += p.bias[row];
       const int64_t o = (int64_t)tok * p.ldy + row;
@@ -241,29 +259,45 @@ __global__ __launch_bounds__(64 * few_waves(RT)) void linear_few_kernel(LinearAr
     return lost;
   };
   sums(std::integral_constant<bool, I8>{});
-  const bool lost = finish();
-  if (!I8 && __syncthreads_or(lost)) {
+  static_assert(TT * RT * 256 / 64 <= 64, "a bit for each of a thread's results");
+  const uint64_t lost = finish(~0ull);
+  if (!I8 && __syncthreads_or(lost != 0)) {
     sums(std::true_type{});
-    finish();
+    finish(lost);
   }
 }
 
-template <bool I8, int GS, int RT>
+template <bool I8, int GS, int RT, int TT>
 static hipError_t launch_few_as(const LinearArgs& p, int waves, hipStream_t s) {
-  if (waves > few_waves(RT)) waves = few_waves(RT);
+  if (waves > few_waves(GS, RT, TT)) waves = few_waves(GS, RT, TT);
   while (waves > 1 && waves > p.kt) waves /= 2;
-  constexpr int kStages = 2 * 16 * (I8 ? 128 : 256), kPerWave = kStages > RT * 1024 ? kStages : RT * 1024;
+  constexpr int kStages = 2 * TT * 16 * (I8 ? 128 : 256), kSums = TT * RT * 1024, kPerWave = kStages > kSums ? kStages : kSums;
   static LdsLimitOnce once;
-  if (const hipError_t e = once.ensure((const void*)&linear_few_kernel<I8, GS, RT>, few_waves(RT) * kPerWave); e != hipSuccess) return e;
-  hipLaunchKernelGGL((linear_few_kernel<I8, GS, RT>), dim3((unsigned)((p.mt + RT - 1) / RT)), dim3(64 * waves), (size_t)(waves * kPerWave), s, p);
+  if (const hipError_t e = once.ensure((const void*)&linear_few_kernel<I8, GS, RT, TT>, few_waves(GS, RT, TT) * kPerWave); e != hipSuccess) return e;
+  hipLaunchKernelGGL((linear_few_kernel<I8, GS, RT, TT>), dim3((unsigned)((p.mt + RT - 1) / RT)), dim3(64 * waves), (size_t)(waves * kPerWave), s, p);
   return hipGetLastError();
+}
+// Tiles of rows per workgroup: the more, the less often the activations are read, the fewer workgroups.  us a call, RT 1 (8 wavefronts) / 2 (4, 8) / 4 (4):
+//              4096 x 4096          11008 x 4096               8192 x 8192                28672 x 8192
+//   1, bf16    4.2 / 6.7 5.4 / 8.7  8.7 / 8.6  8.6  / 9.5      9.7 / 11.4 9.2  / 15.1     35.8 / 31.2 29.6 / 29.9
+//   1, int8    3.4 / 5.7 4.6 / 7.6  6.6 / 7.0  7.2  / 8.2      8.1 / 9.4  8.1  / 13.1     23.3 / 25.3 24.4 / 25.1
+//   16, bf16   5.1 / 7.4 6.2 / 10   10.1 / 9.6 9.6  / 10.7     12.0 / 12.4 10.6 / 16.9    44.3 / 35.1 35.1 / 31.5
+//   16, int8   3.7 / 6.1 4.9 / 8.6  6.8 / 7.6  7.8  / 9.4      8.6 / 10.1 8.7  / 14.2     32.8 / 28.1 28.1 / 27.4
+//   32, bf16   7.5 / 10.4 8.3 / 14  17.6 / 13.9 15.6 / 15.6    19.9 / 17.8 14.3 / 23.4    77.6 / 50.3 54.9 / 42.6
+//   32, int8   5.2 / 7.8 6.2 / 11   9.4 / 9.8  9.6  / 12.0     10.9 / 12.6 10.5 / 18.7    43.0 / 35.5 35.2 / 32.5
+// 16 wavefronts instead of 8, RT 1, one token: 4096 x 11008 8.0 -> 7.6, 1024 x 8192 5.3 -> 5.2, 4096 x 4096 4.2 -> 4.4, 11008 x 4096 8.7 -> 11.2.
+// With more scales a tile, fewer tiles fit in the registers.
+template <bool I8, int GS, int TT>
+static hipError_t launch_few_rows(const LinearArgs& p, hipStream_t s) {
+  constexpr int kMost = GS <= 1 ? 4 : GS == 2 ? (TT == 1 ? 4 : 2) : (TT == 1 ? 2 : 1), kTwo = kMost < 2 ? kMost : 2;
+  if (p.mt >= 1024 && !(I8 && p.tokens <= 8)) return launch_few_as<I8, GS, kMost, TT>(p, kMost == 1 ? 8 : 4, s);
+  if constexpr (!I8)
+    if (p.mt >= 512) return launch_few_as<I8, GS, kTwo, TT>(p, kTwo == 1 || p.kt >= 64 ? 8 : 4, s);
+  return launch_few_as<I8, GS, 1, TT>(p, p.mt < 512 && p.kt >= 64 ? 16 : 8, s);
 }
 template <bool I8, int GS>
 static hipError_t launch_few_of(const LinearArgs& p, hipStream_t s) {
-  static const char* e1 = getenv("FEW_RT"); static const char* e2 = getenv("FEW_W");
-  const int rt = e1 ? atoi(e1) : 1, waves = e2 ? atoi(e2) : 8;
-  if (rt == 4) return launch_few_as<I8, GS == 4 ? 2 : GS, 4>(p, waves, s);
-  return rt == 2 ? launch_few_as<I8, GS, 2>(p, waves, s) : launch_few_as<I8, GS, 1>(p, waves, s);
+  return p.tokens <= 16 ? launch_few_rows<I8, GS, 1>(p, s) : launch_few_rows<I8, GS, 2>(p, s);
 }
 template <bool I8>
 static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
@@ -271,7 +305,7 @@ static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
 }
 
 static hipError_t launch_linear(const LinearArgs& p, int gs, bool i8, float* partial, hipStream_t s) {
-  if (p.tokens > 16) return launch_linear_many(p, gs, i8, partial, s);
+  if (p.tokens > 32) return launch_linear_many(p, gs, i8, partial, s);
   return i8 ? launch_few<true>(p, gs, s) : launch_few<false>(p, gs, s);
 }
 

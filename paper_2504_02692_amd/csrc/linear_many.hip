@@ -13,7 +13,7 @@ typedef __attribute__((ext_vector_type(16))) int32_t i32x16;
 // A byte of W feeds four times the products that a byte of bf16 activations does, so the tile is taller in W.
 // Activations go from memory straight to LDS, 128 columns (a stage) at a time, in a ring of four stages with one barrier a stage, in
 // its middle: it publishes the next stage (whose first fragments are read before the stage ends) and retires the one before.
-// TT tiles of 32 tokens (4, or 1 and 2 where there are no more tokens) and WV wavefronts; with fewer tokens than 128 several workgroups
+// TT tiles of 32 tokens (4, or 2 where there are few tokens or tiles) and WV wavefronts; with fewer tokens than 128 several workgroups
 // share a CU.  A result that too few workgroups would share is taken in parts of the columns, each by workgroups of its own: their sums
 // go to p.partial, and linear_join_kernel adds them in order.
 constexpr int kXRing = 4;
@@ -295,13 +295,13 @@ template <int TT, int WV> static hipError_t launch_many_of(const LinearArgs& p, 
 // 4096 x 1024, 257 tokens 17.0 / 10.6 (384), 1024 19.2 / 16.4 (1024), 2048 23.2 / 28.5 (2048, 256 tiles); 8-bit activations a little more for the small ones.
 static void many_tile(int64_t tokens, int64_t m, int64_t n, int& tt, int& wv) {
   const int64_t large = (tokens + 127) / 128 * ((m + 255) / 256), kt = (n + 127) / 128;
-  tt = tokens <= 32 ? 1 : tokens <= 64 || (large <= 128 && large * kt <= 3072) ? 2 : 4;
+  tt = tokens <= 64 || (large <= 128 && large * kt <= 3072) ? 2 : 4;
   wv = tt == 4 ? 8 : 4;
 }
 // Parts that the columns are taken in: as many as leave room for 512 workgroups of four wavefronts (two a CU) or 256 of eight, of at least eight
-// stages each (four up to 64 tokens, where joining them is cheap).  On 4096 x 4096, 11008 x 4096, 4096 x 11008, 28672 x 8192 and 1024 x 8192, 17 to 1024
-// tokens: room for 256 (128) instead takes 1.0 to 1.7 times as long, for 1024 (512) 0.9 to 1.8 times.  Stages, 8 / 4: 4096 x 4096, 17 tokens 13.7 /
-// 12.3, 4096 x 1024, 512 tokens 12.0 / 19.2, 1024 x 4096, 512 tokens 17.6 / 19.1.
+// stages each (four up to 64 tokens, where joining them is cheap).  On 4096 x 4096, 11008 x 4096, 4096 x 11008, 28672 x 8192 and 1024 x 8192, 33 to 1024
+// tokens: room for 256 (128) instead takes 1.0 to 1.7 times as long, for 1024 (512) 0.9 to 1.8 times.  Stages, 8 / 4: 4096 x 4096, 33 tokens 15.0 /
+// 13.9, 4096 x 1024, 512 tokens 12.0 / 19.2, 1024 x 4096, 512 tokens 17.6 / 19.1.
 static int64_t many_room(int tt) { return tt == 4 ? 256 : 512; }
 static int64_t most_parts(int64_t tokens, int64_t n) { return (n + 127) / 128 / (tokens <= 64 ? 4 : 8); }
 static int64_t many_parts(int64_t tokens, int64_t m, int64_t n) {
@@ -315,8 +315,8 @@ static int64_t many_parts(int64_t tokens, int64_t m, int64_t n) {
 size_t linear_partial_bytes(int64_t tokens, int64_t m, int64_t n) {
   const int64_t ld = (m + 7) / 8 * 8;
   int64_t rows = 0;                                        // of ld floats
-  for (const int tt : {1, 2, 4}) {
-    const int64_t least = tt == 1 ? 17 : 16 * tt + 1, each = many_room(tt) / ((m + 64 * (tt == 4 ? 4 : 2) - 1) / (64 * (tt == 4 ? 4 : 2)));
+  for (const int tt : {2, 4}) {
+    const int64_t least = 16 * tt + 1, each = many_room(tt) / ((m + 64 * (tt == 4 ? 4 : 2) - 1) / (64 * (tt == 4 ? 4 : 2)));
     for (const int64_t t : {tokens < 64 ? tokens : (int64_t)64, tokens}) {
       if (t < least || each < 2 || most_parts(t, n) < 2) continue;
       const int64_t need = each * 32 * tt < most_parts(t, n) * t ? each * 32 * tt : most_parts(t, n) * t;
@@ -332,7 +332,7 @@ hipError_t launch_linear_many(LinearArgs p, int gs, bool i8, float* partial, hip
   p.parts = (int32_t)many_parts(p.tokens, p.m, (int64_t)p.kt * 128);
   p.partial = partial;
   p.ld_partial = (p.m + 7) / 8 * 8;
-  return tt == 1 ? launch_many_of<1, 4>(p, gs, i8, s) : tt == 2 ? launch_many_of<2, 4>(p, gs, i8, s) : launch_many_of<4, 8>(p, gs, i8, s);
+  return tt == 2 ? launch_many_of<2, 4>(p, gs, i8, s) : launch_many_of<4, 8>(p, gs, i8, s);
 }
 
 }  // namespace gptaq

@@ -163,7 +163,7 @@ def test_linear_extremes_of_8_bits(tokens, i8):
                 assert torch.all(Y == float(v * (c - z) * n)), (group, c, z, v, Y[0, 0].item())
 
 
-@pytest.mark.parametrize("tokens", [1, 40, 300])
+@pytest.mark.parametrize("tokens", [1, 7, 16, 30, 40, 300])
 def test_linear_keeps_tokens_apart_and_passes_on_what_is_not_finite(tokens):
     """A token with an infinity or a NaN spoils its own outputs alone; an infinity meets weights of either sign."""
     m, n, group = 48, 256, 64
