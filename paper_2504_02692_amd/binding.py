@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import NamedTuple, Optional
+from typing import Optional
 
 import torch
 
@@ -139,7 +139,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _need(t: torch.Tensor, dtype, name: str) -> None:
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.stride(1) != 1:
+    if not t.is_cuda or t.dtype is not dtype or t.dim() != 2 or t.stride(1) != 1:
         raise GptaqError(f"{name}: expected a 2-D row-major {dtype} CUDA tensor")
 
 
@@ -416,15 +416,15 @@ def gptaq_pack_codes(codes: torch.Tensor, bits: int) -> torch.Tensor:
 
 # ---- running quantised layers
 
-class LinearWeights(NamedTuple):
-    """A layer's weights as gptaq_linear and gptaq_linear_i8 read them."""
-    data: torch.Tensor
-    m: int
-    n: int
-    group: int                                   # 0: one group per row
-    perm: Optional[torch.Tensor]
-    bias: Optional[torch.Tensor]
-    info: torch.Tensor                           # int32 of 1, on the GPU: 0, or 1 + a row whose codes or zeros do not fit in 4 bits
+class LinearWeights:
+    """A layer's weights as gptaq_linear and gptaq_linear_i8 read them: data (uint8), m, n, group (0: one per row), perm, bias, and info,
+    an int32 on the GPU that is 0, or 1 + a row whose codes or zeros do not fit in 4 bits."""
+    __slots__ = ("data", "m", "n", "group", "perm", "bias", "info", "_args")
+
+    def __init__(self, data: torch.Tensor, m: int, n: int, group: int, perm: Optional[torch.Tensor], bias: Optional[torch.Tensor],
+                 info: torch.Tensor):
+        self.data, self.m, self.n, self.group, self.perm, self.bias, self.info = data, m, n, group, perm, bias, info
+        self._args = (_ptr(perm), _ptr(data), m, n, group, _ptr(bias))           # as the C calls take them, in order
 
 
 def gptaq_linear_weights_bytes(m: int, n: int, group: int) -> int:
@@ -461,14 +461,15 @@ def gptaq_linear_workspace_bytes(tokens: int, m: int, n: int) -> int:
 
 
 def _linear_out(X: torch.Tensor, w: LinearWeights, dtype, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
-    if X.shape[1] != w.n:
-        raise GptaqError(f"{name}: X has {X.shape[1]} columns, the weights {w.n}")
+    tokens, n = X.shape
+    if n != w.n:
+        raise GptaqError(f"{name}: X has {n} columns, the weights {w.n}")
     if out is None:
-        if dtype not in (torch.bfloat16, torch.float32):
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise GptaqError(f"{name}: the output is bfloat16 or float32")
-        return torch.empty((X.shape[0], w.m), dtype=dtype, device=X.device)
-    _need(out, out.dtype if out.dtype == torch.float32 else torch.bfloat16, "out")
-    if out.shape != (X.shape[0], w.m):
+        return X.new_empty((tokens, w.m), dtype=dtype)
+    _need(out, torch.float32 if out.dtype is torch.float32 else torch.bfloat16, "out")
+    if out.shape != (tokens, w.m):
         raise GptaqError(f"{name}: out: shape mismatch")
     return out
 
@@ -478,9 +479,9 @@ def gptaq_linear(X: torch.Tensor, weights: LinearWeights, ws: torch.Tensor, out:
     """X W^T + bias for token-major bf16 X; returns (tokens x m), bf16 or fp32 (`dtype`, or the type of `out`)."""
     _need(X, torch.bfloat16, "X")
     Y = _linear_out(X, weights, dtype, out, "gptaq_linear")
-    _check(load().gptaq_linear(_ptr(X), X.shape[0], X.stride(0), _ptr(weights.perm), _ptr(weights.data), weights.m, weights.n, weights.group,
-                               _ptr(weights.bias), _ptr(Y), Y.stride(0), int(Y.dtype == torch.float32), _ptr(ws),
-                               ws.numel() * ws.element_size(), _stream()), "gptaq_linear")
+    perm, data, m, n, group, bias = weights._args
+    _check(load().gptaq_linear(X.data_ptr(), X.shape[0], X.stride(0), perm, data, m, n, group, bias, Y.data_ptr(), Y.stride(0),
+                               Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear")
     return Y
 
 
@@ -488,12 +489,12 @@ def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWe
                     out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
     """gptaq_linear for 8-bit activations scales[t] * codes[t][:]."""
     _need(codes, torch.int8, "codes"); _need_vec(scales, torch.float32, "scales")
-    if scales.numel() != codes.shape[0]:
+    if scales.shape[0] != codes.shape[0]:
         raise GptaqError("gptaq_linear_i8: scales: expected one per token")
     Y = _linear_out(codes, weights, dtype, out, "gptaq_linear_i8")
-    _check(load().gptaq_linear_i8(_ptr(codes), _ptr(scales), codes.shape[0], codes.stride(0), _ptr(weights.perm), _ptr(weights.data),
-                                  weights.m, weights.n, weights.group, _ptr(weights.bias), _ptr(Y), Y.stride(0),
-                                  int(Y.dtype == torch.float32), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "gptaq_linear_i8")
+    perm, data, m, n, group, bias = weights._args
+    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.stride(0), perm, data, m, n, group, bias,
+                                  Y.data_ptr(), Y.stride(0), Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear_i8")
     return Y
 
 
@@ -543,8 +544,7 @@ def gptaq_rms_norm_i8(X: torch.Tensor, weight: Optional[torch.Tensor], eps: floa
     """(codes, scales, total): gptaq_rms_norm with its output as 8-bit codes and a scale per token."""
     total = _norm_args(X, weight, residual, total, "gptaq_rms_norm_i8")
     tokens, n = X.shape
-    codes = torch.empty((tokens, n), dtype=torch.int8, device=X.device)
-    scales = torch.empty(tokens, dtype=torch.float32, device=X.device)
+    codes, scales = X.new_empty((tokens, n), dtype=torch.int8), X.new_empty(tokens, dtype=torch.float32)
     _check(load().gptaq_rms_norm_i8(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, X.stride(0), residual.stride(0) if residual is not None else 0,
                                     float(eps), _ptr(total), total.stride(0) if total is not None else 0, float(clip), _ptr(codes), n,
                                     _ptr(scales), _stream()), "gptaq_rms_norm_i8")
@@ -570,8 +570,7 @@ def gptaq_silu_mul_i8(gate: torch.Tensor, up: torch.Tensor, clip: float = 1.0):
     """(codes, scales): silu(gate) * up as 8-bit codes and a scale per token."""
     _gated_args(gate, up, "gptaq_silu_mul_i8")
     tokens, n = gate.shape
-    codes = torch.empty((tokens, n), dtype=torch.int8, device=gate.device)
-    scales = torch.empty(tokens, dtype=torch.float32, device=gate.device)
+    codes, scales = gate.new_empty((tokens, n), dtype=torch.int8), gate.new_empty(tokens, dtype=torch.float32)
     _check(load().gptaq_silu_mul_i8(_ptr(gate), _ptr(up), tokens, n, gate.stride(0), up.stride(0), float(clip), _ptr(codes), n, _ptr(scales),
                                     _stream()), "gptaq_silu_mul_i8")
     return codes, scales
