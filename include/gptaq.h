@@ -285,6 +285,8 @@ int gptaq_pack_codes(const uint8_t* codes, int64_t m, int64_t n, int64_t ldc, in
  *   info   : int32, out: 0, or 1 + the last row with a code above 15 or a zero that is no integer in 0 .. 15 (the
  *            weights are then garbage).
  * gptaq_linear, gptaq_linear_i8: Y[t][r] = sum_j scale[r][j / group] (code[r][j] - zero[r][j / group]) x[t][p(j)] + bias[r].
+ *   weights, weights_bytes, m, n, group: as given to gptaq_linear_pack; fewer bytes than these sizes take are refused
+ *            (GPTAQ_EWORKSPACE), whatever else does not fit them gives garbage.
  *   perm   : n x int32 or NULL: p(j) = perm[j], for codes in the order of gptaq_act_order (Wp = W[:, perm], the order in
  *            which the solve returns them); NULL: p(j) = j.  An entry outside 0 .. n - 1 stands for an activation of 0.
  *   bias   : m x fp32 or NULL.
@@ -298,12 +300,12 @@ size_t gptaq_linear_weights_bytes(int64_t m, int64_t n, int group);
 int gptaq_linear_pack(const uint8_t* codes, int64_t ldc, const float* scales, const float* zeros, int64_t m, int64_t n,
                       int group, void* weights, size_t weights_bytes, int32_t* info, void* stream);
 size_t gptaq_linear_workspace_bytes(int64_t tokens, int64_t m, int64_t n);
-int gptaq_linear(const uint16_t* X, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights, int64_t m,
-                 int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes,
-                 void* stream);
+int gptaq_linear(const uint16_t* X, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights,
+                 size_t weights_bytes, int64_t m, int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32,
+                 void* ws, size_t ws_bytes, void* stream);
 int gptaq_linear_i8(const int8_t* X, const float* x_scales, int64_t tokens, int64_t ldx, const int32_t* perm,
-                    const void* weights, int64_t m, int64_t n, int group, const float* bias, void* Y, int64_t ldy,
-                    int y_f32, void* ws, size_t ws_bytes, void* stream);
+                    const void* weights, size_t weights_bytes, int64_t m, int64_t n, int group, const float* bias, void* Y,
+                    int64_t ldy, int y_f32, void* ws, size_t ws_bytes, void* stream);
 
 /* gptaq_rms_norm: h = X + residual (X alone if residual is NULL), Y = h * weight / sqrt(mean(h^2) + eps) over each row's n
  *   columns; weight: n x bf16 or NULL for ones (rotated models have theirs in the next layer's weights).  sum, if not

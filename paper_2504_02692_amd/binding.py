@@ -71,10 +71,10 @@ _SIGS = {
     "gptaq_linear_pack": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int, _c.c_void_p,
                                      _c.c_size_t, _c.c_void_p, _c.c_void_p]),
     "gptaq_linear_workspace_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int64, _c.c_int64]),
-    "gptaq_linear": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int, _c.c_void_p,
-                                _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
-    "gptaq_linear_i8": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64,
-                                   _c.c_int, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "gptaq_linear": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_size_t, _c.c_int64, _c.c_int64, _c.c_int,
+                                _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "gptaq_linear_i8": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_size_t, _c.c_int64,
+                                   _c.c_int64, _c.c_int, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "gptaq_rms_norm": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float,
                                   _c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_void_p]),
     "gptaq_rms_norm_i8": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float,
@@ -424,7 +424,7 @@ class LinearWeights:
     def __init__(self, data: torch.Tensor, m: int, n: int, group: int, perm: Optional[torch.Tensor], bias: Optional[torch.Tensor],
                  info: torch.Tensor):
         self.data, self.m, self.n, self.group, self.perm, self.bias, self.info = data, m, n, group, perm, bias, info
-        self._args = (_ptr(perm), _ptr(data), m, n, group, _ptr(bias))           # as the C calls take them, in order
+        self._args = (_ptr(perm), _ptr(data), data.nbytes, m, n, group, _ptr(bias))           # as the C calls take them, in order
 
 
 def gptaq_linear_weights_bytes(m: int, n: int, group: int) -> int:
@@ -479,8 +479,7 @@ def gptaq_linear(X: torch.Tensor, weights: LinearWeights, ws: torch.Tensor, out:
     """X W^T + bias for token-major bf16 X; returns (tokens x m), bf16 or fp32 (`dtype`, or the type of `out`)."""
     _need(X, torch.bfloat16, "X")
     Y = _linear_out(X, weights, dtype, out, "gptaq_linear")
-    perm, data, m, n, group, bias = weights._args
-    _check(load().gptaq_linear(X.data_ptr(), X.shape[0], X.stride(0), perm, data, m, n, group, bias, Y.data_ptr(), Y.stride(0),
+    _check(load().gptaq_linear(X.data_ptr(), X.shape[0], X.stride(0), *weights._args, Y.data_ptr(), Y.stride(0),
                                Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear")
     return Y
 
@@ -492,9 +491,8 @@ def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWe
     if scales.shape[0] != codes.shape[0]:
         raise GptaqError("gptaq_linear_i8: scales: expected one per token")
     Y = _linear_out(codes, weights, dtype, out, "gptaq_linear_i8")
-    perm, data, m, n, group, bias = weights._args
-    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.stride(0), perm, data, m, n, group, bias,
-                                  Y.data_ptr(), Y.stride(0), Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear_i8")
+    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.stride(0), *weights._args, Y.data_ptr(),
+                                  Y.stride(0), Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear_i8")
     return Y
 
 

@@ -320,14 +320,15 @@ static int64_t padded_columns(int64_t n) { return (n + 127) / 128 * 128; }
 
 static size_t gather_bytes(int64_t tokens, int64_t n) { return ((size_t)tokens * padded_columns(n) * 2 + 255) / 256 * 256; }
 
-static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights, int64_t m,
-                      int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes, void* stream) {
+static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights, size_t weights_bytes,
+                      int64_t m, int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes, void* stream) {
   if (!weights || (tokens != 0 && (!X || !Y || !ws || (i8 && !xs)))) return GPTAQ_ENULL;      // (no tokens: nothing to point to)
   const uintptr_t y_align = y_f32 ? 3 : 1;
   if (tokens < 0 || tokens > kMaxTokens || m <= 0 || n <= 0 || m > kMaxSide || n > kMaxSide || ldx < n || ldy < m ||
       ((uintptr_t)weights & 255) || ((uintptr_t)Y & y_align) || (!i8 && ((uintptr_t)X & 1)) || (((uintptr_t)xs | (uintptr_t)bias | (uintptr_t)perm) & 3))
     return GPTAQ_EDIM;
   if (!good_group(n, group)) return GPTAQ_EUNSUPPORTED;
+  if (weights_bytes < linear_layout(m, n, group > 0 ? group : 0).bytes) return GPTAQ_EWORKSPACE;
   if (tokens == 0) return GPTAQ_OK;
   if (((uintptr_t)ws & 255) || ws_bytes < gptaq_linear_workspace_bytes(tokens, m, n)) return GPTAQ_EWORKSPACE;
   if (group < 0) group = 0;
@@ -398,13 +399,13 @@ extern "C" size_t gptaq_linear_workspace_bytes(int64_t tokens, int64_t m, int64_
   return gather_bytes(tokens, n) + (linear_partial_bytes(tokens, m, n) + 255) / 256 * 256;
 }
 
-extern "C" int gptaq_linear(const uint16_t* X, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights, int64_t m, int64_t n,
-                            int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes, void* stream) {
-  return run_linear(false, X, nullptr, tokens, ldx, perm, weights, m, n, group, bias, Y, ldy, y_f32, ws, ws_bytes, stream);
+extern "C" int gptaq_linear(const uint16_t* X, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights, size_t weights_bytes,
+                            int64_t m, int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes, void* stream) {
+  return run_linear(false, X, nullptr, tokens, ldx, perm, weights, weights_bytes, m, n, group, bias, Y, ldy, y_f32, ws, ws_bytes, stream);
 }
 
 extern "C" int gptaq_linear_i8(const int8_t* X, const float* x_scales, int64_t tokens, int64_t ldx, const int32_t* perm, const void* weights,
-                               int64_t m, int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes,
+                               size_t weights_bytes, int64_t m, int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes,
                                void* stream) {
-  return run_linear(true, X, x_scales, tokens, ldx, perm, weights, m, n, group, bias, Y, ldy, y_f32, ws, ws_bytes, stream);
+  return run_linear(true, X, x_scales, tokens, ldx, perm, weights, weights_bytes, m, n, group, bias, Y, ldy, y_f32, ws, ws_bytes, stream);
 }

@@ -51,15 +51,16 @@ def test_pack_refusals(lib):
 def test_linear_refusals(lib):
     big = 1 << 30
 
-    def both(want, x=ONE, xs=ONE, tokens=4, ldx=128, perm=NULL, w=ONE, m=16, n=128, group=128, bias=NULL, y=ONE, ldy=16, f32=0, ws=ONE, nb=big):
-        assert lib.gptaq_linear(x, tokens, ldx, perm, w, m, n, group, bias, y, ldy, f32, ws, nb, NULL) == want
-        assert lib.gptaq_linear_i8(x, xs, tokens, ldx, perm, w, m, n, group, bias, y, ldy, f32, ws, nb, NULL) == want
+    def both(want, x=ONE, xs=ONE, tokens=4, ldx=128, perm=NULL, w=ONE, wb=big, m=16, n=128, group=128, bias=NULL, y=ONE, ldy=16, f32=0, ws=ONE,
+             nb=big):
+        assert lib.gptaq_linear(x, tokens, ldx, perm, w, wb, m, n, group, bias, y, ldy, f32, ws, nb, NULL) == want
+        assert lib.gptaq_linear_i8(x, xs, tokens, ldx, perm, w, wb, m, n, group, bias, y, ldy, f32, ws, nb, NULL) == want
 
     both(-1, x=NULL)
     both(-1, w=NULL)
     both(-1, y=NULL)
     both(-1, ws=NULL)
-    assert lib.gptaq_linear_i8(ONE, NULL, 4, 128, NULL, ONE, 16, 128, 128, NULL, ONE, 16, 0, ONE, big, NULL) == -1
+    assert lib.gptaq_linear_i8(ONE, NULL, 4, 128, NULL, ONE, big, 16, 128, 128, NULL, ONE, 16, 0, ONE, big, NULL) == -1
     both(-2, tokens=-1)
     both(-2, tokens=(1 << 23) + 1)
     both(-2, ldx=127)
@@ -74,9 +75,12 @@ def test_linear_refusals(lib):
     both(-3, group=16)
     both(-3, n=120, group=32)
     both(-4, nb=512)
+    both(-4, wb=lib.gptaq_linear_weights_bytes(16, 128, 128) - 1)                # weights of another size
+    both(-4, wb=lib.gptaq_linear_weights_bytes(16, 128, 128), group=32)
+    both(-4, tokens=0, wb=0)
     both(-4, ws=ctypes.c_void_p(264))
     both(0, tokens=0)                                                             # nothing to do
-    assert lib.gptaq_linear(ODD, 4, 128, NULL, ONE, 16, 128, 128, NULL, ONE, 16, 0, ONE, big, NULL) == -2
+    assert lib.gptaq_linear(ODD, 4, 128, NULL, ONE, big, 16, 128, 128, NULL, ONE, 16, 0, ONE, big, NULL) == -2
 
 
 def test_row_refusals(lib):
