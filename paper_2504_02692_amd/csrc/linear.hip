@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t 
 
 // ---- few tokens
 //
-// Up to 32 tokens, TT = 1 or 2 tiles of v_mfma 16x16.  A workgroup takes RT tiles of 16 rows; its wavefronts share the tiles of 128 columns out
+// TT = 1 or 2 tiles of v_mfma 16x16: 16 or 32 tokens at a time.  A workgroup takes RT tiles of 16 rows; its wavefronts share the tiles of 128 columns out
 // among themselves and add their sums through LDS, in the wavefronts' order.  The weights go straight from memory to the lanes that
 // feed the matrix unit, two tiles of columns ahead (three or four ahead were slower: registers): nothing of W is read twice, and with everything of a
 // wavefront independent many loads are in flight.  The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the
@@ -77,6 +77,7 @@ __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t 
 // Activations go to LDS in runs of a token's whole 128 columns, to a place of the wavefront's own, so that no wavefront waits for another.  (A load of
 // 16 tokens by 64 bytes to registers takes about four times as long as one of 1 KB in one run: 4096 x 11008, 16 tokens, 14.5 us; through LDS 9.3.)
 // GS: groups per 128 columns (1, 2, 4), 0: one group per row.
+
 // Most wavefronts of a workgroup: 16 leave a lane 128 registers.
 constexpr int few_waves(int gs, int rt, int tt) { return rt > 1 || tt > 1 || gs == 4 ? 8 : 16; }
 
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
   extern __shared__ __attribute__((aligned(256))) float lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int l16 = lane & 15, q = lane >> 4;
-  const int rt0 = blockIdx.x * RT;
+  const int rt0 = blockIdx.x * RT, tok0 = blockIdx.y * TT * 16, tokens = min(p.tokens - tok0, TT * 16);
   constexpr int G = GS ? GS : 1;       // groups per tile of 128 columns
 
   f32x4 total[TT][RT], acc[TT][RT];    // I8: acc holds the bits of int32
@@ -102,21 +103,22 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
   constexpr int XROW = I8 ? 128 : 256, XSTAGE = TT * 16 * XROW, CHUNKS = XROW / 16, PER_LOAD = 1024 / XROW, NL = TT * 16 / PER_LOAD;
   auto swizzle = [](int row) { return I8 ? (row >> 1) & 7 : row & 15; };
   unsigned char* const xlds = reinterpret_cast<unsigned char*>(lds) + wave * 2 * XSTAGE;
-  const LdsLoader xfrom((const unsigned char*)p.x);
+  const LdsLoader xfrom((const unsigned char*)p.x + (int64_t)tok0 * p.ldx * (I8 ? 1 : 2));
   int xsrc[NL];
 #pragma unroll
   for (int j = 0; j < NL; ++j) {
     const int row = j * PER_LOAD + lane / CHUNKS;
-    xsrc[j] = min(row, p.tokens - 1) * (int)p.ldx * (I8 ? 1 : 2) + ((lane % CHUNKS ^ swizzle(row)) << 4);
+    xsrc[j] = min(row, tokens - 1) * (int)p.ldx * (I8 ? 1 : 2) + ((lane % CHUNKS ^ swizzle(row)) << 4);
   }
 
   struct Stage { u32x4 w[RT]; uint32_t zero[RT][G]; float scale[RT][G]; };
   auto load = [&](Stage& s, int k, int place) {
-    // the activations first: where the weights are there, so are they
+    // The activations first: where the weights are there, so are they.  The place's last reads are over.
     asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);          // lgkmcnt == 0
 #pragma unroll
     for (int j = 0; j < NL; ++j)
-      if (j == 0 || j * PER_LOAD < p.tokens) xfrom.load(xlds + place * XSTAGE + j * 1024, xsrc[j], __builtin_amdgcn_readfirstlane(k * XROW));
+      if (j == 0 || j * PER_LOAD < tokens) xfrom.load(xlds + place * XSTAGE + j * 1024, xsrc[j], __builtin_amdgcn_readfirstlane(k * XROW));
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -245,14 +247,14 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
     for (int at = threadIdx.x; at < TT * RT * 256; at += blockDim.x, ++bit) {
       // 16 RT rows of W in a run of threads, so that a token's outputs are written together
       const int r = at % (16 * RT), tok = at / (16 * RT), row = rt0 * 16 + r;
-      if (row >= p.m || tok >= p.tokens || !(wanted >> bit & 1)) continue;
+      if (row >= p.m || tok >= tokens || !(wanted >> bit & 1)) continue;
       const int slot = (((tok >> 4) * RT + (r >> 4)) * 64 + (tok & 15) / 4 * 16 + (r & 15)) * 4 + (tok & 3);
       float v = 0.f;
       for (int w = 0; w < waves; ++w) v += lds[w * TT * RT * 256 + slot];
       if (!(fabsf(v) < __builtin_inff())) lost |= 1ull << bit;
-      if (I8) v *= p.xs[tok];
+      if (I8) v *= p.xs[tok0 + tok];
       if (p.bias) v += p.bias[row];
-      const int64_t o = (int64_t)tok * p.ldy + row;
+      const int64_t o = (int64_t)(tok0 + tok) * p.ldy + row;
       if (p.y_f32) ((float*)p.y)[o] = v;
       else ((uint16_t*)p.y)[o] = __builtin_bit_cast(uint16_t, (__bf16)v);
     }
@@ -274,7 +276,7 @@ static hipError_t launch_few_as(const LinearArgs& p, int waves, hipStream_t s) {
   constexpr int kStages = 2 * TT * 16 * (I8 ? 128 : 256), kSums = TT * RT * 1024, kPerWave = kStages > kSums ? kStages : kSums;
   static LdsLimitOnce once;
   if (const hipError_t e = once.ensure((const void*)&linear_few_kernel<I8, GS, RT, TT>, few_waves(GS, RT, TT) * kPerWave); e != hipSuccess) return e;
-  hipLaunchKernelGGL((linear_few_kernel<I8, GS, RT, TT>), dim3((unsigned)((p.mt + RT - 1) / RT)), dim3(64 * waves), (size_t)(waves * kPerWave), s, p);
+  hipLaunchKernelGGL((linear_few_kernel<I8, GS, RT, TT>), dim3((unsigned)((p.mt + RT - 1) / RT), (unsigned)((p.tokens + TT * 16 - 1) / (TT * 16))), dim3(64 * waves), (size_t)(waves * kPerWave), s, p);
   return hipGetLastError();
 }
 // Tiles of rows per workgroup: the more, the less often the activations are read, the fewer workgroups.  us a call, RT 1 (8 wavefronts) / 2 (4, 8) / 4 (4):
@@ -304,8 +306,17 @@ static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
   return gs == 0 ? launch_few_of<I8, 0>(p, s) : gs == 1 ? launch_few_of<I8, 1>(p, s) : gs == 2 ? launch_few_of<I8, 2>(p, s) : launch_few_of<I8, 4>(p, s);
 }
 
+// Above 32 tokens, in blocks of 32, as far as few workgroups have the work: us a call with this kernel / with that for many tokens, bf16 (workgroups times
+// tiles of columns): 4096 x 4096, 64 tokens 13.1 / 14.6 (512 x 32), 96 18.6 / 16.7; 1024 x 8192, 128 tokens 10.7 / 16.5 (256 x 64), 192 18.7 / 17.1;
+// 2048 x 2048, 192 tokens 13.2 / 14.9 (768 x 16), 256 17.8 / 16.0; 4096 x 11008, 64 tokens 24.9 / 22.6 (512 x 86).  8-bit: 4096 x 4096, 128 tokens 12.4 / 13.6
+// (1024 x 32), 256 20.9 / 18.8; 4096 x 11008, 64 tokens 13.7 / 19.4 (512 x 86), 128 24.6 / 21.2; 4096 x 1024, 128 tokens 5.9 / 6.7 (1024 x 8), 192 8.0 / 6.9.
+static bool few_tokens(const LinearArgs& p, bool i8) {
+  const int64_t workgroups = (int64_t)p.mt * ((p.tokens + 31) / 32);
+  return p.tokens <= 32 || (workgroups <= (i8 ? 1280 : 768) && workgroups * p.kt <= (i8 ? 49152 : 16384));
+}
+
 static hipError_t launch_linear(const LinearArgs& p, int gs, bool i8, float* partial, hipStream_t s) {
-  if (p.tokens > 32) return launch_linear_many(p, gs, i8, partial, s);
+  if (!few_tokens(p, i8)) return launch_linear_many(p, gs, i8, partial, s);
   return i8 ? launch_few<true>(p, gs, s) : launch_few<false>(p, gs, s);
 }
 

@@ -509,3 +509,79 @@ def test_mlp_from_solve_to_answers(group, act_order):
         # 4-bit weights keep most of the signal
         ref = Q.full_precision(x, residual, mlp.norm, *full)
         assert (y.float() - ref).norm().item() <= 0.35 * ref.norm().item()
+
+
+# The kernel of many tokens starts where the work is more than a few workgroups': tiles of 64 and of 128 tokens, with and without parts.
+MANY = [(40, 1100, 16384, 128), (70, 2100, 16384, 0), (130, 4100, 4224, 32), (300, 2050, 8192, 64), (600, 2050, 11008, 128), (1030, 4100, 1024, 0),
+        (1100, 2100, 512, 32), (2050, 4097, 256, 128), (129, 20500, 1280, 64)]
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("tokens,m,n,group", MANY)
+def test_linear_many_is_the_formula(tokens, m, n, group, i8):
+    linear_case(tokens, m, n, 4, group, i8)
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("tokens,m", [(1100, 2100), (1030, 4100)])
+@pytest.mark.parametrize("bits,group,sym,perm,bias,f32,extra,shift", [(2, 64, False, True, False, True, 0, 0), (3, 128, True, False, True, False, 3, 0),
+                                                                     (4, 0, True, True, True, True, 16, 5), (4, 32, False, False, False, False, 0, 1)])
+def test_linear_many_forms(tokens, m, bits, group, sym, perm, bias, f32, extra, shift, i8):
+    linear_case(tokens, m, 512, bits, group, i8, sym, perm, bias, f32, extra, shift)
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("tokens,m,n", [(700, 2100, 2048), (2050, 4100, 1024), (200, 2100, 8192)])
+def test_linear_many_is_exact_where_the_sums_are(tokens, m, n, i8):
+    test_linear_is_exact_where_the_sums_are(tokens, m, n, 64, i8)
+    for c, z, v in ((15, 0, 127), (0, 15, -128)):
+        w = pack(np.full((m, n), c, np.uint8), np.ones((m, 1), np.float32), np.full((m, 1), z, np.float32), 0)
+        ws = B.workspace(B.gptaq_linear_workspace_bytes(tokens, m, n))
+        if i8:
+            Y = B.gptaq_linear_i8(torch.full((tokens, n), v, dtype=torch.int8, device="cuda"), torch.ones(tokens, device="cuda"), w, ws, dtype=torch.float32)
+        else:
+            Y = B.gptaq_linear(torch.full((tokens, n), float(v), dtype=torch.bfloat16, device="cuda"), w, ws, dtype=torch.float32)
+        assert torch.all(Y == float(v * (c - z) * n))
+
+
+@pytest.mark.parametrize("tokens,m,n", [(400, 2100, 256), (2050, 4100, 256), (200, 2100, 8192)])
+def test_linear_many_keeps_tokens_apart(tokens, m, n):
+    codes, scales, zeros = quantised(m, n, 4, 64, False, rng(60))
+    w = pack(codes, scales, zeros, 64)
+    col = dequantised(codes, scales, zeros, 64)[:, 37]
+    clean = bf16(rng(61).standard_normal((tokens, n)))
+    bad = clean.clone()
+    bad[0, 37], bad[17, 3], bad[tokens - 1, n - 1] = float("inf"), float("nan"), float("-inf")
+    ws = B.workspace(B.gptaq_linear_workspace_bytes(tokens, m, n))
+    a, b = B.gptaq_linear(clean, w, ws, dtype=torch.float32), B.gptaq_linear(bad, w, ws, dtype=torch.float32)
+    fine = [t for t in range(tokens) if t not in (0, 17, tokens - 1)]
+    assert torch.equal(a[fine], b[fine])
+    got = b[0].cpu().numpy()
+    assert np.all(np.isposinf(got[col > 0])) and np.all(np.isneginf(got[col < 0])) and np.all(np.isnan(got[col == 0]))
+    assert torch.isnan(b[17]).all() and not torch.isfinite(b[tokens - 1]).any()
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("tokens,m,n,group", [(200, 2100, 8192, 128), (1030, 4100, 384, 64), (40, 1100, 16384, 32)])
+def test_linear_many_keeps_to_its_memory(tokens, m, n, group, i8):
+    test_linear_keeps_to_its_memory(tokens, m, n, group, i8)
+
+
+def test_linear_in_parts_in_a_graph():
+    """Sums in parts of the columns and their join, replayed on new activations."""
+    tokens, m, n = 200, 2100, 8192
+    w = pack(*quantised(m, n, 4, 128, False, rng(70)), 128)
+    ws = B.workspace(B.gptaq_linear_workspace_bytes(tokens, m, n))
+    x = bf16(rng(71).standard_normal((tokens, n)))
+    B.gptaq_linear(x, w, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = B.gptaq_linear(x, w, ws)
+    for k in range(4):
+        x.copy_(bf16(rng(72, k).standard_normal((tokens, n))))
+        graph.replay()
+        got = y.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got, B.gptaq_linear(x, w, ws)), k
+        ws.fill_(k)
