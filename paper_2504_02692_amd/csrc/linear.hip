@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t 
 // feed the matrix unit, two tiles of columns ahead (three or four ahead were slower: registers): nothing of W is read twice, and with everything of a
 // wavefront independent many loads are in flight.  The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the
 // result has the row of W in l % 16 and tokens 4 (l / 16) .. + 3 in the lane's four values, so one scale per lane serves a result.
-// Bound by the weights' bytes where there are many: 28672 x 8192, one token, 8-bit activations 23 us, 5.4 TB/s; bf16 28 to 30 us, where unpacking the codes
+// Bound by the weights' bytes where there are many: 28672 x 8192, one token, 8-bit activations 23 to 25 us, 5.0 to 5.4 TB/s; bf16 26 to 31 us, where unpacking the codes
 // takes most of the time that the bytes leave.  4096 x 4096 4.2 us, 2.2 TB/s: the launch, one trip to memory and the join.
 // Activations go to LDS in runs of a token's whole 128 columns, to a place of the wavefront's own, so that no wavefront waits for another.  (A load of
 // 16 tokens by 64 bytes to registers takes about four times as long as one of 1 KB in one run: 4096 x 11008, 16 tokens, 14.5 us; through LDS 9.3.)

@@ -13,7 +13,7 @@ typedef __attribute__((ext_vector_type(16))) int32_t i32x16;
 // A byte of W feeds four times the products that a byte of bf16 activations does, so the tile is taller in W.
 // Activations go from memory straight to LDS, 128 columns (a stage) at a time, in a ring of four stages with one barrier a stage, in
 // its middle: it publishes the next stage (whose first fragments are read before the stage ends) and retires the one before.
-// 2048 x 11008 x 4096 bf16 181 to 191 us, 1.0 PFLOP/s (the library's bf16 product of this card: 1.46), 8192 x 28672 x 8192 8-bit 2.25 ms, 1.7 POP/s (2.43).
+// 2048 x 11008 x 4096 bf16 181 to 198 us on two cards, 0.93 to 1.0 PFLOP/s (the library's bf16 product of this card: 1.46), 8192 x 28672 x 8192 8-bit 2.25 to 2.4 ms, 1.6 to 1.7 POP/s (2.43).
 // A 32x32 matrix instruction takes 32 cycles of the matrix unit and 16 of the SIMD's vector issue, a vector instruction 4: with n of these to each it is
 // max(32, 16 + 4 n) cycles.  bf16 has 7 (5 of them unpack codes, 2 scale sums), 8 bits 12 (4 and 8), and the chip's power holds bf16 to about 2.1 GHz:
 // with inputs of zeros the same products take four fifths of the time.

@@ -115,7 +115,7 @@ struct RowArgs {
   float eps, clip;
 };
 
-// Bound by memory: 16384 x 8192 with residual 194 us, 5.5 TB/s read and written (a plain copy reaches 5.0); gated 16384 x 11008 194 us, 5.6 TB/s; one
+// Bound by memory: 16384 x 8192 with residual 190 us, 5.7 TB/s read and written (a plain copy reaches 5.0); gated 16384 x 11008 187 us, 5.8 TB/s; one
 // row of 4096 4 us, most of it the launch.
 // One row per workgroup (T threads) or, rows of one wavefront, several rows per workgroup.  A thread keeps its first KEEP pieces of
 // eight columns between the pass that takes the row's sums and the one that writes; later pieces are read again.  Outputs may be
