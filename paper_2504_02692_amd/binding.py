@@ -418,13 +418,22 @@ def gptaq_pack_codes(codes: torch.Tensor, bits: int) -> torch.Tensor:
 
 class LinearWeights:
     """A layer's weights as gptaq_linear and gptaq_linear_i8 read them: data (uint8), m, n, group (0: one per row), perm, bias, and info,
-    an int32 on the GPU that is 0, or 1 + a row whose codes or zeros do not fit in 4 bits."""
-    __slots__ = ("data", "m", "n", "group", "perm", "bias", "info", "_args")
+    an int32 on the GPU that is 0, or 1 + a row whose codes or zeros do not fit in 4 bits.  Fixed once made: gptaq_linear_pack has checked
+    that they fit each other."""
+    __slots__ = ("data", "m", "n", "group", "perm", "bias", "info")
 
     def __init__(self, data: torch.Tensor, m: int, n: int, group: int, perm: Optional[torch.Tensor], bias: Optional[torch.Tensor],
                  info: torch.Tensor):
-        self.data, self.m, self.n, self.group, self.perm, self.bias, self.info = data, m, n, group, perm, bias, info
-        self._args = (_ptr(perm), _ptr(data), data.nbytes, m, n, group, _ptr(bias))           # as the C calls take them, in order
+        for name, value in zip(self.__slots__, (data, m, n, group, perm, bias, info)):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"LinearWeights.{name}: weights are fixed; lay out new ones with gptaq_linear_pack")
+
+    def _args(self):
+        """As the C calls take them, in order."""
+        return (None if self.perm is None else self.perm.data_ptr(), self.data.data_ptr(), self.data.nbytes, self.m, self.n, self.group,
+                None if self.bias is None else self.bias.data_ptr())
 
 
 def gptaq_linear_weights_bytes(m: int, n: int, group: int) -> int:
@@ -479,7 +488,7 @@ def gptaq_linear(X: torch.Tensor, weights: LinearWeights, ws: torch.Tensor, out:
     """X W^T + bias for token-major bf16 X; returns (tokens x m), bf16 or fp32 (`dtype`, or the type of `out`)."""
     _need(X, torch.bfloat16, "X")
     Y = _linear_out(X, weights, dtype, out, "gptaq_linear")
-    _check(load().gptaq_linear(X.data_ptr(), X.shape[0], X.stride(0), *weights._args, Y.data_ptr(), Y.stride(0),
+    _check(load().gptaq_linear(X.data_ptr(), X.shape[0], X.stride(0), *weights._args(), Y.data_ptr(), Y.stride(0),
                                Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear")
     return Y
 
@@ -491,7 +500,7 @@ def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWe
     if scales.shape[0] != codes.shape[0]:
         raise GptaqError("gptaq_linear_i8: scales: expected one per token")
     Y = _linear_out(codes, weights, dtype, out, "gptaq_linear_i8")
-    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.stride(0), *weights._args, Y.data_ptr(),
+    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.stride(0), *weights._args(), Y.data_ptr(),
                                   Y.stride(0), Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear_i8")
     return Y
 

@@ -143,7 +143,8 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
   f32x4 accx[TT];                      // sums of the group's activations (the same in all of a token's lanes)
   // EXACT: the products are those of code - zero.  Else (bf16 only): of 16 + code, which is two instructions for two codes where the difference
   // takes five, and (16 + zero) times the activations' sum, one more matrix instruction for all RT, is taken off each group's sum.
-  // Where a result is not finite this subtraction may be why, and the workgroup takes its sums again with EXACT.
+  // The difference is off by some 2^-24 * 31 sum |x|, 2^-22 of the largest code times sum |x|: for activations that are not one column alone less than
+  // a bf16 output's rounding by far.  Where a result is not finite this subtraction may be why, and the workgroup takes its sums again with EXACT.
   auto add_scaled = [&](auto exact, int r, float s, uint32_t zero) {
     const float z = -16.f - (float)zero;
 #pragma unroll

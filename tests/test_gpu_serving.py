@@ -585,3 +585,18 @@ def test_linear_in_parts_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(got, B.gptaq_linear(x, w, ws)), k
         ws.fill_(k)
+
+
+def test_linear_weights_are_fixed_and_read_where_they_are():
+    """What a layer's weights were checked with cannot be exchanged; a bias whose memory is another by the time of the call is read there."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    codes = torch.randint(0, 16, (48, 128), dtype=torch.uint8, device="cuda", generator=g)
+    scales, zeros = torch.full((48, 1), 0.5, device="cuda"), torch.full((48, 1), 8.0, device="cuda")
+    bias = torch.zeros(48, device="cuda")
+    w = B.gptaq_linear_pack(codes, scales, zeros, 0, bias=bias)
+    with pytest.raises(AttributeError):
+        w.bias = torch.zeros(3, device="cuda")
+    ws = B.workspace(B.gptaq_linear_workspace_bytes(4, 48, 128))
+    X = torch.zeros((4, 128), dtype=torch.bfloat16, device="cuda")
+    bias.data = torch.arange(48, device="cuda").float()
+    assert torch.equal(B.gptaq_linear(X, w, ws, dtype=torch.float32), bias.expand(4, 48))
