@@ -294,10 +294,10 @@ int gptaq_pack_codes(const uint8_t* codes, int64_t m, int64_t n, int64_t ldc, in
  *   ws     : >= gptaq_linear_workspace_bytes(tokens, m, n) bytes, 256-byte aligned; the size for more tokens serves fewer.
  *   m, n   : at most 2^20; tokens at most 2^23.
  * Weights enter the products exactly; sums are taken in fp32 (bf16 activations) or, inside a group, in int32 (8 bits),
- * group sums are scaled and added in fp32, and the result is rounded once.  With few tokens and bf16 activations a
- * group's sum is that of (16 + code) x less (16 + zero) times that of x: its error is some 2^-19 of the group's
- * scale * sum |x|, also where the codes are close to the zero (results that overflow that way are taken again with
- * code - zero).
+ * group sums are scaled and added in fp32, and the result is rounded once.  With up to 16 tokens, many rows, bf16 activations
+ * and a bf16 output, the sum of a group, or of 128 columns of a longer one, may be that of (16 + code) x less (16 + zero)
+ * times that of x: its roundings in fp32 are those of numbers up to 31 sum |x| over these columns, also where the codes
+ * are close to the zero (results that overflow that way are taken again with code - zero).
  */
 size_t gptaq_linear_weights_bytes(int64_t m, int64_t n, int group);
 int gptaq_linear_pack(const uint8_t* codes, int64_t ldc, const float* scales, const float* zeros, int64_t m, int64_t n,

@@ -3,7 +3,8 @@
 //
 // code - zero is an integer between -15 and 15, exact in bfloat16 and in 8 bits, so the matrix instructions multiply exact weights:
 // per group of columns the sum of (code - zero) x is taken in fp32 (bf16 activations) or exactly in int32 (8-bit activations),
-// multiplied by the group's fp32 scale, and added to the fp32 total.  No weight is rounded.
+// multiplied by the group's fp32 scale, and added to the fp32 total.  No weight is rounded.  With up to 16 tokens, many rows, and bf16 in and
+// out it is the sum of (16 + code) x less (16 + zero) times that of x: exact weights too, but larger sums (linear_few_kernel).
 #include "linear.h"
 #include <type_traits>
 
@@ -141,10 +142,15 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
   uint32_t sixteen = 0x41804180u;
   asm volatile("" : "+v"(sixteen));    // (in a register, where the mask and it are one instruction)
   f32x4 accx[TT];                      // sums of the group's activations (the same in all of a token's lanes)
-  // EXACT: the products are those of code - zero.  Else (bf16 only): of 16 + code, which is two instructions for two codes where the difference
-  // takes five, and (16 + zero) times the activations' sum, one more matrix instruction for all RT, is taken off each group's sum.
-  // The difference is off by some 2^-24 * 31 sum |x|, 2^-22 of the largest code times sum |x|: for activations that are not one column alone less than
-  // a bf16 output's rounding by far.  Where a result is not finite this subtraction may be why, and the workgroup takes its sums again with EXACT.
+  // EXACT: the products are those of code - zero.  Else: of 16 + code, which is two instructions for two codes where the difference takes
+  // five, and (16 + zero) times the activations' sum, one more matrix instruction for all RT, is taken off each group's sum, of a group as long as the row
+  // off each 128 columns': what is subtracted stays below 31 times the 128 columns' sum |x|, so its rounding does, and does not grow with the row.
+  // A bf16 output's own rounding hides that; outputs in fp32 are EXACT, and where a result is not finite the subtraction may be why, and the workgroup takes
+  // its sums again with EXACT.
+  // One matrix instruction for an operand (TT 1) and one sum of activations for several operands (RT) is where it pays: us a call, EXACT / else, one token:
+  // 28672 x 8192 33 / 29, 22016 x 4096 15.9 / 13.0, 11008 x 4096 10.3 / 9.1; RT 1: 4096 x 11008 7.7 / 7.8, 16 tokens 9.2 / 9.7; TT 2, 32 tokens:
+  // 4096 x 11008 13.1 / 14.3, 11008 x 4096 13.5 / 14.0, 28672 x 8192 42 / 49 (registers spill).
+  constexpr bool kSixteen = !I8 && TT == 1 && RT > 1;
   auto add_scaled = [&](auto exact, int r, float s, uint32_t zero) {
     const float z = -16.f - (float)zero;
 #pragma unroll
@@ -161,7 +167,8 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
     asm volatile("" :: "v"(s.w[RT - 1]) : "memory");
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const bool first = GS && i % (4 / G) == 0, last = GS && (i + 1) % (4 / G) == 0;
+      constexpr bool kGrouped = GS || !decltype(exact)::value;       // (else the sum runs over the row)
+      const bool first = kGrouped && i % (4 / G) == 0, last = kGrouped && (i + 1) % (4 / G) == 0;
       u32x4 x[TT];
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
@@ -204,7 +211,7 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
           else
             acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[t]), __builtin_bit_cast(bf16x8, v), c, 0, 0, 0);
         }
-        if (last) add_scaled(exact, r, s.scale[r][i * G / 4], zero);
+        if (last) add_scaled(exact, r, GS ? s.scale[r][i * G / 4] : 1.f, zero);
       }
     }
   };
@@ -232,7 +239,13 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
     __syncthreads();                   // (the sums go where other wavefronts' activations are)
     if (!GS) {
 #pragma unroll
-      for (int r = 0; r < RT; ++r) add_scaled(exact, r, p.scales[group[r]], row_zero[r]);
+      for (int r = 0; r < RT; ++r) {
+        const float s = p.scales[group[r]];
+        if (exact) add_scaled(exact, r, s, row_zero[r]);
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+          if (!exact) total[t][r] *= s;
+      }
     }
   };
   // Joins the wavefronts' sums, [wave][t][r][lane][4], and stores those of this thread's results that `wanted` has a bit for; returns which are not
@@ -261,13 +274,17 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
     }
     return lost;
   };
-  sums(std::integral_constant<bool, I8>{});
   static_assert(TT * RT * 256 / 64 <= 64, "a bit for each of a thread's results");
-  const uint64_t lost = finish(~0ull);
-  if (!I8 && __syncthreads_or(lost != 0)) {
-    sums(std::true_type{});
-    finish(lost);
+  uint64_t wanted = ~0ull;
+  if constexpr (kSixteen) {
+    if (!p.y_f32) {
+      sums(std::false_type{});
+      wanted = finish(wanted);
+      if (!__syncthreads_or(wanted != 0)) return;
+    }
   }
+  sums(std::true_type{});
+  finish(wanted);
 }
 
 template <bool I8, int GS, int RT, int TT>
