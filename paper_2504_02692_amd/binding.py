@@ -418,8 +418,8 @@ def gptaq_pack_codes(codes: torch.Tensor, bits: int) -> torch.Tensor:
 
 class LinearWeights:
     """A layer's weights as gptaq_linear and gptaq_linear_i8 read them: data (uint8), m, n, group (0: one per row), perm, bias, and info,
-    an int32 on the GPU that is 0, or 1 + a row whose codes or zeros do not fit in 4 bits.  Fixed once made: gptaq_linear_pack has checked
-    that they fit each other."""
+    an int32 on the GPU that is 0, or 1 + a row whose codes or zeros do not fit in 4 bits.  Fixed once made, as gptaq_linear_pack has checked
+    that they fit each other; what a call reads of the tensors is their memory at that time, which has to be of the same kind and size still."""
     __slots__ = ("data", "m", "n", "group", "perm", "bias", "info")
 
     def __init__(self, data: torch.Tensor, m: int, n: int, group: int, perm: Optional[torch.Tensor], bias: Optional[torch.Tensor],
@@ -432,8 +432,14 @@ class LinearWeights:
 
     def _args(self):
         """As the C calls take them, in order."""
-        return (None if self.perm is None else self.perm.data_ptr(), self.data.data_ptr(), self.data.nbytes, self.m, self.n, self.group,
-                None if self.bias is None else self.bias.data_ptr())
+        def address(t, dtype, count, name):
+            if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
+                raise GptaqError(f"LinearWeights.{name}: no longer {count} contiguous {dtype}")
+            return t.data_ptr()
+
+        data, perm, bias = self.data, self.perm, self.bias
+        return (None if perm is None else address(perm, torch.int32, self.n, "perm"), address(data, torch.uint8, data.numel(), "data"), data.numel(),
+                self.m, self.n, self.group, None if bias is None else address(bias, torch.float32, self.m, "bias"))
 
 
 def gptaq_linear_weights_bytes(m: int, n: int, group: int) -> int:

@@ -120,3 +120,38 @@ def test_row_refusals(lib):
     gated(-2, u=ODD)
     gated(-2, n=(1 << 24) + 8, ldg=1 << 25, ldu=1 << 25, ldy=1 << 25)
     gated(0, tokens=0)
+
+
+def weights(m=48, n=128, **other):
+    """LinearWeights as a program could have them, in host memory: what follows looks at them, and launches nothing."""
+    import torch
+    from paper_2504_02692_amd import binding as B
+    have = dict(data=torch.zeros(B.gptaq_linear_weights_bytes(m, n, 0), dtype=torch.uint8), perm=torch.arange(n, dtype=torch.int32),
+                bias=torch.zeros(m), info=torch.zeros(1, dtype=torch.int32))
+    have.update(other)
+    return B.LinearWeights(m=m, n=n, group=0, **have)
+
+
+@pytest.mark.parametrize("name,memory", [("bias", lambda t: t[:3]), ("bias", lambda t: t.double()), ("bias", lambda t: t[:1].expand(48)),
+                                         ("perm", lambda t: t[:100]), ("perm", lambda t: t.long()), ("perm", lambda t: t.repeat(2)[::2]),
+                                         ("data", lambda t: t.view(2, -1).t()), ("data", lambda t: t.short())])
+def test_weights_whose_memory_became_another_are_refused(lib, name, memory):
+    """A layer's tensors are read where they are at the call, as many elements as the layer has: memory that holds fewer would be read past its end."""
+    from paper_2504_02692_amd import binding as B
+    w = weights()
+    before = w._args()
+    assert before[0] == w.perm.data_ptr() and before[1:3] == (w.data.data_ptr(), w.data.numel()) and before[6] == w.bias.data_ptr()
+    t = getattr(w, name)
+    t.data = memory(t.detach().clone())
+    with pytest.raises(B.GptaqError, match=name):
+        w._args()
+    with pytest.raises(B.GptaqError, match=name):
+        weights(**{name: memory(getattr(weights(), name))})._args()
+
+
+def test_weights_whose_memory_moved_are_read_there(lib):
+    import torch
+    w = weights()
+    w.bias.data, w.perm.data = torch.ones(48), torch.zeros(128, dtype=torch.int32)
+    args = w._args()
+    assert args[0] == w.perm.data_ptr() and args[6] == w.bias.data_ptr()
