@@ -128,14 +128,30 @@ def _check(status: int, what: str) -> None:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream() -> int:
+def _stream(device: Optional[int] = None) -> int:
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(torch.cuda.current_device() if device is None else device)
     return torch.cuda.current_stream().cuda_stream
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+def _ws(ws: torch.Tensor, device: Optional[int] = None) -> int:
+    """A workspace's address; on the GPU `device`, where that is given."""
+    if not (ws.is_cuda if device is None else ws.get_device() == device) or not ws.is_contiguous():
+        raise GptaqError(f"ws: expected contiguous memory of the GPU that runs the call, not of {ws.device}")
+    return ws.data_ptr()
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> int:
+    """The current GPU, where all of a call's tensors have to be."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise GptaqError(f"a tensor of {t.device} in a call that runs on GPU {device}")
+    return device
 
 
 def _need(t: torch.Tensor, dtype, name: str) -> None:
@@ -173,7 +189,7 @@ def _accumulate(name: str, X: torch.Tensor, Xtilde: torch.Tensor, H: torch.Tenso
             or H.stride(0) != dXXT.stride(0):
         raise GptaqError(f"{name}: shape mismatch")
     _check(getattr(load(), name)(_ptr(X), _ptr(Xtilde), tokens, n, X.stride(0), _ptr(H), _ptr(dXXT),
-                                 H.stride(0), _ptr(ws), ws.numel(), _stream()), name)
+                                 H.stride(0), _ws(ws), ws.numel(), _stream()), name)
 
 
 def gptaq_accumulate(X: torch.Tensor, Xtilde: torch.Tensor, H: torch.Tensor, dXXT: torch.Tensor,
@@ -218,7 +234,7 @@ def gptaq_accumulate_staged(X: Optional[torch.Tensor], Xtilde: Optional[torch.Te
         raise GptaqError("gptaq_accumulate_staged: shape mismatch")
     p = _c.c_int64(int(pending))
     _check(getattr(load(), fn)(_ptr(X), _ptr(Xtilde), tokens, n, ldx, _ptr(H), _ptr(dXXT), H.stride(0),
-                               _ptr(ws), ws.numel() * ws.element_size(), _c.byref(p), int(bool(flush)),
+                               _ws(ws), ws.numel() * ws.element_size(), _c.byref(p), int(bool(flush)),
                                _stream()), fn)
     return p.value
 
@@ -240,7 +256,7 @@ def gptaq_prepare(H: torch.Tensor, dXXT: torch.Tensor, damp: float, ws: torch.Te
     if info is None:
         info = torch.empty(2, dtype=torch.int32, device=H.device)
     _check(load().gptaq_prepare(_ptr(H), _ptr(dXXT), n, H.stride(0), float(damp), _ptr(dead), _ptr(info),
-                                _ptr(ws), ws.numel(), _stream()), "gptaq_prepare")
+                                _ws(ws), ws.numel(), _stream()), "gptaq_prepare")
     return dead, info
 
 
@@ -266,7 +282,7 @@ def gptaq_quantize_layer(W: torch.Tensor, U: torch.Tensor, P: torch.Tensor, bits
     if zeros is None:
         zeros = torch.empty((m, G), dtype=torch.float32, device=W.device)
     args = (_ptr(W), m, n, W.stride(0), _ptr(U), _ptr(P), U.stride(0), _ptr(dead), int(bits), int(group),
-            int(bool(sym)), int(blocksize), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(ws), ws.numel(), _stream())
+            int(bool(sym)), int(blocksize), _ptr(codes), _ptr(scales), _ptr(zeros), _ws(ws), ws.numel(), _stream())
     if mse_steps > 0:
         _check(load().gptaq_quantize_layer_ex(*args, int(terms), int(mse_grid), int(mse_steps)), "gptaq_quantize_layer_ex")
     elif terms == 3:
@@ -296,7 +312,7 @@ def gptaq_measure_mfma_peak(random_data: bool, millis: int = 50):
     """(TFLOP/s, core clock in GHz) of a pure bf16 MFMA loop on every CU, on all-ones or on random operands."""
     ws = workspace(1 << 20)
     tf, ghz = _c.c_double(0.0), _c.c_double(0.0)
-    _check(load().gptaq_measure_mfma_peak(int(bool(random_data)), int(millis), _ptr(ws), ws.numel() * ws.element_size(),
+    _check(load().gptaq_measure_mfma_peak(int(bool(random_data)), int(millis), _ws(ws), ws.numel() * ws.element_size(),
                                           _c.byref(tf), _c.byref(ghz), _stream()), "gptaq_measure_mfma_peak")
     return tf.value, ghz.value
 
@@ -305,7 +321,7 @@ def gptaq_measure_hbm_copy(nbytes: int = 1 << 30, reps: int = 10) -> float:
     """GB/s (read + written) of a plain streaming copy of `nbytes`."""
     ws = workspace(2 * nbytes)
     g = _c.c_double(0.0)
-    _check(load().gptaq_measure_hbm_copy(int(nbytes), int(reps), _ptr(ws), ws.numel() * ws.element_size(), _c.byref(g),
+    _check(load().gptaq_measure_hbm_copy(int(nbytes), int(reps), _ws(ws), ws.numel() * ws.element_size(), _c.byref(g),
                                          _stream()), "gptaq_measure_hbm_copy")
     return g.value
 
@@ -351,7 +367,7 @@ def gptaq_accumulate_upper_permuted(X: torch.Tensor, Xtilde: torch.Tensor, inv_p
             or not inv_perm.is_contiguous():
         raise GptaqError("gptaq_accumulate_upper_permuted: shape mismatch")
     _check(load().gptaq_accumulate_upper_permuted(_ptr(X), _ptr(Xtilde), tokens, n, X.stride(0), _ptr(inv_perm), _ptr(H),
-                                                  _ptr(dXXT), H.stride(0), _ptr(ws), ws.numel(), _stream()),
+                                                  _ptr(dXXT), H.stride(0), _ws(ws), ws.numel(), _stream()),
            "gptaq_accumulate_upper_permuted")
 
 
@@ -364,7 +380,7 @@ def gptaq_permute_hessian(H: torch.Tensor, dXXT: torch.Tensor, perm: torch.Tenso
     n = H.shape[0]
     if dXXT.shape != (n, n) or H.stride(0) != dXXT.stride(0) or perm.dtype != torch.int32 or perm.numel() != n:
         raise GptaqError("gptaq_permute_hessian: shape mismatch")
-    _check(load().gptaq_permute_hessian(_ptr(H), _ptr(dXXT), n, H.stride(0), _ptr(perm), _ptr(ws), ws.numel(),
+    _check(load().gptaq_permute_hessian(_ptr(H), _ptr(dXXT), n, H.stride(0), _ptr(perm), _ws(ws), ws.numel(),
                                         _stream()), "gptaq_permute_hessian")
 
 
@@ -416,6 +432,14 @@ def gptaq_pack_codes(codes: torch.Tensor, bits: int) -> torch.Tensor:
 
 # ---- running quantised layers
 
+def _address(t: torch.Tensor, device: int, dtype, count: int, name: str) -> int:
+    if t.get_device() != device:
+        raise GptaqError(f"LinearWeights.{name}: in memory of {t.device}, in a call that runs on GPU {device}")
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
+        raise GptaqError(f"LinearWeights.{name}: no longer {count} contiguous {dtype}")
+    return t.data_ptr()
+
+
 class LinearWeights:
     """A layer's weights as gptaq_linear and gptaq_linear_i8 read them: data (uint8), m, n, group (0: one per row), perm, bias, and info,
     an int32 on the GPU that is 0, or 1 + a row whose codes or zeros do not fit in 4 bits.  Fixed once made, as gptaq_linear_pack has checked
@@ -430,16 +454,12 @@ class LinearWeights:
     def __setattr__(self, name, value):
         raise AttributeError(f"LinearWeights.{name}: weights are fixed; lay out new ones with gptaq_linear_pack")
 
-    def _args(self):
-        """As the C calls take them, in order."""
-        def address(t, dtype, count, name):
-            if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
-                raise GptaqError(f"LinearWeights.{name}: no longer {count} contiguous {dtype}")
-            return t.data_ptr()
-
+    def _args(self, device: int):
+        """As the C calls take them, in order; on the GPU `device`."""
         data, perm, bias = self.data, self.perm, self.bias
-        return (None if perm is None else address(perm, torch.int32, self.n, "perm"), address(data, torch.uint8, data.numel(), "data"), data.numel(),
-                self.m, self.n, self.group, None if bias is None else address(bias, torch.float32, self.m, "bias"))
+        size = data.numel()
+        return (None if perm is None else _address(perm, device, torch.int32, self.n, "perm"), _address(data, device, torch.uint8, size, "data"), size,
+                self.m, self.n, self.group, None if bias is None else _address(bias, device, torch.float32, self.m, "bias"))
 
 
 def gptaq_linear_weights_bytes(m: int, n: int, group: int) -> int:
@@ -464,10 +484,11 @@ def gptaq_linear_pack(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Te
         _need_vec(bias, torch.float32, "bias")
         if bias.numel() != m:
             raise GptaqError("gptaq_linear_pack: bias: expected one entry per row")
+    device = _here(codes, scales, zeros, perm, bias)
     data = workspace(gptaq_linear_weights_bytes(m, n, group), codes.device)
     info = torch.empty(1, dtype=torch.int32, device=codes.device)
     _check(load().gptaq_linear_pack(_ptr(codes), codes.stride(0), _ptr(scales), _ptr(zeros), m, n, int(group), _ptr(data), data.numel(),
-                                    _ptr(info), _stream()), "gptaq_linear_pack")
+                                    _ptr(info), _stream(device)), "gptaq_linear_pack")
     return LinearWeights(data, m, n, max(0, int(group)), perm, bias, info)
 
 
@@ -493,9 +514,10 @@ def gptaq_linear(X: torch.Tensor, weights: LinearWeights, ws: torch.Tensor, out:
                  dtype=torch.bfloat16) -> torch.Tensor:
     """X W^T + bias for token-major bf16 X; returns (tokens x m), bf16 or fp32 (`dtype`, or the type of `out`)."""
     _need(X, torch.bfloat16, "X")
+    device = _here(X, out)
     Y = _linear_out(X, weights, dtype, out, "gptaq_linear")
-    _check(load().gptaq_linear(X.data_ptr(), X.shape[0], X.stride(0), *weights._args(), Y.data_ptr(), Y.stride(0),
-                               Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear")
+    _check(load().gptaq_linear(X.data_ptr(), X.shape[0], X.stride(0), *weights._args(device), Y.data_ptr(), Y.stride(0),
+                               Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear")
     return Y
 
 
@@ -505,9 +527,10 @@ def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWe
     _need(codes, torch.int8, "codes"); _need_vec(scales, torch.float32, "scales")
     if scales.shape[0] != codes.shape[0]:
         raise GptaqError("gptaq_linear_i8: scales: expected one per token")
+    device = _here(codes, scales, out)
     Y = _linear_out(codes, weights, dtype, out, "gptaq_linear_i8")
-    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.stride(0), *weights._args(), Y.data_ptr(),
-                                  Y.stride(0), Y.dtype is torch.float32, ws.data_ptr(), ws.nbytes, _stream()), "gptaq_linear_i8")
+    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.stride(0), *weights._args(device), Y.data_ptr(),
+                                  Y.stride(0), Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear_i8")
     return Y
 
 
@@ -543,11 +566,12 @@ def gptaq_rms_norm(X: torch.Tensor, weight: Optional[torch.Tensor], eps: float, 
                    total: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None):
     """(Y, total): total = X + residual, Y = its root-mean-square norm times weight (None: ones).  Without a residual and without
     `total`, total is None.  `total` may be the residual itself (in place)."""
+    device = _here(X, weight, residual, total, out)
     total = _norm_args(X, weight, residual, total, "gptaq_rms_norm")
     tokens, n = X.shape
     Y = _like(X, out, "gptaq_rms_norm")
     _check(load().gptaq_rms_norm(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, X.stride(0), residual.stride(0) if residual is not None else 0,
-                                 float(eps), _ptr(total), total.stride(0) if total is not None else 0, _ptr(Y), Y.stride(0), _stream()),
+                                 float(eps), _ptr(total), total.stride(0) if total is not None else 0, _ptr(Y), Y.stride(0), _stream(device)),
            "gptaq_rms_norm")
     return Y, total
 
@@ -555,12 +579,13 @@ def gptaq_rms_norm(X: torch.Tensor, weight: Optional[torch.Tensor], eps: float, 
 def gptaq_rms_norm_i8(X: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None,
                       total: Optional[torch.Tensor] = None, clip: float = 1.0):
     """(codes, scales, total): gptaq_rms_norm with its output as 8-bit codes and a scale per token."""
+    device = _here(X, weight, residual, total)
     total = _norm_args(X, weight, residual, total, "gptaq_rms_norm_i8")
     tokens, n = X.shape
     codes, scales = X.new_empty((tokens, n), dtype=torch.int8), X.new_empty(tokens, dtype=torch.float32)
     _check(load().gptaq_rms_norm_i8(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, X.stride(0), residual.stride(0) if residual is not None else 0,
                                     float(eps), _ptr(total), total.stride(0) if total is not None else 0, float(clip), _ptr(codes), n,
-                                    _ptr(scales), _stream()), "gptaq_rms_norm_i8")
+                                    _ptr(scales), _stream(device)), "gptaq_rms_norm_i8")
     return codes, scales, total
 
 
@@ -572,18 +597,20 @@ def _gated_args(gate: torch.Tensor, up: torch.Tensor, name: str) -> None:
 
 def gptaq_silu_mul(gate: torch.Tensor, up: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """silu(gate) * up in bf16; gate and up may be the two halves of one product's output."""
+    device = _here(gate, up, out)
     _gated_args(gate, up, "gptaq_silu_mul")
     tokens, n = gate.shape
     Y = _like(gate, out, "gptaq_silu_mul")
-    _check(load().gptaq_silu_mul(_ptr(gate), _ptr(up), tokens, n, gate.stride(0), up.stride(0), _ptr(Y), Y.stride(0), _stream()), "gptaq_silu_mul")
+    _check(load().gptaq_silu_mul(_ptr(gate), _ptr(up), tokens, n, gate.stride(0), up.stride(0), _ptr(Y), Y.stride(0), _stream(device)), "gptaq_silu_mul")
     return Y
 
 
 def gptaq_silu_mul_i8(gate: torch.Tensor, up: torch.Tensor, clip: float = 1.0):
     """(codes, scales): silu(gate) * up as 8-bit codes and a scale per token."""
+    device = _here(gate, up)
     _gated_args(gate, up, "gptaq_silu_mul_i8")
     tokens, n = gate.shape
     codes, scales = gate.new_empty((tokens, n), dtype=torch.int8), gate.new_empty(tokens, dtype=torch.float32)
     _check(load().gptaq_silu_mul_i8(_ptr(gate), _ptr(up), tokens, n, gate.stride(0), up.stride(0), float(clip), _ptr(codes), n, _ptr(scales),
-                                    _stream()), "gptaq_silu_mul_i8")
+                                    _stream(device)), "gptaq_silu_mul_i8")
     return codes, scales

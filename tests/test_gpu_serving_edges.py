@@ -55,3 +55,34 @@ def test_fp32_outputs_keep_small_activations_beside_a_large_one(tokens, group, m
     ws = B.workspace(B.gptaq_linear_workspace_bytes(tokens, m, n))
     got = B.gptaq_linear(bf16(x), w, ws, dtype=torch.float32)
     assert np.array_equal(f64(got), x @ dequantised(codes, scales, zeros, group).T)
+
+
+# ---- arguments
+
+def test_memory_of_another_device_is_refused(monkeypatch):
+    """Tensors in host memory, or on a GPU that is not the current one, are refused by every call before anything is launched."""
+    w = pack(*quantised(16, 64, 4, 32, False, rng(1)), 32, perm=np.arange(64, dtype=np.int32), bias=np.zeros(16, np.float32))
+    ws = B.workspace(B.gptaq_linear_workspace_bytes(4, 16, 64))
+    x, row = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda"), torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    q, s = torch.zeros((4, 64), dtype=torch.int8, device="cuda"), torch.ones(4, device="cuda")
+    y = torch.zeros((4, 16), dtype=torch.bfloat16, device="cuda")
+    host = lambda **other: B.LinearWeights(**{**{k: getattr(w, k) for k in ("data", "m", "n", "group", "perm", "bias", "info")}, **other})
+    calls = [lambda: B.gptaq_linear(x, w, ws.cpu()), lambda: B.gptaq_linear_i8(q, s, w, ws.cpu()), lambda: B.gptaq_linear(x, w, ws, out=y.cpu()),
+             lambda: B.gptaq_linear(x, host(data=w.data.cpu()), ws), lambda: B.gptaq_linear(x, host(perm=w.perm.cpu()), ws),
+             lambda: B.gptaq_linear_i8(q, s, host(bias=w.bias.cpu()), ws), lambda: B.gptaq_linear_i8(q, s.cpu(), w, ws),
+             lambda: B.gptaq_rms_norm(x, row.cpu(), 1e-5), lambda: B.gptaq_rms_norm(x, row, 1e-5, residual=x.cpu()),
+             lambda: B.gptaq_rms_norm_i8(x, row, 1e-5, total=x.cpu()), lambda: B.gptaq_silu_mul(x, x.cpu()),
+             lambda: B.gptaq_silu_mul(x, x, out=x.cpu()), lambda: B.gptaq_silu_mul_i8(x.cpu(), x),
+             lambda: B.gptaq_accumulate(x, x, torch.zeros((64, 64), device="cuda"), torch.zeros((64, 64), device="cuda"), torch.empty(1 << 20, dtype=torch.uint8)),
+             lambda: B.gptaq_prepare(torch.eye(64, device="cuda"), torch.zeros((64, 64), device="cuda"), 0.01, torch.empty(1 << 20, dtype=torch.uint8))]
+    for k, call in enumerate(calls):
+        with pytest.raises(B.GptaqError):
+            call()
+            pytest.fail(f"call {k} was taken")
+    here = torch.cuda.current_device()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: here + 1)
+    for k, call in enumerate([lambda: B.gptaq_linear(x, w, ws), lambda: B.gptaq_linear_i8(q, s, w, ws), lambda: B.gptaq_rms_norm(x, row, 1e-5),
+                              lambda: B.gptaq_rms_norm_i8(x, row, 1e-5), lambda: B.gptaq_silu_mul(x, x), lambda: B.gptaq_silu_mul_i8(x, x)]):
+        with pytest.raises(B.GptaqError):
+            call()
+            pytest.fail(f"call {k} was taken")

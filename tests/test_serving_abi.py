@@ -123,7 +123,7 @@ def test_row_refusals(lib):
 
 
 def weights(m=48, n=128, **other):
-    """LinearWeights as a program could have them, in host memory: what follows looks at them, and launches nothing."""
+    """LinearWeights as a program could have them, in host memory (device -1): what follows looks at them, and launches nothing."""
     import torch
     from paper_2504_02692_amd import binding as B
     have = dict(data=torch.zeros(B.gptaq_linear_weights_bytes(m, n, 0), dtype=torch.uint8), perm=torch.arange(n, dtype=torch.int32),
@@ -139,19 +139,50 @@ def test_weights_whose_memory_became_another_are_refused(lib, name, memory):
     """A layer's tensors are read where they are at the call, as many elements as the layer has: memory that holds fewer would be read past its end."""
     from paper_2504_02692_amd import binding as B
     w = weights()
-    before = w._args()
+    before = w._args(-1)
     assert before[0] == w.perm.data_ptr() and before[1:3] == (w.data.data_ptr(), w.data.numel()) and before[6] == w.bias.data_ptr()
     t = getattr(w, name)
     t.data = memory(t.detach().clone())
     with pytest.raises(B.GptaqError, match=name):
-        w._args()
+        w._args(-1)
     with pytest.raises(B.GptaqError, match=name):
-        weights(**{name: memory(getattr(weights(), name))})._args()
+        weights(**{name: memory(getattr(weights(), name))})._args(-1)
 
 
 def test_weights_whose_memory_moved_are_read_there(lib):
     import torch
     w = weights()
     w.bias.data, w.perm.data = torch.ones(48), torch.zeros(128, dtype=torch.int32)
-    args = w._args()
+    args = w._args(-1)
     assert args[0] == w.perm.data_ptr() and args[6] == w.bias.data_ptr()
+
+
+def test_memory_of_another_device_is_refused(lib, monkeypatch):
+    """Addresses in host memory, or in that of a GPU other than the one the kernels run on, do not reach the library."""
+    import torch
+    from paper_2504_02692_amd import binding as B
+    ws = torch.empty(1024, dtype=torch.uint8)
+    for device in (0, 1):
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: device)
+        for kept in ("perm", "bias", "data"):
+            with pytest.raises(B.GptaqError, match="LinearWeights.perm" if kept == "perm" else "LinearWeights.data"):
+                weights(**{k: None for k in ("perm", "bias") if k != kept})._args(device)
+        with pytest.raises(B.GptaqError, match="ws"):
+            B._ws(ws, device)
+        with pytest.raises(B.GptaqError, match="cpu"):
+            B._here(None, torch.empty(4))
+    with pytest.raises(B.GptaqError, match="ws"):
+        B._ws(ws)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)                 # host memory's own number
+    assert B._ws(ws, -1) == ws.data_ptr() and B._here(ws, None) == -1
+    with pytest.raises(B.GptaqError, match="ws"):
+        B._ws(ws[:1].expand(1 << 20), -1)                                         # more bytes by its shape than it has
+
+
+def test_workspaces_of_every_call_are_looked_at(lib, monkeypatch):
+    """No call hands a workspace's address to the library unseen."""
+    import inspect
+    from paper_2504_02692_amd import binding as B
+    for name, f in inspect.getmembers(B, inspect.isfunction):
+        source = inspect.getsource(f)
+        assert name == "_ws" or "ws.data_ptr()" not in source and "_ptr(ws)" not in source, name
