@@ -454,6 +454,10 @@ class LinearWeights:
     def __setattr__(self, name, value):
         raise AttributeError(f"LinearWeights.{name}: weights are fixed; lay out new ones with gptaq_linear_pack")
 
+    def __reduce__(self):
+        """Copied, pickled and saved through its constructor (the default sets attributes)."""
+        return LinearWeights, tuple(getattr(self, name) for name in self.__slots__)
+
     def _args(self, device: int):
         """As the C calls take them, in order; on the GPU `device`."""
         data, perm, bias = self.data, self.perm, self.bias

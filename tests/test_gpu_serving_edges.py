@@ -86,3 +86,12 @@ def test_memory_of_another_device_is_refused(monkeypatch):
         with pytest.raises(B.GptaqError):
             call()
             pytest.fail(f"call {k} was taken")
+
+
+def test_stored_weights_run_as_before(tmp_path):
+    w = pack(*quantised(40, 96, 4, 32, False, rng(2)), 32, perm=rng(3).permutation(96).astype(np.int32), bias=np.ones(40, np.float32))
+    x, ws = bf16(rng(4).standard_normal((3, 96))), B.workspace(B.gptaq_linear_workspace_bytes(3, 40, 96))
+    torch.save(w, tmp_path / "layer.pt")
+    with torch.serialization.safe_globals([B.LinearWeights]):
+        again = torch.load(tmp_path / "layer.pt", weights_only=True)
+    assert torch.equal(B.gptaq_linear(x, again, ws), B.gptaq_linear(x, w, ws))

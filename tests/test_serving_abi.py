@@ -186,3 +186,23 @@ def test_workspaces_of_every_call_are_looked_at(lib, monkeypatch):
     for name, f in inspect.getmembers(B, inspect.isfunction):
         source = inspect.getsource(f)
         assert name == "_ws" or "ws.data_ptr()" not in source and "_ptr(ws)" not in source, name
+
+
+def test_weights_are_copied_pickled_and_saved(lib, tmp_path):
+    """A program that has laid a model out can store it and copy it; what comes back is as fixed as the weights it came from."""
+    import copy
+    import pickle
+    import torch
+    from paper_2504_02692_amd import binding as B
+    w = weights(bias=torch.randn(48))
+    torch.save({"layer": w}, tmp_path / "layer.pt")
+    again = [copy.copy(w), copy.deepcopy(w), pickle.loads(pickle.dumps(w)), torch.load(tmp_path / "layer.pt", weights_only=False)["layer"]]
+    with torch.serialization.safe_globals([B.LinearWeights]):
+        again.append(torch.load(tmp_path / "layer.pt", weights_only=True)["layer"])
+    for k, v in enumerate(again):
+        assert type(v) is B.LinearWeights and (v.m, v.n, v.group) == (w.m, w.n, w.group)
+        for name in ("data", "perm", "bias", "info"):
+            assert torch.equal(getattr(v, name), getattr(w, name)) and (getattr(v, name) is getattr(w, name)) == (k == 0)
+        with pytest.raises(AttributeError):
+            v.bias = None
+    assert copy.deepcopy(weights(perm=None, bias=None)).perm is None
