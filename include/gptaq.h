@@ -312,7 +312,9 @@ int gptaq_linear_i8(const int8_t* X, const float* x_scales, int64_t tokens, int6
 
 /* gptaq_rms_norm: h = X + residual (X alone if residual is NULL), Y = h * weight / sqrt(mean(h^2) + eps) over each row's n
  *   columns; weight: n x bf16 or NULL for ones (rotated models have theirs in the next layer's weights).  sum, if not
- *   NULL, receives h (the next residual).  h is not rounded on its way to Y.
+ *   NULL, receives h (the next residual).  h is not rounded on its way to Y.  eps >= 0; a row of zeros gives zeros, also with
+ *   eps = 0.  Squares are taken in fp32: a row whose sum of squares is above its range (values of 2^64 / sqrt(n) and more), or
+ *   with eps = 0 below it, gives zeros, too.
  * gptaq_silu_mul: Y = gate / (1 + exp(-gate)) * up; gate and up may be the two halves of one product's rows.
  * _i8: the same Y, in fp32, as codes on a symmetric 8-bit grid: scales[t] = clip * max|Y[t][:]| / 127,
  *   code = clamp(rint(Y / scale), -127, 127), with Y / scale taken as Y * (1 / scale) (a code within 2^-15 of a

@@ -184,7 +184,11 @@ __global__ __launch_bounds__(1024) void row_kernel(RowArgs p) {
     }
     ro_reduce(ss, top, waves, part);
   }
-  const float r = NORM ? 1.f / sqrtf(ss / (float)n + p.eps) : 1.f;
+  float r = 1.f;
+  if (NORM) {
+    const float square = ss / (float)n + p.eps;
+    r = square == 0.f ? 0.f : 1.f / sqrtf(square);     // (eps = 0 and a row of zeros: zeros, as for every other eps)
+  }
   float scale = 0.f, inv = 0.f;
   bool divide = false;
   if (CODES) {

@@ -57,6 +57,27 @@ def test_fp32_outputs_keep_small_activations_beside_a_large_one(tokens, group, m
     assert np.array_equal(f64(got), x @ dequantised(codes, scales, zeros, group).T)
 
 
+# ---- rows
+
+@pytest.mark.parametrize("n", [40, 4096, 33000])
+@pytest.mark.parametrize("eps", [0.0, 1e-5])
+def test_rows_of_zeros_are_zeros_with_any_eps(n, eps):
+    """h / sqrt(mean(h^2) + eps) of a row of zeros is 0 for every eps above 0, and so for eps = 0; other rows follow the formula there too."""
+    x = bf16(rng(n, 90).standard_normal((5, n)))
+    x[1], x[3] = 0.0, -0.0
+    w = bf16(1.0 + rng(n, 91).standard_normal((1, n)))[0].contiguous()
+    y, _ = B.gptaq_rms_norm(x, w, eps)
+    codes, scales, total = B.gptaq_rms_norm_i8(x, w, eps, residual=torch.zeros_like(x))
+    for k in (1, 3):
+        assert torch.all(y[k] == 0) and torch.all(codes[k] == 0) and scales[k] == 0 and torch.all(total[k] == 0)
+    h = f64(x)[[0, 2, 4]]
+    want = h / np.sqrt(np.mean(h * h, 1, keepdims=True) + eps) * f64(w)
+    rel = (n + 16) * 2.0 ** -24
+    assert np.all(np.abs(f64(y)[[0, 2, 4]] - want) <= np.abs(want) * (2.0 ** -8 * (1 + 2.0 ** -6) + rel) + 2.0 ** -133)
+    s = np.abs(want).max(1) / 127.0
+    assert np.all(np.abs(f64(scales)[[0, 2, 4]] - s) <= rel * s)
+
+
 # ---- arguments
 
 def test_memory_of_another_device_is_refused(monkeypatch):
