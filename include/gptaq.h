@@ -320,8 +320,9 @@ int gptaq_linear_i8(const int8_t* X, const float* x_scales, int64_t tokens, int6
  *   code = clamp(rint(Y / scale), -127, 127), with Y / scale taken as Y * (1 / scale) (a code within 2^-15 of a
  *   rounding boundary may go either way).  clip in (0, 1].  A row of zeros has scale 0; a row with a value that is not
  *   finite has scale NaN.
- * All sums and products in fp32, each output rounded once.  An output may be an input's own memory (same pointer and
- * leading dimension); otherwise they must not overlap. */
+ * All sums and products in fp32, each output rounded once.  A bf16 output may be an input's own memory (same pointer and
+ * leading dimension); otherwise they must not overlap, and codes must not overlap an input (GPTAQ_EUNSUPPORTED where they begin
+ * where one does: a row of codes ends inside the inputs' rows that others still read). */
 int gptaq_rms_norm(const uint16_t* X, const uint16_t* residual, const uint16_t* weight, int64_t tokens, int64_t n,
                    int64_t ldx, int64_t ldr, float eps, uint16_t* sum, int64_t lds, uint16_t* Y, int64_t ldy,
                    void* stream);

@@ -118,8 +118,8 @@ struct RowArgs {
 // Bound by memory: 16384 x 8192 with residual 190 us, 5.7 TB/s read and written (a plain copy reaches 5.0); gated 16384 x 11008 187 us, 5.8 TB/s; one
 // row of 4096 4 us, most of it the launch.
 // One row per workgroup (T threads) or, rows of one wavefront, several rows per workgroup.  A thread keeps its first KEEP pieces of
-// eight columns between the pass that takes the row's sums and the one that writes; later pieces are read again.  Outputs may be
-// the inputs' own memory: a thread writes only columns that it has read, and reads no others.
+// eight columns between the pass that takes the row's sums and the one that writes; later pieces are read again.  Outputs in bf16 may be
+// the inputs' own memory: a thread writes only columns that it has read, and reads no others.  (Codes take half the bytes: not where other threads' columns were.)
 // 8 bits: scale = clip * max|y| / 127, code = rint(y / scale); the maximum is taken of |h w| and multiplied by the positive 1 / rms
 // afterwards, so one pass and one reduction give both.
 template <bool NORM, bool CODES>
@@ -259,6 +259,7 @@ static int launch_rows(RowArgs p, bool norm, void* stream) {
 
 constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 8, kMaxColumns = (int64_t)1 << 24;
 static bool odd(const void* a) { return ((uintptr_t)a & 1) != 0; }
+static bool same(const void* a, const void* b) { return a == b; }
 
 static int norm_args(RowArgs& p, const uint16_t* X, const uint16_t* residual, const uint16_t* weight, int64_t tokens, int64_t n,
                      int64_t ldx, int64_t ldr, float eps, uint16_t* sum, int64_t lds, int64_t ldy) {
@@ -304,6 +305,7 @@ extern "C" int gptaq_rms_norm_i8(const uint16_t* X, const uint16_t* residual, co
   RowArgs p;
   if (const int rc = norm_args(p, X, residual, weight, tokens, n, ldx, ldr, eps, sum, lds, ldc)) return rc;
   if (!(clip > 0.f && clip <= 1.f)) return GPTAQ_EUNSUPPORTED;
+  if (tokens != 0 && (same(codes, X) || same(codes, residual) || same(codes, sum))) return GPTAQ_EUNSUPPORTED;
   p.codes = codes; p.scales = scales; p.clip = clip;
   return launch_rows(p, true, stream);
 }
@@ -324,6 +326,7 @@ extern "C" int gptaq_silu_mul_i8(const uint16_t* gate, const uint16_t* up, int64
   RowArgs p;
   if (const int rc = gated_args(p, gate, up, tokens, n, ldg, ldu, ldc)) return rc;
   if (!(clip > 0.f && clip <= 1.f)) return GPTAQ_EUNSUPPORTED;
+  if (tokens != 0 && (same(codes, gate) || same(codes, up))) return GPTAQ_EUNSUPPORTED;
   p.codes = codes; p.scales = scales; p.clip = clip;
   return launch_rows(p, false, stream);
 }

@@ -206,3 +206,16 @@ def test_weights_are_copied_pickled_and_saved(lib, tmp_path):
         with pytest.raises(AttributeError):
             v.bias = None
     assert copy.deepcopy(weights(perm=None, bias=None)).perm is None
+
+
+def test_codes_in_the_inputs_memory_are_refused(lib):
+    """One byte an element against two: rows of codes would lie where other rows' inputs are still read.  bf16 outputs may lie there."""
+    other = [ctypes.c_void_p(4096 * k) for k in (1, 2, 3, 4)]
+    for k in (0, 1, 3):                                                             # codes as x, residual, sum
+        x, r, codes, s = other
+        codes = (x, r, None, s)[k]
+        assert lib.gptaq_rms_norm_i8(x, r, NULL, 4, 64, 64, 64, 1e-5, s, 64, 1.0, codes, 64, ONE, NULL) == -3
+        assert lib.gptaq_rms_norm_i8(x, r, NULL, 0, 64, 64, 64, 1e-5, s, 64, 1.0, codes, 64, ONE, NULL) == 0
+    for codes in other[:2]:
+        assert lib.gptaq_silu_mul_i8(other[0], other[1], 4, 64, 64, 64, 1.0, codes, 64, ONE, NULL) == -3
+        assert lib.gptaq_silu_mul_i8(other[0], other[1], 0, 64, 64, 64, 1.0, codes, 64, ONE, NULL) == 0
