@@ -292,7 +292,7 @@ int gptaq_pack_codes(const uint8_t* codes, int64_t m, int64_t n, int64_t ldc, in
  *   bias   : m x fp32 or NULL.
  *   Y      : (tokens x m), leading dimension ldy, fp32 where y_f32 != 0, else bf16.  Must not overlap the inputs.
  *   ws     : >= gptaq_linear_workspace_bytes(tokens, m, n) bytes, 256-byte aligned; the size for more tokens serves fewer.
- *   m, n   : at most 2^20; tokens at most 2^23.
+ *   m, n   : at most 2^20, and m n (m rounded up to a multiple of 16, n to one of 128) at most 2^34; tokens at most 2^23.
  * Weights enter the products exactly; sums are taken in fp32 (bf16 activations) or, inside a group, in int32 (8 bits),
  * group sums are scaled and added in fp32, and the result is rounded once.  With up to 16 tokens, many rows, bf16 activations
  * and a bf16 output, the sum of a group, or of 128 columns of a longer one, may be that of (16 + code) x less (16 + zero)

@@ -340,7 +340,11 @@ static hipError_t launch_linear(const LinearArgs& p, int gs, bool i8, float* par
 
 // ---- argument checks
 
-constexpr int64_t kMaxSide = (int64_t)1 << 20, kMaxTokens = (int64_t)1 << 23;
+constexpr int64_t kMaxSide = (int64_t)1 << 20, kMaxTokens = (int64_t)1 << 23, kMaxTiles = (int64_t)1 << 23;
+// (A workgroup a tile lays the weights out, and a grid has less than 2^32 threads.)
+static bool good_size(int64_t m, int64_t n) {
+  return m > 0 && n > 0 && m <= kMaxSide && n <= kMaxSide && ((m + 15) / 16) * ((n + 127) / 128) <= kMaxTiles;
+}
 static bool good_group(int64_t n, int group) {
   return group <= 0 || ((group == 32 || group == 64 || group == 128) && n % group == 0);
 }
@@ -353,7 +357,7 @@ static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, i
                       int64_t m, int64_t n, int group, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes, void* stream) {
   if (!weights || (tokens != 0 && (!X || !Y || !ws || (i8 && !xs)))) return GPTAQ_ENULL;      // (no tokens: nothing to point to)
   const uintptr_t y_align = y_f32 ? 3 : 1;
-  if (tokens < 0 || tokens > kMaxTokens || m <= 0 || n <= 0 || m > kMaxSide || n > kMaxSide || ldx < n || ldy < m ||
+  if (tokens < 0 || tokens > kMaxTokens || !good_size(m, n) || ldx < n || ldy < m ||
       ((uintptr_t)weights & 255) || ((uintptr_t)Y & y_align) || (!i8 && ((uintptr_t)X & 1)) || (((uintptr_t)xs | (uintptr_t)bias | (uintptr_t)perm) & 3))
     return GPTAQ_EDIM;
   if (!good_group(n, group)) return GPTAQ_EUNSUPPORTED;
@@ -398,18 +402,17 @@ static int run_linear(bool i8, const void* X, const float* xs, int64_t tokens, i
 using namespace gptaq;
 
 extern "C" size_t gptaq_linear_weights_bytes(int64_t m, int64_t n, int group) {
-  if (m <= 0 || n <= 0 || m > kMaxSide || n > kMaxSide || !good_group(n, group)) return 0;
+  if (!good_size(m, n) || !good_group(n, group)) return 0;
   return linear_layout(m, n, group > 0 ? group : 0).bytes;
 }
 
 extern "C" int gptaq_linear_pack(const uint8_t* codes, int64_t ldc, const float* scales, const float* zeros, int64_t m, int64_t n, int group,
                                  void* weights, size_t weights_bytes, int32_t* info, void* stream) {
   if (!codes || !scales || !zeros || !weights || !info) return GPTAQ_ENULL;
-  if (m <= 0 || n <= 0 || m > kMaxSide || n > kMaxSide || ldc < n || (((uintptr_t)scales | (uintptr_t)zeros | (uintptr_t)info) & 3)) return GPTAQ_EDIM;
+  if (!good_size(m, n) || ldc < n || (((uintptr_t)scales | (uintptr_t)zeros | (uintptr_t)info) & 3)) return GPTAQ_EDIM;
   if (!good_group(n, group)) return GPTAQ_EUNSUPPORTED;
   const LinearLayout l = linear_layout(m, n, group > 0 ? group : 0);
   if (((uintptr_t)weights & 255) || weights_bytes < l.bytes) return GPTAQ_EWORKSPACE;
-  if (l.mt * l.kt > ((int64_t)1 << 23)) return GPTAQ_EDIM;
   const hipStream_t s = (hipStream_t)stream;
   uint8_t* to = (uint8_t*)weights;
   const size_t end = l.zeros + (size_t)(l.mt * l.groups) * 16;
@@ -424,7 +427,7 @@ extern "C" int gptaq_linear_pack(const uint8_t* codes, int64_t ldc, const float*
 }
 
 extern "C" size_t gptaq_linear_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
-  if (tokens <= 0 || tokens > kMaxTokens || m <= 0 || n <= 0 || m > kMaxSide || n > kMaxSide) return 0;
+  if (tokens <= 0 || tokens > kMaxTokens || !good_size(m, n)) return 0;
   return gather_bytes(tokens, n) + (linear_partial_bytes(tokens, m, n) + 255) / 256 * 256;
 }
 

@@ -219,3 +219,14 @@ def test_codes_in_the_inputs_memory_are_refused(lib):
     for codes in other[:2]:
         assert lib.gptaq_silu_mul_i8(other[0], other[1], 4, 64, 64, 64, 1.0, codes, 64, ONE, NULL) == -3
         assert lib.gptaq_silu_mul_i8(other[0], other[1], 0, 64, 64, 64, 1.0, codes, 64, ONE, NULL) == 0
+
+
+def test_sizes_are_those_that_pack_takes(lib):
+    """A layer has a size of weights, and of a workspace, where gptaq_linear_pack and gptaq_linear take it, and only there."""
+    k, off = 1 << 10, ctypes.c_void_p(264)                                          # (misaligned weights: what is refused last)
+    for m, n, fits in ((128 * k, 128 * k, True), (128 * k + 1, 128 * k, False), (128 * k, 128 * k + 1, False), (k * k, k * k, False), (k * k, 16 * k, True),
+                       (k * k, 16 * k + 1, False), (16 * k, k * k, True), (16 * k + 1, k * k, False), (1, k * k, True), (k * k, 1, True), (k * k + 1, 1, False),
+                       (0, 1, False), (4096, 11008, True)):
+        assert (lib.gptaq_linear_weights_bytes(m, n, 0) > 0) == fits and (lib.gptaq_linear_workspace_bytes(1, m, n) > 0) == fits, (m, n)
+        assert lib.gptaq_linear_pack(ONE, n, ONE, ONE, m, n, 0, off, 1 << 62, ONE, NULL) == (-4 if fits else -2), (m, n)
+        assert lib.gptaq_linear(ONE, 1, n, NULL, ONE, 1 << 62, m, n, 0, NULL, ONE, m, 0, off, 1 << 62, NULL) == (-4 if fits else -2), (m, n)
