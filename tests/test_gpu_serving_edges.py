@@ -116,3 +116,31 @@ def test_stored_weights_run_as_before(tmp_path):
     with torch.serialization.safe_globals([B.LinearWeights]):
         again = torch.load(tmp_path / "layer.pt", weights_only=True)
     assert torch.equal(B.gptaq_linear(x, again, ws), B.gptaq_linear(x, w, ws))
+
+
+def test_one_row_or_one_column_with_any_stride():
+    """A row alone is row-major whatever its stride is, and so is a column alone: torch says contiguous, and so do the calls."""
+    n, m = 96, 40
+    lone = lambda t: t.reshape(-1, 1).clone().t()                                 # (1, n), strides (1, 1)
+    x, res, g = (bf16(rng(k, 95).standard_normal((1, n))) for k in range(3))
+    assert lone(x).stride(0) == 1 and lone(x).is_contiguous()
+    codes, scales, zeros = quantised(m, n, 4, 32, False, rng(96))
+    w, ws = pack(codes, scales, zeros, 32), B.workspace(B.gptaq_linear_workspace_bytes(4, m, n))
+    y = B.gptaq_linear(x, w, ws)
+    assert torch.equal(B.gptaq_linear(lone(x), w, ws), y) and torch.equal(B.gptaq_linear(x.expand(4, n)[:1], w, ws, out=lone(y)), y)
+    c, s, total = B.gptaq_rms_norm_i8(x, None, 1e-5, residual=res)
+    assert all(torch.equal(a, b) for a, b in zip(B.gptaq_rms_norm_i8(lone(x), None, 1e-5, residual=lone(res), total=lone(x)), (c, s, total)))
+    assert torch.equal(B.gptaq_linear_i8(lone(c), s, w, ws), B.gptaq_linear_i8(c, s, w, ws))
+    h, _ = B.gptaq_rms_norm(x, None, 1e-5)
+    assert torch.equal(B.gptaq_rms_norm(lone(x), None, 1e-5, out=lone(x))[0], h)
+    assert torch.equal(B.gptaq_silu_mul(lone(g), lone(x), out=lone(x)), B.gptaq_silu_mul(g, x))
+    assert all(torch.equal(a, b) for a, b in zip(B.gptaq_silu_mul_i8(lone(g), lone(x)), B.gptaq_silu_mul_i8(g, x)))
+    one = [torch.from_numpy(a[:1].copy()).cuda() for a in (codes, scales, zeros)]
+    v = B.gptaq_linear_pack(lone(one[0]), one[1], one[2], 32)
+    assert torch.equal(B.gptaq_linear(x, v, ws), y[:, :1])
+    column = bf16(rng(97).standard_normal((1, 3))).t()                            # (3, 1), strides (1, 3)
+    assert column.stride(1) == 3
+    assert torch.equal(B.gptaq_silu_mul(column, column), B.gptaq_silu_mul(column.contiguous().clone(), column.clone()))
+    wide = torch.zeros((3, 8), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(B.GptaqError):
+        B.gptaq_silu_mul(wide[:, ::2], wide[:, ::2])
