@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2504_02692_amd import binding as B
-from tests.test_gpu_serving import bf16, dequantised, f64, pack, quantised, rng
+from tests.test_gpu_serving import bf16, dequantised, f64, pack, padded, quantised, rng
 
 pytestmark = pytest.mark.gpu
 
@@ -57,7 +57,148 @@ def test_fp32_outputs_keep_small_activations_beside_a_large_one(tokens, group, m
     assert np.array_equal(f64(got), x @ dequantised(codes, scales, zeros, group).T)
 
 
+def whole(tokens, m, n, group, perm=False, bias=False):
+    """Activations of at most two bits and a sign, all codes and zeros, scales of 1/2 and 1: sums below 2^24 halves, and (16 + code) x likewise.
+    Returns (weights, activations as fp64, outputs in fp64), on the GPU."""
+    assert 2 * 31 * 3 * n < 2 ** 24
+    g = torch.Generator(device="cuda").manual_seed(tokens + 7 * m + 11 * n + group)
+    rand = lambda hi, *shape: torch.randint(0, hi, shape, device="cuda", generator=g)
+    G = n // group if group else 1
+    codes, zeros, scales = rand(16, m, n).to(torch.uint8), rand(16, m, G).float(), 0.5 * (1 + rand(2, m, G)).float()
+    x = (rand(7, tokens, n) - 3).double()
+    p = torch.randperm(n, device="cuda", generator=g).to(torch.int32) if perm else None
+    b = (rand(64, m) - 32).float() if bias else None
+    w = B.gptaq_linear_pack(codes, scales, zeros, group, perm=p, bias=b)
+    assert w.info.item() == 0
+    W = ((codes.view(m, G, -1).double() - zeros.double()[:, :, None]) * scales.double()[:, :, None]).view(m, n)
+    want = torch.matmul(x[:, p.long()] if perm else x, W.t())
+    return w, x, want + b.double() if bias else want
+
+
+def product(x, w, dtype, i8, ws=None, out=None):
+    ws = B.workspace(B.gptaq_linear_workspace_bytes(x.shape[0], w.m, w.n)) if ws is None else ws
+    if i8:
+        return B.gptaq_linear_i8(x.to(torch.int8), torch.ones(x.shape[0], device="cuda"), w, ws, dtype=dtype, out=out)
+    return B.gptaq_linear(x.to(torch.bfloat16), w, ws, dtype=dtype, out=out)
+
+
+def check_whole(tokens, m, n, group, i8, **other):
+    print("whole", tokens, m, n, group, i8, other, flush=True)
+    w, x, want = whole(tokens, m, n, group, **other)
+    assert torch.equal(want.float().double(), want)
+    for dtype in (torch.float32, torch.bfloat16):
+        y = product(x, w, dtype, i8)
+        assert torch.equal(y, want.float().to(dtype)), (dtype, (y.double() - want).abs().max().item())
+
+
+# Rows in their hundreds of tiles, not a whole number of 32 or 64: a workgroup of the kernel of few tokens takes two tiles of them, then four.  Columns: several
+# tiles to each wavefront and a remainder.
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+@pytest.mark.parametrize("m,n", [(8200, 2176), (8200, 8320), (16400, 2176), (16400, 8320)])
+@pytest.mark.parametrize("tokens", [1, 9, 16, 17, 32])
+def test_few_tokens_of_large_layers_are_exact(tokens, m, n, group, i8):
+    check_whole(tokens, m, n, group, i8)
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("tokens,m,n,perm", [(1, 8200, 2100, False), (16, 16400, 2100, True), (20, 8200, 1700, True), (32, 16400, 2100, False)])
+def test_few_tokens_of_large_layers_of_any_width_are_exact(tokens, m, n, perm, i8):
+    check_whole(tokens, m, n, 0, i8, perm=perm, bias=True)
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+@pytest.mark.parametrize("tokens,m,n", [(1, 100, 16384), (16, 100, 16384), (30, 100, 16384), (200, 2100, 8320), (700, 2100, 16384), (1100, 4100, 8192)])
+def test_long_rows_are_exact(tokens, m, n, group, i8):
+    check_whole(tokens, m, n, group, i8)
+
+
+@pytest.mark.parametrize("group", [0, 64, 128])
+@pytest.mark.parametrize("tokens,m", [(5, 8200), (16, 8200), (1, 16400), (16, 16400)])
+def test_large_layers_pass_on_what_is_not_finite(tokens, m, group):
+    """An infinity or a NaN spoils its own token alone.  An activation that overflows times 16 + code, but meets codes equal to their zeros, spoils nothing."""
+    n = 2176
+    w, x, want = whole(tokens, m, n, group)
+    G = n // group if group else 1
+    W = torch.empty((m, n), dtype=torch.float64, device="cuda")
+    for lo in range(0, n, 16):                                     # the weights' columns, by the products themselves
+        unit = torch.zeros((16, n), dtype=torch.float64, device="cuda")
+        unit[torch.arange(16), torch.arange(lo, lo + 16)] = 1.0
+        W[:, lo:lo + 16] = product(unit, w, torch.float32, False).t()
+    assert torch.equal(torch.matmul(x, W.t()), want)
+    ws = B.workspace(B.gptaq_linear_workspace_bytes(tokens, m, n))
+    for at, value in ((37, float("inf")), (n - 1, float("-inf")), (5, float("nan"))):
+        bad = x.clone()
+        bad[0, at] = value
+        y = product(bad, w, torch.bfloat16, False, ws)
+        assert torch.equal(y[1:], want[1:].float().to(torch.bfloat16))
+        col = W[:, at]
+        if value == value:
+            sign = col if value > 0 else -col
+            assert torch.all(torch.isposinf(y[0][sign > 0])) and torch.all(torch.isneginf(y[0][sign < 0])) and torch.all(torch.isnan(y[0][sign == 0]))
+        else:
+            assert torch.isnan(y[0]).all()
+    codes = torch.randint(0, 16, (m, n), dtype=torch.uint8, device="cuda")
+    codes[:, 41] = 7
+    v = B.gptaq_linear_pack(codes, torch.ones((m, G), device="cuda"), torch.full((m, G), 7.0, device="cuda"), group)
+    huge = x.clone()
+    huge[:, 41] = 0.0
+    plain = product(huge, v, torch.bfloat16, False, ws)
+    huge[0, 41], huge[tokens - 1, 41] = 2.0 ** 127, -2.0 ** 127
+    assert torch.equal(product(huge, v, torch.bfloat16, False, ws), plain)
+
+
+@pytest.mark.parametrize("i8", [False, True])
+@pytest.mark.parametrize("tokens,m,n,group", [(700, 2100, 2048, 64), (1030, 4100, 1024, 0), (200, 2100, 8192, 128), (40, 1100, 16384, 32), (33, 8200, 256, 128)])
+def test_many_tokens_with_rows_apart_are_read_in_place(tokens, m, n, group, i8):
+    """Rows that start at 16 bytes but do not follow each other; what lies between them is NaN or 77."""
+    w, x, _ = whole(tokens, m, n, group)
+    x = x.to(torch.int8 if i8 else torch.bfloat16)
+    apart = padded(x, 48)
+    assert apart.data_ptr() % 16 == 0 and apart.stride(0) == n + 48
+    ws, ones = B.workspace(B.gptaq_linear_workspace_bytes(tokens, m, n)), torch.ones(tokens, device="cuda")
+    call = (lambda t: B.gptaq_linear_i8(t, ones, w, ws)) if i8 else (lambda t: B.gptaq_linear(t, w, ws))
+    assert torch.equal(call(apart), call(x))
+
+
+@pytest.mark.parametrize("ldx", [(1 << 23) - 8, 1 << 23])
+def test_many_tokens_with_rows_far_apart(ldx):
+    """As far as the kernel of many tokens reads them in place, and farther; outputs more than 2^32 elements from the first."""
+    tokens, m, n, ldy = 300, 2100, 256, 1 << 24
+    w, x, want = whole(tokens, m, n, 64)
+    X = torch.empty((tokens - 1) * ldx + n, dtype=torch.bfloat16, device="cuda").as_strided((tokens, n), (ldx, 1))
+    Y = torch.empty((tokens - 1) * ldy + m, dtype=torch.bfloat16, device="cuda").as_strided((tokens, m), (ldy, 1))
+    X.copy_(x)
+    B.gptaq_linear(X, w, B.workspace(B.gptaq_linear_workspace_bytes(tokens, m, n)), out=Y)
+    assert torch.equal(Y, want.float().to(torch.bfloat16))
+
+
+def test_more_tokens_than_one_launch_takes():
+    """The most rows that a layer may have: 4096 tokens to a launch, the rest to another."""
+    tokens, m, n = 4100, 1 << 20, 128
+    g = torch.Generator(device="cuda").manual_seed(5)
+    codes = torch.randint(0, 16, (m, n), dtype=torch.uint8, device="cuda", generator=g)
+    w = B.gptaq_linear_pack(codes, torch.ones((m, 1), device="cuda"), torch.full((m, 1), 8.0, device="cuda"), 128)
+    x = (torch.randint(0, 7, (tokens, n), device="cuda", generator=g) - 3).float()
+    y = B.gptaq_linear(x.to(torch.bfloat16), w, B.workspace(B.gptaq_linear_workspace_bytes(tokens, m, n)))
+    for lo in range(0, m, 1 << 17):
+        want = torch.matmul(x, (codes[lo:lo + (1 << 17)].float() - 8.0).t())
+        assert torch.equal(y[:, lo:lo + (1 << 17)], want.to(torch.bfloat16)), lo
+
+
 # ---- rows
+
+def test_more_rows_than_one_launch_takes():
+    tokens, n = (1 << 21) + 5, 8
+    x = torch.randn((tokens, n), device="cuda", generator=torch.Generator(device="cuda").manual_seed(6)).to(torch.bfloat16)
+    y, _ = B.gptaq_rms_norm(x, None, 1e-5)
+    codes, scales = B.gptaq_silu_mul_i8(x, x)
+    for part in (slice(0, 100), slice((1 << 21) - 50, tokens)):
+        assert torch.equal(y[part], B.gptaq_rms_norm(x[part].clone(), None, 1e-5)[0])
+        c, s = B.gptaq_silu_mul_i8(x[part].clone(), x[part].clone())
+        assert torch.equal(codes[part], c) and torch.equal(scales[part], s)
+
 
 @pytest.mark.parametrize("n", [40, 4096, 33000])
 @pytest.mark.parametrize("eps", [0.0, 1e-5])
