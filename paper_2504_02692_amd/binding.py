@@ -154,9 +154,9 @@ def _here(*tensors: Optional[torch.Tensor]) -> int:
     return device
 
 
-def _ld(t: torch.Tensor) -> int:
-    """Distance between rows; of one row alone torch may give any stride."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _ld(t: torch.Tensor, rows: int, n: int) -> int:
+    """Distance between the rows of a rows x n tensor; of one row alone torch may give any stride."""
+    return t.stride(0) if rows > 1 else n
 
 
 def _need(t: torch.Tensor, dtype, name: str) -> None:
@@ -496,7 +496,7 @@ def gptaq_linear_pack(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Te
     device = _here(codes, scales, zeros, perm, bias)
     data = workspace(gptaq_linear_weights_bytes(m, n, group), codes.device)
     info = torch.empty(1, dtype=torch.int32, device=codes.device)
-    _check(load().gptaq_linear_pack(_ptr(codes), _ld(codes), _ptr(scales), _ptr(zeros), m, n, int(group), _ptr(data), data.numel(),
+    _check(load().gptaq_linear_pack(_ptr(codes), _ld(codes, m, n), _ptr(scales), _ptr(zeros), m, n, int(group), _ptr(data), data.numel(),
                                     _ptr(info), _stream(device)), "gptaq_linear_pack")
     return LinearWeights(data, m, n, max(0, int(group)), perm, bias, info)
 
@@ -505,8 +505,7 @@ def gptaq_linear_workspace_bytes(tokens: int, m: int, n: int) -> int:
     return load().gptaq_linear_workspace_bytes(tokens, m, n)
 
 
-def _linear_out(X: torch.Tensor, w: LinearWeights, dtype, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
-    tokens, n = X.shape
+def _linear_out(X: torch.Tensor, tokens: int, n: int, w: LinearWeights, dtype, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
     if n != w.n:
         raise GptaqError(f"{name}: X has {n} columns, the weights {w.n}")
     if out is None:
@@ -524,8 +523,9 @@ def gptaq_linear(X: torch.Tensor, weights: LinearWeights, ws: torch.Tensor, out:
     """X W^T + bias for token-major bf16 X; returns (tokens x m), bf16 or fp32 (`dtype`, or the type of `out`)."""
     _need(X, torch.bfloat16, "X")
     device = _here(X, out)
-    Y = _linear_out(X, weights, dtype, out, "gptaq_linear")
-    _check(load().gptaq_linear(X.data_ptr(), X.shape[0], _ld(X), *weights._args(device), Y.data_ptr(), _ld(Y),
+    tokens, n = X.shape
+    Y = _linear_out(X, tokens, n, weights, dtype, out, "gptaq_linear")
+    _check(load().gptaq_linear(X.data_ptr(), tokens, _ld(X, tokens, n), *weights._args(device), Y.data_ptr(), _ld(Y, tokens, weights.m),
                                Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear")
     return Y
 
@@ -534,12 +534,13 @@ def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWe
                     out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
     """gptaq_linear for 8-bit activations scales[t] * codes[t][:]."""
     _need(codes, torch.int8, "codes"); _need_vec(scales, torch.float32, "scales")
-    if scales.shape[0] != codes.shape[0]:
+    tokens, n = codes.shape
+    if scales.numel() != tokens:
         raise GptaqError("gptaq_linear_i8: scales: expected one per token")
     device = _here(codes, scales, out)
-    Y = _linear_out(codes, weights, dtype, out, "gptaq_linear_i8")
-    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), codes.shape[0], _ld(codes), *weights._args(device), Y.data_ptr(),
-                                  _ld(Y), Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear_i8")
+    Y = _linear_out(codes, tokens, n, weights, dtype, out, "gptaq_linear_i8")
+    _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), tokens, _ld(codes, tokens, n), *weights._args(device), Y.data_ptr(),
+                                  _ld(Y, tokens, weights.m), Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear_i8")
     return Y
 
 
@@ -579,8 +580,8 @@ def gptaq_rms_norm(X: torch.Tensor, weight: Optional[torch.Tensor], eps: float, 
     total = _norm_args(X, weight, residual, total, "gptaq_rms_norm")
     tokens, n = X.shape
     Y = _like(X, out, "gptaq_rms_norm")
-    _check(load().gptaq_rms_norm(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, _ld(X), _ld(residual) if residual is not None else 0,
-                                 float(eps), _ptr(total), _ld(total) if total is not None else 0, _ptr(Y), _ld(Y), _stream(device)),
+    _check(load().gptaq_rms_norm(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, _ld(X, tokens, n), _ld(residual, tokens, n) if residual is not None else 0,
+                                 float(eps), _ptr(total), _ld(total, tokens, n) if total is not None else 0, _ptr(Y), _ld(Y, tokens, n), _stream(device)),
            "gptaq_rms_norm")
     return Y, total
 
@@ -592,8 +593,8 @@ def gptaq_rms_norm_i8(X: torch.Tensor, weight: Optional[torch.Tensor], eps: floa
     total = _norm_args(X, weight, residual, total, "gptaq_rms_norm_i8")
     tokens, n = X.shape
     codes, scales = X.new_empty((tokens, n), dtype=torch.int8), X.new_empty(tokens, dtype=torch.float32)
-    _check(load().gptaq_rms_norm_i8(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, _ld(X), _ld(residual) if residual is not None else 0,
-                                    float(eps), _ptr(total), _ld(total) if total is not None else 0, float(clip), _ptr(codes), n,
+    _check(load().gptaq_rms_norm_i8(_ptr(X), _ptr(residual), _ptr(weight), tokens, n, _ld(X, tokens, n), _ld(residual, tokens, n) if residual is not None else 0,
+                                    float(eps), _ptr(total), _ld(total, tokens, n) if total is not None else 0, float(clip), _ptr(codes), n,
                                     _ptr(scales), _stream(device)), "gptaq_rms_norm_i8")
     return codes, scales, total
 
@@ -610,7 +611,7 @@ def gptaq_silu_mul(gate: torch.Tensor, up: torch.Tensor, out: Optional[torch.Ten
     _gated_args(gate, up, "gptaq_silu_mul")
     tokens, n = gate.shape
     Y = _like(gate, out, "gptaq_silu_mul")
-    _check(load().gptaq_silu_mul(_ptr(gate), _ptr(up), tokens, n, _ld(gate), _ld(up), _ptr(Y), _ld(Y), _stream(device)), "gptaq_silu_mul")
+    _check(load().gptaq_silu_mul(_ptr(gate), _ptr(up), tokens, n, _ld(gate, tokens, n), _ld(up, tokens, n), _ptr(Y), _ld(Y, tokens, n), _stream(device)), "gptaq_silu_mul")
     return Y
 
 
@@ -620,6 +621,6 @@ def gptaq_silu_mul_i8(gate: torch.Tensor, up: torch.Tensor, clip: float = 1.0):
     _gated_args(gate, up, "gptaq_silu_mul_i8")
     tokens, n = gate.shape
     codes, scales = gate.new_empty((tokens, n), dtype=torch.int8), gate.new_empty(tokens, dtype=torch.float32)
-    _check(load().gptaq_silu_mul_i8(_ptr(gate), _ptr(up), tokens, n, _ld(gate), _ld(up), float(clip), _ptr(codes), n, _ptr(scales),
+    _check(load().gptaq_silu_mul_i8(_ptr(gate), _ptr(up), tokens, n, _ld(gate, tokens, n), _ld(up, tokens, n), float(clip), _ptr(codes), n, _ptr(scales),
                                     _stream(device)), "gptaq_silu_mul_i8")
     return codes, scales
