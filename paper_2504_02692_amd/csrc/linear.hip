@@ -55,7 +55,8 @@ __global__ void linear_clear_kernel(int32_t* info, uint8_t* tail, int count) {
 }
 
 // ---- activations that the products cannot read as they are: columns in another order, rows that do not start at 16 bytes or end
-// inside a piece of 16.  Rows of `out` have `ldo` elements, zeros behind the n-th.
+// inside a piece of 16.  Rows of `out` have `ldo` elements, zeros behind the n-th.  A workgroup a row, each thread's loads one behind the other: 5 us for
+// one row of 4096, 18 to 19 for one to 2048 rows of 8192 or 11008, latency throughout; more than the product of few tokens behind it.
 template <typename T>
 __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t ldx, const int32_t* perm, int n, T* out, int64_t ldo) {
   const T* row = x + (int64_t)blockIdx.x * ldx;
@@ -74,9 +75,9 @@ __global__ __launch_bounds__(256) void linear_gather_kernel(const T* x, int64_t 
 // wavefront independent many loads are in flight.  The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W (lane l: row l % 16), the
 // result has the row of W in l % 16 and tokens 4 (l / 16) .. + 3 in the lane's four values, so one scale per lane serves a result.
 // Bound by the weights' bytes where there are many: 28672 x 8192, one token, 8-bit activations 23 to 25 us, 5.0 to 5.4 TB/s; bf16 26 to 31 us, where unpacking the codes
-// takes most of the time that the bytes leave.  4096 x 4096 4.2 us, 2.2 TB/s: the launch, one trip to memory and the join.
+// takes most of the time that the bytes leave.  4096 x 4096 4.3 us, 2.1 TB/s: the launch, one trip to memory and the join.
 // Activations go to LDS in runs of a token's whole 128 columns, to a place of the wavefront's own, so that no wavefront waits for another.  (A load of
-// 16 tokens by 64 bytes to registers takes about four times as long as one of 1 KB in one run: 4096 x 11008, 16 tokens, 14.5 us; through LDS 9.3.)
+// 16 tokens by 64 bytes to registers takes about four times as long as one of 1 KB in one run: 4096 x 11008, 16 tokens, 14.5 us; through LDS 9.2.)
 // GS: groups per 128 columns (1, 2, 4), 0: one group per row.
 
 // Most wavefronts of a workgroup: 16 leave a lane 128 registers.
@@ -299,14 +300,14 @@ static hipError_t launch_few_as(const LinearArgs& p, int waves, hipStream_t s) {
 }
 // Tiles of rows per workgroup: the more, the less often the activations are read, the fewer workgroups.  us a call, RT 1 (8 wavefronts) / 2 (4, 8) / 4 (4):
 //              4096 x 4096          11008 x 4096               8192 x 8192                28672 x 8192
-//   1, bf16    4.2 / 6.7 5.4 / 8.7  8.7 / 8.6  8.6  / 9.5      9.7 / 11.4 9.2  / 15.1     35.8 / 31.2 29.6 / 29.9
+//   1, bf16    4.3 / 7.1 5.5 / 8.8  8.4 / 8.6  8.3  / 9.2      10.4 / 12.0 9.4 / 15.6     34.4 / 28.3 28.7 / 27.2
 //   1, int8    3.4 / 5.7 4.6 / 7.6  6.6 / 7.0  7.2  / 8.2      8.1 / 9.4  8.1  / 13.1     23.3 / 25.3 24.4 / 25.1
-//   16, bf16   5.1 / 7.4 6.2 / 10   10.1 / 9.6 9.6  / 10.7     12.0 / 12.4 10.6 / 16.9    44.3 / 35.1 35.1 / 31.5
+//   16, bf16   5.2 / 7.8 6.2 / 10   9.7 / 10.0 9.8  / 10.8     12.1 / 13.2 10.7 / 17.5    44.7 / 37.0 37.0 / 31.8
 //   16, int8   3.7 / 6.1 4.9 / 8.6  6.8 / 7.6  7.8  / 9.4      8.6 / 10.1 8.7  / 14.2     32.8 / 28.1 28.1 / 27.4
-//   32, bf16   7.5 / 10.4 8.3 / 14  17.6 / 13.9 15.6 / 15.6    19.9 / 17.8 14.3 / 23.4    77.6 / 50.3 54.9 / 42.6
+//   32, bf16   6.8 / 9.9 8.3 / 15   16.5 / 13.6 15.4 / 15.2    18.4 / 16.6 13.7 / 24.4    73.9 / 50.5 54.2 / 42.8
 //   32, int8   5.2 / 7.8 6.2 / 11   9.4 / 9.8  9.6  / 12.0     10.9 / 12.6 10.5 / 18.7    43.0 / 35.5 35.2 / 32.5
-// 16 wavefronts instead of 8, RT 1, one token: 4096 x 11008 8.0 -> 7.6, 1024 x 8192 5.3 -> 5.2, 4096 x 4096 4.2 -> 4.4, 11008 x 4096 8.7 -> 11.2.
-// With more scales a tile, fewer tiles fit in the registers.
+// 16 wavefronts instead of 8, RT 1, one token: 4096 x 11008 8.3 -> 7.6, 1024 x 8192 5.7 -> 5.3, 4096 x 4096 4.4 -> 4.2, 11008 x 4096 8.3 -> 10.5.
+// With more scales a tile, fewer tiles fit in the registers: 242 of 256 with two groups a tile (RT 4, one tile of tokens), 208 with one group and two tiles of tokens.
 template <bool I8, int GS, int TT>
 static hipError_t launch_few_rows(const LinearArgs& p, hipStream_t s) {
   constexpr int kMost = GS <= 1 ? 4 : GS == 2 ? (TT == 1 ? 4 : 2) : (TT == 1 ? 2 : 1), kTwo = kMost < 2 ? kMost : 2;
@@ -325,9 +326,9 @@ static hipError_t launch_few(const LinearArgs& p, int gs, hipStream_t s) {
 }
 
 // Above 32 tokens, in blocks of 32, as far as few workgroups have the work: us a call with this kernel / with that for many tokens, bf16 (workgroups times
-// tiles of columns): 4096 x 4096, 64 tokens 13.1 / 14.6 (512 x 32), 96 18.6 / 16.7; 1024 x 8192, 128 tokens 10.7 / 16.5 (256 x 64), 192 18.7 / 17.1;
-// 2048 x 2048, 192 tokens 13.2 / 14.9 (768 x 16), 256 17.8 / 16.0; 4096 x 11008, 64 tokens 24.9 / 22.6 (512 x 86).  8-bit: 4096 x 4096, 128 tokens 12.4 / 13.6
-// (1024 x 32), 256 20.9 / 18.8; 4096 x 11008, 64 tokens 13.7 / 19.4 (512 x 86), 128 24.6 / 21.2; 4096 x 1024, 128 tokens 5.9 / 6.7 (1024 x 8), 192 8.0 / 6.9.
+// tiles of columns): 4096 x 4096, 64 tokens 11.8 / 14.5 (512 x 32), 96 16.7 / 16.4; 1024 x 8192, 128 tokens 9.8 / 16.3 (256 x 64), 192 17.6 / 16.7;
+// 2048 x 2048, 192 tokens 10.9 / 13.5 (768 x 16), 256 15.2 / 15.0; 4096 x 11008, 64 tokens 23.9 / 22.7 (512 x 86).  8-bit: 4096 x 4096, 128 tokens 12.9 / 14.6
+// (1024 x 32), 256 22.2 / 19.0; 4096 x 11008, 64 tokens 14.1 / 19.4 (512 x 86), 128 26.2 / 20.8; 4096 x 1024, 128 tokens 5.7 / 6.6 (1024 x 8), 192 7.8 / 6.7.
 static bool few_tokens(const LinearArgs& p, bool i8) {
   const int64_t workgroups = (int64_t)p.mt * ((p.tokens + 31) / 32);
   return p.tokens <= 32 || (workgroups <= (i8 ? 1280 : 768) && workgroups * p.kt <= (i8 ? 49152 : 16384));

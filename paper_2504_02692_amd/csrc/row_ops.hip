@@ -236,7 +236,7 @@ __global__ __launch_bounds__(1024) void row_kernel(RowArgs p) {
 static int launch_rows(RowArgs p, bool norm, void* stream) {
   const int pieces = (p.n + 7) / 8;
   // Threads of a row.  With few rows, or nothing to reduce, one piece each: a row takes the least time.  With many rows two to four pieces, and 512
-  // threads as far as these hold a row, so that four rows share a CU and one reads while another waits in its reduction.
+  // threads as far as these hold a row, so that three rows share a CU (76 to 79 registers: six wavefronts a SIMD) and one reads while another waits in its reduction.
   // 16384 x 8192, norm / 8 bits, 1024, 512, 256 threads: 237 / 254, 194 / 197, 203 / 191 us; 16384 x 11008, 1024, 704, 512: 338 / 388, 277 / 307, 265 / 268.
   const bool reduces = norm || p.codes;
   int T = p.tokens < 512 || !reduces ? pieces : pieces <= 2048 ? (pieces + 1) / 2 : (pieces + 3) / 4;
