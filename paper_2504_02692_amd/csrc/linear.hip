@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * few_waves(GS, RT, TT)) void linear_few_kernel(
   // A bf16 output's own rounding hides that; outputs in fp32 are EXACT, and where a result is not finite the subtraction may be why, and the workgroup takes
   // its sums again with EXACT.
   // One matrix instruction for an operand (TT 1) and one sum of activations for several operands (RT) is where it pays: us a call, EXACT / else, one token:
-  // 28672 x 8192 33 / 29, 22016 x 4096 15.9 / 13.0, 11008 x 4096 10.3 / 9.1; RT 1: 4096 x 11008 7.7 / 7.8, 16 tokens 9.2 / 9.7; TT 2, 32 tokens:
+  // 28672 x 8192 33 / 29 (groups of 32 40 / 41), 22016 x 4096 15.9 / 12.9, 11008 x 4096 10.3 / 9.1; RT 1: 4096 x 11008 7.7 / 7.8, 16 tokens 9.2 / 9.7; TT 2, 32 tokens:
   // 4096 x 11008 13.1 / 14.3, 11008 x 4096 13.5 / 14.0, 28672 x 8192 42 / 49 (registers spill).
   constexpr bool kSixteen = !I8 && TT == 1 && RT > 1;
   auto add_scaled = [&](auto exact, int r, float s, uint32_t zero) {
