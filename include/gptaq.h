@@ -334,6 +334,69 @@ int gptaq_silu_mul(const uint16_t* gate, const uint16_t* up, int64_t tokens, int
 int gptaq_silu_mul_i8(const uint16_t* gate, const uint16_t* up, int64_t tokens, int64_t n, int64_t ldg, int64_t ldu,
                       float clip, int8_t* codes, int64_t ldc, float* scales, void* stream);
 
+/* gptaq_linear8_pack, gptaq_linear8_i8: the same for layers solved with up to 8 bits, one scale and zero a row (gptaq_quantize_layer with group <= 0;
+ *   with 5 to 8 bits the only grid these products take), and 8-bit activations: Y[t][r] = scales[t] scale[r] sum_j (code[r][j] - zero[r]) x[t][p(j)] + bias[r].
+ *   codes  : 0 .. 255.  zeros: integers 0 .. 255.  Others as in gptaq_linear_pack and gptaq_linear_i8, but:
+ *   perm   : given to gptaq_linear8_pack: n x int32 or NULL, p(j) = perm[j]; a permutation of 0 .. n - 1.  The columns are laid out in the order of
+ *            the activations, so products of layers in another order take no longer.
+ *   weights: gptaq_linear8_weights_bytes(m, n) bytes, about m n + 8 m + 4 n.
+ *   info   : int32, out: 0, or 1 + a row whose zero is no integer in 0 .. 255, or -1 - a column that no entry of perm names (the weights are then garbage).
+ *   m      : at most 2^20, n at most 65536, and m n as in gptaq_linear.  Activation codes may be -128, too.
+ * The sum is exact in int32; it is converted to fp32, multiplied by scales[t] scale[r] (rounded once), the bias is added with that rounding, and the result is
+ * rounded to Y's type. */
+size_t gptaq_linear8_weights_bytes(int64_t m, int64_t n);
+int gptaq_linear8_pack(const uint8_t* codes, int64_t ldc, const float* scales, const float* zeros, int64_t m, int64_t n,
+                       const int32_t* perm, void* weights, size_t weights_bytes, int32_t* info, void* stream);
+size_t gptaq_linear8_workspace_bytes(int64_t tokens, int64_t m, int64_t n);
+int gptaq_linear8_i8(const int8_t* X, const float* x_scales, int64_t tokens, int64_t ldx, const void* weights, size_t weights_bytes,
+                     int64_t m, int64_t n, const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes,
+                     void* stream);
+
+/* gptaq_quant_activations_i8: rows that are in bf16 already (what attention leaves in front of o_proj) as 8-bit codes: scales[t] = clip * max|X[t][:]| / 127,
+ *   codes = clamp(rint(X / scale), -127, 127), rint of the fp32 quotient, half to even.  clip in (0, 1].  A row of zeros has scale 0 and codes 0; a row with a
+ *   value that is not finite has scale NaN.  codes must not overlap X (GPTAQ_EUNSUPPORTED where they begin there). */
+int gptaq_quant_activations_i8(const uint16_t* X, int64_t tokens, int64_t n, int64_t ldx, float clip, int8_t* codes, int64_t ldc,
+                               float* scales, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * What lies between the qkv product and o_proj of a decoder block: a paged cache of keys and values, and attention over it.
+ *
+ * The cache: keys (pages, kv_heads, d / 8, page, 8) and values (pages, kv_heads, page / 8, d, 8), bf16, contiguous, 16-byte aligned; `page` positions to a
+ *   page, a power of two from 16 to 256.  Entry e of the key of position p lies in keys[id][head][e / 8][p % page][e % 8], that of its value in
+ *   values[id][head][p % page / 8][e][p % 8], with id = table[s][p / page].
+ *   table  : (seqs x table_pages) int32, leading dimension ld_table: the pages of each sequence in order; those behind its length are not looked at.  An entry
+ *            outside 0 .. pages - 1 stands for a page that is not there (given back, for instance): nothing is written to it, and no token sees its positions.
+ *   starts : seqs + 1 int32, ascending: the new tokens of sequence s are rows starts[s] .. starts[s + 1] - 1 of q, k, v and out.  A sequence may have none.
+ *            Rows of no sequence are neither read nor written.
+ *   lengths: seqs int32: tokens of each sequence with the new ones; token i of count new ones has position lengths[s] - count + i.  Tokens with a
+ *            position below 0 or beyond the table are not written to the cache, and those below 0 see nothing.
+ *   q, k, v, out : (tokens x heads x d) and (tokens x kv_heads x d) bf16, element strides ld* between tokens and h* between heads, so that they may be parts of
+ *            one product's rows.  heads is a multiple of kv_heads: head h uses key head h / (heads / kv_heads).  heads at most 4096, tokens heads at most 2^30.
+ * starts, lengths and table are read on the device, when the kernels run: a captured graph serves every later step that fits its shapes.
+ * Calls with tokens = 0 or seqs = 0 do nothing.
+ *
+ * gptaq_cache_append: rotates the queries into `out` and the keys into the cache, and copies the values there.  Pair j of a head's `pairs` rotated ones is entries
+ *   (j, pairs + j), or (2 j, 2 j + 1) where interleaved != 0; with angle = position * freqs[j], freqs in fp64, radians:
+ *   (a, b) -> (a cos - b sin, b cos + a sin), taken in fp32 and rounded once.  Entries from 2 pairs on are copied.  d is a multiple of 16 up to 256, pairs one of 8
+ *   up to d / 2.  out may be q itself (same strides); other overlaps are not allowed.  Queries of positions below 0 are not written.
+ * gptaq_attention: out[i] = sum_j w_ij v_j / sum_j w_ij with w_ij = exp(scale q_i k_j) over the positions j that token i, at position p, sees: j <= p, and with
+ *   window > 0 only j > p - window or j < sinks.  d is 64, 96 or 128.  A token that sees nothing gives zeros.  What lies where no token sees it (other sequences'
+ *   remains, infinities, NaN) changes nothing.
+ *   ws     : >= gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d) bytes, 256-byte aligned; the size for more tokens serves fewer.
+ * Scores, the softmax's maximum and sum, and the outputs' sums are fp32; weights w are rounded to bf16 for the product with the values.  The order of a sum depends on
+ * the shapes and the lengths alone: no atomics, the same bits every time. */
+int gptaq_cache_append(const uint16_t* q, int64_t ldq, int64_t hq, const uint16_t* k, int64_t ldk, int64_t hk, const uint16_t* v,
+                       int64_t ldv, int64_t hv, uint16_t* keys, uint16_t* values, int64_t pages, int64_t page, const int32_t* table,
+                       int64_t ld_table, int64_t table_pages, const int32_t* starts, const int32_t* lengths, int64_t seqs,
+                       int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d, const double* freqs, int64_t pairs,
+                       int interleaved, uint16_t* out, int64_t ldo, int64_t ho, void* stream);
+size_t gptaq_attention_workspace_bytes(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t d);
+int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const uint16_t* keys, const uint16_t* values, int64_t pages,
+                    int64_t page, const int32_t* table, int64_t ld_table, int64_t table_pages, const int32_t* starts,
+                    const int32_t* lengths, int64_t seqs, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d,
+                    int64_t window, int64_t sinks, float scale, uint16_t* out, int64_t ldo, int64_t ho, void* ws, size_t ws_bytes,
+                    void* stream);
+
 /* ---------------------------------------------------------------------------------------
  * Measurement aid (not part of the method).  While enabled, the library brackets its kernels
  * with HIP events on the caller's stream, grouped by tag:

@@ -83,6 +83,21 @@ _SIGS = {
                                   _c.c_void_p]),
     "gptaq_silu_mul_i8": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float, _c.c_void_p,
                                      _c.c_int64, _c.c_void_p, _c.c_void_p]),
+    "gptaq_linear8_weights_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int64]),
+    "gptaq_linear8_pack": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p,
+                                      _c.c_size_t, _c.c_void_p, _c.c_void_p]),
+    "gptaq_linear8_workspace_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int64, _c.c_int64]),
+    "gptaq_linear8_i8": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_size_t, _c.c_int64, _c.c_int64,
+                                    _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "gptaq_quant_activations_i8": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float, _c.c_void_p, _c.c_int64, _c.c_void_p,
+                                              _c.c_void_p]),
+    "gptaq_cache_append": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64] * 3 + [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_int64,
+                                     _c.c_int64, _c.c_void_p, _c.c_void_p] + [_c.c_int64] * 5 + [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_int64,
+                                     _c.c_int64, _c.c_void_p]),
+    "gptaq_attention_workspace_bytes": (_c.c_size_t, [_c.c_int64] * 5),
+    "gptaq_attention": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64,
+                                   _c.c_void_p, _c.c_void_p] + [_c.c_int64] * 7 + [_c.c_float, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_size_t,
+                                   _c.c_void_p]),
     "gptaq_profile_enable": (_c.c_int, [_c.c_int]),
     "gptaq_profile_read": (_c.c_int, [_c.c_int, _c.POINTER(_c.c_int64), _c.POINTER(_c.c_double)]),
     "gptaq_measure_mfma_peak": (_c.c_int, [_c.c_int, _c.c_int, _c.c_void_p, _c.c_size_t, _c.POINTER(_c.c_double),
@@ -437,31 +452,36 @@ def gptaq_pack_codes(codes: torch.Tensor, bits: int) -> torch.Tensor:
 
 # ---- running quantised layers
 
-def _address(t: torch.Tensor, device: int, dtype, count: int, name: str) -> int:
+def _address(t: torch.Tensor, device: int, dtype, count: int, name: str, of: str = "LinearWeights") -> int:
     if t.get_device() != device:
-        raise GptaqError(f"LinearWeights.{name}: in memory of {t.device}, in a call that runs on GPU {device}")
+        raise GptaqError(f"{of}.{name}: in memory of {t.device}, in a call that runs on GPU {device}")
     if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
-        raise GptaqError(f"LinearWeights.{name}: no longer {count} contiguous {dtype}")
+        raise GptaqError(f"{of}.{name}: no longer {count} contiguous {dtype}")
     return t.data_ptr()
 
 
-class LinearWeights:
+class _Weights:
+    """Fixed once made; copied, pickled and saved through the constructor (the default sets attributes)."""
+    __slots__ = ()
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{type(self).__name__}.{name}: weights are fixed; lay out new ones with {self._packs}")
+
+    def __reduce__(self):
+        return type(self), tuple(getattr(self, name) for name in self.__slots__)
+
+
+class LinearWeights(_Weights):
     """A layer's weights as gptaq_linear and gptaq_linear_i8 read them: data (uint8), m, n, group (0: one per row), perm, bias, and info,
     an int32 on the GPU that is 0, or 1 + a row whose codes or zeros do not fit in 4 bits.  Fixed once made, as gptaq_linear_pack has checked
     that they fit each other; what a call reads of the tensors is their memory at that time, which has to be of the same kind and size still."""
     __slots__ = ("data", "m", "n", "group", "perm", "bias", "info")
+    _packs = "gptaq_linear_pack"
 
     def __init__(self, data: torch.Tensor, m: int, n: int, group: int, perm: Optional[torch.Tensor], bias: Optional[torch.Tensor],
                  info: torch.Tensor):
         for name, value in zip(self.__slots__, (data, m, n, group, perm, bias, info)):
             object.__setattr__(self, name, value)
-
-    def __setattr__(self, name, value):
-        raise AttributeError(f"LinearWeights.{name}: weights are fixed; lay out new ones with gptaq_linear_pack")
-
-    def __reduce__(self):
-        """Copied, pickled and saved through its constructor (the default sets attributes)."""
-        return LinearWeights, tuple(getattr(self, name) for name in self.__slots__)
 
     def _args(self, device: int):
         """As the C calls take them, in order; on the GPU `device`."""
@@ -505,7 +525,7 @@ def gptaq_linear_workspace_bytes(tokens: int, m: int, n: int) -> int:
     return load().gptaq_linear_workspace_bytes(tokens, m, n)
 
 
-def _linear_out(X: torch.Tensor, tokens: int, n: int, w: LinearWeights, dtype, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
+def _linear_out(X: torch.Tensor, tokens: int, n: int, w: _Weights, dtype, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
     if n != w.n:
         raise GptaqError(f"{name}: X has {n} columns, the weights {w.n}")
     if out is None:
@@ -541,6 +561,71 @@ def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWe
     Y = _linear_out(codes, tokens, n, weights, dtype, out, "gptaq_linear_i8")
     _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), tokens, _ld(codes, tokens, n), *weights._args(device), Y.data_ptr(),
                                   _ld(Y, tokens, weights.m), Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear_i8")
+    return Y
+
+
+class Linear8Weights(_Weights):
+    """A layer's weights as gptaq_linear8_i8 reads them: data (uint8), m, n, bias, and info, an int32 on the GPU that is 0, or 1 + a row whose zero does not
+    fit in 8 bits, or -1 - a column that the permutation does not name.  Fixed once made, as LinearWeights are."""
+    __slots__ = ("data", "m", "n", "bias", "info")
+    _packs = "gptaq_linear8_pack"
+
+    def __init__(self, data: torch.Tensor, m: int, n: int, bias: Optional[torch.Tensor], info: torch.Tensor):
+        for name, value in zip(self.__slots__, (data, m, n, bias, info)):
+            object.__setattr__(self, name, value)
+
+    def _args(self, device: int):
+        """As the C call takes them, in order; on the GPU `device`."""
+        data, bias = self.data, self.bias
+        size = data.numel()
+        return (_address(data, device, torch.uint8, size, "data", "Linear8Weights"), size, self.m, self.n,
+                None if bias is None else _address(bias, device, torch.float32, self.m, "bias", "Linear8Weights"))
+
+
+def gptaq_linear8_weights_bytes(m: int, n: int) -> int:
+    return load().gptaq_linear8_weights_bytes(m, n)
+
+
+def gptaq_linear8_pack(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, perm: Optional[torch.Tensor] = None,
+                       bias: Optional[torch.Tensor] = None) -> Linear8Weights:
+    """Lays out what gptaq_quantize_layer returned (bits <= 8, one scale and zero a row).  perm: the columns' order where the layer was solved with
+    act_order; bias: fp32."""
+    _need(codes, torch.uint8, "codes")
+    m, n = codes.shape
+    for t, name in ((scales, "scales"), (zeros, "zeros")):
+        if not t.is_cuda or t.dtype != torch.float32 or t.shape != (m, 1) or not t.is_contiguous():
+            raise GptaqError(f"gptaq_linear8_pack: {name}: expected a contiguous {m} x 1 float32 CUDA tensor")
+    if perm is not None:
+        _need_vec(perm, torch.int32, "perm")
+        if perm.numel() != n:
+            raise GptaqError("gptaq_linear8_pack: perm: expected one entry per column")
+    if bias is not None:
+        _need_vec(bias, torch.float32, "bias")
+        if bias.numel() != m:
+            raise GptaqError("gptaq_linear8_pack: bias: expected one entry per row")
+    device = _here(codes, scales, zeros, perm, bias)
+    data = workspace(gptaq_linear8_weights_bytes(m, n), codes.device)
+    info = torch.empty(1, dtype=torch.int32, device=codes.device)
+    _check(load().gptaq_linear8_pack(_ptr(codes), _ld(codes, m, n), _ptr(scales), _ptr(zeros), m, n, _ptr(perm), _ptr(data), data.numel(), _ptr(info),
+                                     _stream(device)), "gptaq_linear8_pack")
+    return Linear8Weights(data, m, n, bias, info)
+
+
+def gptaq_linear8_workspace_bytes(tokens: int, m: int, n: int) -> int:
+    return load().gptaq_linear8_workspace_bytes(tokens, m, n)
+
+
+def gptaq_linear8_i8(codes: torch.Tensor, scales: torch.Tensor, weights: Linear8Weights, ws: torch.Tensor,
+                     out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
+    """X W^T + bias for 8-bit activations X = scales[t] * codes[t][:] and weights of up to 8 bits; returns (tokens x m), bf16 or fp32."""
+    _need(codes, torch.int8, "codes"); _need_vec(scales, torch.float32, "scales")
+    tokens, n = codes.shape
+    if scales.numel() != tokens:
+        raise GptaqError("gptaq_linear8_i8: scales: expected one per token")
+    device = _here(codes, scales, out)
+    Y = _linear_out(codes, tokens, n, weights, dtype, out, "gptaq_linear8_i8")
+    _check(load().gptaq_linear8_i8(codes.data_ptr(), scales.data_ptr(), tokens, _ld(codes, tokens, n), *weights._args(device), Y.data_ptr(),
+                                   _ld(Y, tokens, weights.m), Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear8_i8")
     return Y
 
 
@@ -624,3 +709,92 @@ def gptaq_silu_mul_i8(gate: torch.Tensor, up: torch.Tensor, clip: float = 1.0):
     _check(load().gptaq_silu_mul_i8(_ptr(gate), _ptr(up), tokens, n, _ld(gate, tokens, n), _ld(up, tokens, n), float(clip), _ptr(codes), n, _ptr(scales),
                                     _stream(device)), "gptaq_silu_mul_i8")
     return codes, scales
+
+
+def gptaq_quant_activations_i8(X: torch.Tensor, clip: float = 1.0):
+    """(codes, scales): bf16 rows as 8-bit codes and a scale per token, scale = clip * max|X| / 127."""
+    _need(X, torch.bfloat16, "X")
+    device = _here(X)
+    tokens, n = X.shape
+    codes, scales = X.new_empty((tokens, n), dtype=torch.int8), X.new_empty(tokens, dtype=torch.float32)
+    _check(load().gptaq_quant_activations_i8(X.data_ptr(), tokens, n, _ld(X, tokens, n), float(clip), codes.data_ptr(), n, scales.data_ptr(),
+                                             _stream(device)), "gptaq_quant_activations_i8")
+    return codes, scales
+
+
+# ---- the cache and attention
+
+def _need_heads(t: torch.Tensor, name: str):
+    """(address, stride of tokens, stride of heads) of a (tokens x heads x d) bf16 tensor."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
+        raise GptaqError(f"{name}: expected a (tokens, heads, d) bfloat16 CUDA tensor with adjacent entries")
+    tokens, heads, d = t.shape
+    return t.data_ptr(), t.stride(0) if tokens > 1 else heads * t.stride(1) if heads > 1 else d, t.stride(1) if heads > 1 else d
+
+
+def _cache_args(keys: torch.Tensor, values: torch.Tensor, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, d: int, name: str):
+    """The cache's arguments as the C calls take them: (keys, values, pages, page, table, ld_table, table_pages, starts, lengths, seqs), and kv_heads."""
+    if keys.dtype is not torch.bfloat16 or keys.dim() != 5 or not keys.is_contiguous() or keys.shape[2] * 8 != d or keys.shape[4] != 8:
+        raise GptaqError(f"{name}: keys: expected contiguous bfloat16 (pages, kv_heads, {d} / 8, page, 8)")
+    pages, kv_heads, _, page, _ = keys.shape
+    if values.dtype is not torch.bfloat16 or values.shape != (pages, kv_heads, page // 8, d, 8) or not values.is_contiguous():
+        raise GptaqError(f"{name}: values: expected contiguous bfloat16 ({pages}, {kv_heads}, {page} / 8, {d}, 8)")
+    if lengths.dtype is not torch.int32 or lengths.dim() != 1 or not lengths.is_contiguous():
+        raise GptaqError(f"{name}: lengths: expected a contiguous int32 vector")
+    seqs = lengths.shape[0]
+    if starts.dtype is not torch.int32 or starts.shape != (seqs + 1,) or not starts.is_contiguous():
+        raise GptaqError(f"{name}: starts: expected {seqs + 1} contiguous int32")
+    if table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != seqs or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise GptaqError(f"{name}: table: expected a row-major int32 tensor with a row for each of {seqs} sequences")
+    width = table.shape[1]
+    return (keys.data_ptr(), values.data_ptr(), pages, page, table.data_ptr(), table.stride(0) if seqs > 1 else width, width, starts.data_ptr(),
+            lengths.data_ptr(), seqs), kv_heads
+
+
+def _heads_out(q: torch.Tensor, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
+    if out is None:
+        return torch.empty_like(q, memory_format=torch.contiguous_format)
+    if out.shape != q.shape:
+        raise GptaqError(f"{name}: out: shape mismatch")
+    return out
+
+
+def gptaq_cache_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, table: torch.Tensor,
+                       starts: torch.Tensor, lengths: torch.Tensor, freqs: Optional[torch.Tensor], interleaved: bool = False,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Writes the keys k, rotated by their positions, and the values v of new tokens into the cache; returns the rotated queries (in `out`, which may be q
+    itself).  q, k, v: (tokens, heads, d), for instance parts of one product's rows; sequence s has rows starts[s] .. starts[s + 1] - 1, its
+    lengths[s] count them.  freqs: float64, the angle per position of each rotated pair (None: no rotation)."""
+    device = _here(q, k, v, keys, values, table, starts, lengths, freqs, out)
+    qp, kp, vp = _need_heads(q, "q"), _need_heads(k, "k"), _need_heads(v, "v")
+    tokens, heads, d = q.shape
+    cache, kv_heads = _cache_args(keys, values, table, starts, lengths, d, "gptaq_cache_append")
+    if k.shape != (tokens, kv_heads, d) or v.shape != (tokens, kv_heads, d):
+        raise GptaqError(f"gptaq_cache_append: k, v: expected ({tokens}, {kv_heads}, {d})")
+    pairs = 0
+    if freqs is not None:
+        if freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+            raise GptaqError("gptaq_cache_append: freqs: expected a contiguous float64 vector")
+        pairs = freqs.shape[0]
+    out = _heads_out(q, out, "gptaq_cache_append")
+    _check(load().gptaq_cache_append(*qp, *kp, *vp, *cache, tokens, heads, kv_heads, d, _ptr(freqs), pairs, bool(interleaved), *_need_heads(out, "out"),
+                                     _stream(device)), "gptaq_cache_append")
+    return out
+
+
+def gptaq_attention_workspace_bytes(tokens: int, seqs: int, heads: int, kv_heads: int, d: int) -> int:
+    return load().gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d)
+
+
+def gptaq_attention(q: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor,
+                    ws: torch.Tensor, window: int = 0, sinks: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention of new tokens' queries (tokens, heads, d) over the cache, which holds their own keys and values already.  window: positions a
+    token sees, itself among them (0: all); sinks: first positions that stay visible.  scale: 1 / sqrt(d) if not given."""
+    device = _here(q, keys, values, table, starts, lengths, out)
+    qp = _need_heads(q, "q")
+    tokens, heads, d = q.shape
+    cache, kv_heads = _cache_args(keys, values, table, starts, lengths, d, "gptaq_attention")
+    out = _heads_out(q, out, "gptaq_attention")
+    _check(load().gptaq_attention(*qp, *cache, tokens, heads, kv_heads, d, int(window), int(sinks), d ** -0.5 if scale is None else float(scale),
+                                  *_need_heads(out, "out"), _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_attention")
+    return out

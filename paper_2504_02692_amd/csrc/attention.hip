@@ -1,0 +1,299 @@
+// Attention of new tokens over a paged cache: y_i = sum_j softmax_j(scale q_i k_j) v_j over the keys that token i sees, with an optional window and first
+// tokens that stay visible.  In one pass over the keys, with the running maximum and sum of the softmax in fp32.
+#include "attention.h"
+
+namespace gptaq {
+
+// ---- few rows: a block is 16 rows (a step of decoding: the heads that share a key head).  Bound by memory: keys and values go from the cache straight to the
+// registers of the lanes that feed v_mfma 16x16x32, and nothing is read twice.  Both products are taken transposed: S^T = K Q^T leaves a lane the scores of one
+// row (l % 16), and O^T = V^T P^T takes them from there, with the keys in such an order that a lane's scores of 32 keys are what the second product wants of it: row
+// 4 a + i of the first product's tile T has key 8 a + 4 T + i.  The four wavefronts of a block take 32 keys each in turn and join through LDS.
+// Weights are rounded to bf16 for the second product (2^-9 each, as the output is once more); their sum is taken of the fp32 values.
+template <int D>
+__global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
+  constexpr int KS = D / 32, VT = D / 16, PAD = D + 4;
+  __shared__ __attribute__((aligned(16))) float joined[4][16][PAD];
+  __shared__ float maxima[4][16], sums[4][16];
+  const CacheShape& c = a.c;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, quad = lane >> 4;
+  const int head = (int)(blockIdx.x % (unsigned)c.kv_heads), rest = (int)(blockIdx.x / (unsigned)c.kv_heads);
+  const int part = rest % a.parts;
+  const int64_t block = a.first_block + rest / a.parts;
+  const int s = cache_find(c, block, c.group, 4, 1);
+  const Sequence seq = cache_sequence(c, s);
+  const int64_t in_seq = block - cache_block_of(c, s, c.group, 4, 1);
+  const int rows = seq.count * c.group;
+  if (in_seq < 0 || in_seq * 16 >= rows) return;
+  const int row0 = (int)in_seq * 16, last = min(row0 + 15, rows - 1);
+  const int pmin = seq.before + row0 / c.group, pmax = seq.before + last / c.group;
+  const Tiles tiles = attention_tiles(a, pmin, pmax);
+  const Parts parts = attention_parts(a, tiles.count);
+  if (part > 0 && part >= parts.count) return;                       // (part 0 writes the zeros of rows that see nothing)
+  const int begin = part * parts.each, end = min(begin + parts.each, tiles.count);
+
+  const int row = min(row0 + l16, last), token = row / c.group, p_row = seq.before + token;
+  const uint16_t* const qrow = a.q + (int64_t)(seq.first + token) * a.ldq + (int64_t)(head * c.group + row % c.group) * a.hq;
+  typedef u32x4 __attribute__((aligned(2))) u32x4_at2;
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int i = 0; i < KS; ++i) qf[i] = __builtin_bit_cast(bf16x8, (u32x4) * reinterpret_cast<const u32x4_at2*>(qrow + i * 32 + quad * 8));
+
+  const int page = 1 << c.page_bits;
+  const int64_t head_elements = (int64_t)D << c.page_bits;           // of a page, of one head
+  const int kslot = 8 * (l16 >> 2) + (l16 & 3);                      // key of 32 that lane has in tile 0 (4 more in tile 1)
+  struct Stage { u32x4 k[2][KS], v[VT]; int j0; int ok; };          // ok: bit 0, 1: keys 0 .. 15, 16 .. 31 have a page
+  auto load = [&](Stage& g, int step) {
+    g.j0 = tiles.at(begin + (step >> 1)) * kTile + (step & 1) * 32;
+    const int id0 = cache_page(c, s, g.j0), id1 = cache_page(c, s, g.j0 + 16);
+    g.ok = (id0 >= 0 ? 1 : 0) | (id1 >= 0 ? 2 : 0);
+    const int64_t at0 = ((int64_t)max(id0, 0) * c.kv_heads + head) * head_elements, at1 = ((int64_t)max(id1, 0) * c.kv_heads + head) * head_elements;
+    const int off = g.j0 & (page - 1);
+    const uint16_t* kfrom = a.keys + (l16 < 8 ? at0 : at1) + (((off + kslot) & (page - 1)) + quad * page) * 8;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < KS; ++i) g.k[t][i] = *reinterpret_cast<const u32x4*>(kfrom + t * 32 + i * 32 * page);
+    const uint16_t* vfrom = a.values + (quad < 2 ? at0 : at1) + (int64_t)(((off + quad * 8) & (page - 1)) >> 3) * (D * 8) + l16 * 8;
+#pragma unroll
+    for (int i = 0; i < VT; ++i) g.v[i] = *reinterpret_cast<const u32x4*>(vfrom + i * 128);
+  };
+
+  f32x4 acc[VT];
+#pragma unroll
+  for (int i = 0; i < VT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float top = -__builtin_inff(), total = 0.f;                        // total: this lane's keys alone
+  auto work = [&](Stage& g) {
+    f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < KS; ++i) sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, g.k[t][i]), qf[i], sc[t], 0, 0, 0);
+    const bool whole = g.ok == 3 && g.j0 + 31 <= pmin && (a.window == 0 || g.j0 > pmax - a.window || g.j0 + 31 < a.sinks);
+    float v[8];
+    uint32_t seen = 255;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = sc[e >> 2][e & 3] * a.scale;
+    if (!whole) {
+      seen = 0;
+      const int j = g.j0 + quad * 8;
+      const bool have = quad < 2 ? (g.ok & 1) : (g.ok & 2);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool here = have && attention_sees(a, p_row, j + e);
+        seen |= (here ? 1u : 0u) << e;
+        v[e] = here ? v[e] : -__builtin_inff();
+      }
+    }
+    float most = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+    if (__ballot(most > top + kSlack)) {
+      most = fmaxf(most, __shfl_xor(most, 16));
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const float now = fmaxf(top, most), factor = at_factor(top, now);
+      top = now;
+      total *= factor;
+#pragma unroll
+      for (int i = 0; i < VT; ++i) acc[i] *= factor;
+    }
+    const float from = at_origin(top);
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { w[e] = at_exp2(v[e] - from); total += w[e]; }
+    const u32x4 wp = {at_bf16x2(w[0], w[1]), at_bf16x2(w[2], w[3]), at_bf16x2(w[4], w[5]), at_bf16x2(w[6], w[7])};
+    if (!whole) {
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < VT; ++i) any |= attention_strange(g.v[i]);
+      if (__ballot(any)) {
+        u32x4 ones;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ones[i] = (seen >> (2 * i) & 1 ? 0x3f80u : 0u) | (seen >> (2 * i + 1) & 1 ? 0x3f800000u : 0u);
+#pragma unroll
+        for (int i = 0; i < VT; ++i) {
+          u32x4 marks;
+          attention_marks(g.v[i], marks);
+          const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][e] += attention_strange_sum(n[e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VT; ++i)
+      acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, g.v[i]), __builtin_bit_cast(bf16x8, wp), acc[i], 0, 0, 0);
+  };
+  const int steps = 2 * max(0, end - begin);
+  Stage x, y;
+  int step = wave;
+  if (step < steps) load(x, step);
+  for (; step < steps; step += 8) {
+    if (step + 4 < steps) load(y, step + 4);
+    work(x);
+    if (step + 8 < steps) load(x, step + 8);
+    if (step + 4 < steps) work(y);
+  }
+
+  // ---- the wavefronts' sums: a lane has row l % 16, entries 16 i + 4 quad + e
+  total += __shfl_xor(total, 16);
+  total += __shfl_xor(total, 32);
+  if (quad == 0) { maxima[wave][l16] = top; sums[wave][l16] = total; }
+#pragma unroll
+  for (int i = 0; i < VT; ++i) *reinterpret_cast<f32x4*>(&joined[wave][l16][i * 16 + quad * 4]) = acc[i];
+  __syncthreads();
+  const int r = threadIdx.x >> 4, e0 = threadIdx.x & 15;
+  if (row0 + r > last) return;
+  float m = maxima[0][r];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) m = fmaxf(m, maxima[w][r]);
+  float sum = 0.f, factor[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    factor[w] = at_factor(maxima[w][r], m);
+    sum += factor[w] * sums[w][r];
+  }
+  const int rr = row0 + r, tok = rr / c.group;
+  const int64_t call_row = (int64_t)(seq.first + tok) * c.heads + head * c.group + rr % c.group;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t* const to = a.out + (int64_t)(seq.first + tok) * a.ldo + (int64_t)(head * c.group + rr % c.group) * a.ho;
+  float* const to_part = a.partial + ((int64_t)part * c.tokens * c.heads + call_row) * D;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const int e = i * 32 + e0 * 2;
+    float o[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      o[h] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) o[h] += factor[w] * joined[w][r][e + h];
+    }
+    if (parts.count > 1) {
+      to_part[e] = o[0];
+      to_part[e + 1] = o[1];
+    } else {
+      typedef uint32_t __attribute__((aligned(2))) u32_at2;
+      *reinterpret_cast<u32_at2*>(to + e) = at_bf16x2(o[0] * inv, o[1] * inv);
+    }
+  }
+  if (parts.count > 1 && e0 == 0) {
+    float* st = a.stats + ((int64_t)part * c.tokens * c.heads + call_row) * 2;
+    st[0] = m;
+    st[1] = sum;
+  }
+}
+
+// The parts of a row, a wavefront a row.
+template <int D>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, int64_t first_row) {
+  const CacheShape& c = a.c;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = first_row + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (int64_t)c.tokens * c.heads;
+  if (row >= rows) return;
+  const int token = (int)(row / c.heads), h = (int)(row % c.heads);
+  const int s = cache_find(c, token, 1, 0, 0);
+  const Sequence seq = cache_sequence(c, s);
+  const int in_seq = token - seq.first;
+  if (in_seq < 0 || in_seq >= seq.count) return;                     // (no sequence's)
+  // as the block of this row dealt its tiles out
+  const int rows_seq = seq.count * c.group, row0 = (in_seq * c.group + h % c.group) >> a.rows_bits << a.rows_bits;
+  const int last = min(row0 + (1 << a.rows_bits) - 1, rows_seq - 1);
+  const Parts parts = attention_parts(a, attention_tiles(a, seq.before + row0 / c.group, seq.before + last / c.group).count);
+  if (parts.count <= 1) return;
+  float m = -__builtin_inff();
+  for (int i = 0; i < parts.count; ++i) m = fmaxf(m, a.stats[(i * rows + row) * 2]);
+  float sum = 0.f, o[D / 64 + 1];
+  constexpr int N = (D + 63) / 64;
+#pragma unroll
+  for (int k = 0; k < N; ++k) o[k] = 0.f;
+  for (int i = 0; i < parts.count; ++i) {
+    const float* st = a.stats + (i * rows + row) * 2;
+    const float factor = at_factor(st[0], m);
+    sum += factor * st[1];
+    const float* from = a.partial + (i * rows + row) * D;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (D % 64 == 0 || k * 64 + lane < D) o[k] += factor * from[k * 64 + lane];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t* const to = a.out + (int64_t)token * a.ldo + (int64_t)h * a.ho;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (D % 64 == 0 || k * 64 + lane < D) to[k * 64 + lane] = __builtin_bit_cast(uint16_t, (__bf16)(o[k] * inv));
+}
+
+// ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
+constexpr int64_t kMostParts = 64, kFewBits = 4, kPartialRows = 32768;
+static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
+// Parts of the keys: blocks for eight workgroups a CU, if the keys last.
+static int64_t attention_part_count(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads) {
+  const int64_t group = heads / kv_heads, blocks = ((tokens * group + 15) / 16 > seqs ? (tokens * group + 15) / 16 : seqs) * kv_heads;
+  const int64_t parts = 2048 / blocks;
+  return parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts;
+}
+// Room for the parts' sums: parts times blocks is 2048 at most, so parts times rows 32768.  (More tokens never take less, so a workspace serves all smaller calls.)
+static int64_t partial_rows(int64_t tokens, int64_t heads) { return kMostParts * tokens * heads < kPartialRows ? kMostParts * tokens * heads : kPartialRows; }
+
+template <int D>
+static hipError_t launch_attention(const AttentionArgs& all, hipStream_t s) {
+  AttentionArgs a = all;
+  a.rows_bits = kFewBits;
+  const int64_t blocks = attention_blocks(a.c.tokens, a.c.seqs, a.c.group, kFewBits), each = (int64_t)a.parts * a.c.kv_heads;
+  const int64_t most = ((int64_t)1 << 23) / each;                    // (a grid has less than 2^32 threads)
+  for (int64_t first = 0; first < blocks; first += most) {
+    a.first_block = first;
+    const int64_t n = blocks - first < most ? blocks - first : most;
+    hipLaunchKernelGGL(attention_few_kernel<D>, dim3((unsigned)(n * each)), dim3(256), 0, s, a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  if (a.parts == 1) return hipSuccess;
+  const int64_t rows = (int64_t)a.c.tokens * a.c.heads;
+  for (int64_t first = 0; first < rows; first += (int64_t)1 << 25) {
+    const int64_t n = rows - first < ((int64_t)1 << 25) ? rows - first : (int64_t)1 << 25;
+    hipLaunchKernelGGL(attention_join_kernel<D>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, a, first);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+static bool attention_size(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t d) {
+  return tokens >= 0 && tokens <= (1 << 24) && seqs >= 0 && seqs <= (1 << 20) && heads > 0 && heads <= 4096 && tokens * heads <= (1 << 30) && kv_heads > 0 && heads % kv_heads == 0 &&
+         (d == 64 || d == 96 || d == 128);
+}
+
+}  // namespace gptaq
+
+using namespace gptaq;
+
+extern "C" size_t gptaq_attention_workspace_bytes(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t d) {
+  if (!attention_size(tokens, seqs, heads, kv_heads, d) || tokens == 0 || seqs == 0) return 0;
+  return ((size_t)partial_rows(tokens, heads) * (d + 2) * 4 + 255) / 256 * 256;
+}
+
+extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const uint16_t* keys, const uint16_t* values, int64_t pages, int64_t page,
+                               const int32_t* table, int64_t ld_table, int64_t table_pages, const int32_t* starts, const int32_t* lengths, int64_t seqs,
+                               int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d, int64_t window, int64_t sinks, float scale, uint16_t* out, int64_t ldo,
+                               int64_t ho, void* ws, size_t ws_bytes, void* stream) {
+  if (tokens != 0 && seqs != 0 && (!q || !out || !starts || !lengths || !ws || (table_pages != 0 && !table) || (pages != 0 && (!keys || !values)))) return GPTAQ_ENULL;
+  AttentionArgs a{};
+  if (const int rc = cache_shape(a.c, table, ld_table, table_pages, starts, lengths, seqs, tokens, heads, kv_heads, d, page, pages)) return rc;
+  if (d != 64 && d != 96 && d != 128) return GPTAQ_EUNSUPPORTED;
+  if ((((uintptr_t)q | (uintptr_t)out) & 1) || (((uintptr_t)keys | (uintptr_t)values) & 15) || ldq < 0 || hq < 0 || window < 0 || sinks < 0 ||
+      !cache_rows_apart(tokens, ldo, heads, ho, d))
+    return GPTAQ_EDIM;
+  if (!(scale > -__builtin_inff() && scale < __builtin_inff())) return GPTAQ_EUNSUPPORTED;
+  if (tokens == 0 || seqs == 0) return GPTAQ_OK;
+  if (((uintptr_t)ws & 255) || ws_bytes < gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d)) return GPTAQ_EWORKSPACE;
+  constexpr int64_t kFar = (int64_t)1 << 30;                          // (positions are below this)
+  a.q = q; a.keys = keys; a.values = values; a.ldq = ldq; a.hq = hq;
+  a.out = out; a.ldo = ldo; a.ho = ho;
+  a.scale = scale * 1.4426950408889634f;
+  a.window = (int32_t)(window < kFar ? window : 0);
+  a.sinks = (int32_t)(sinks < kFar ? sinks : kFar);
+  a.parts = (int32_t)attention_part_count(tokens, seqs, heads, kv_heads);
+  a.min_tiles = 2;
+  a.partial = (float*)ws;
+  a.stats = a.partial + (int64_t)a.parts * tokens * heads * d;
+  if (pages == 0) a.c.table_pages = 0;                                // no key anywhere: zeros
+  const hipError_t e = d == 64 ? launch_attention<64>(a, (hipStream_t)stream) : d == 96 ? launch_attention<96>(a, (hipStream_t)stream)
+                                                                            : launch_attention<128>(a, (hipStream_t)stream);
+  if (e != hipSuccess) { set_last_hip_error(e); return GPTAQ_ELAUNCH; }
+  return GPTAQ_OK;
+}

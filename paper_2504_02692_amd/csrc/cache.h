@@ -1,0 +1,77 @@
+// A paged cache of keys and values as gptaq_cache_append writes it and gptaq_attention reads it.
+#pragma once
+#include "common.h"
+
+namespace gptaq {
+
+// keys (pages, kv_heads, d / 8, page, 8), values (pages, kv_heads, page / 8, d, 8), both bf16: eight contraction elements (of a key's entries; of
+// positions) are 16 bytes, so a lane's operand of a matrix instruction is one 16-byte load, lanes side by side read bytes side by side, and neither product
+// needs a transposition.
+struct CacheShape {
+  const int32_t* table; int64_t ld_table; int32_t table_pages;      // pages of a sequence, in order; entries outside 0 .. pages - 1: no page there
+  const int32_t *starts, *lengths;                                  // seqs + 1 first rows; tokens of each sequence, the new ones among them
+  int32_t seqs, tokens, heads, kv_heads, group, d, page_bits;       // group: heads / kv_heads; a page has 1 << page_bits positions
+  int64_t pages;
+};
+// A sequence's new tokens: rows first .. first + count - 1, positions before .. before + count - 1 (before may be negative where `lengths` says less than
+// `starts`; positions below 0 are no tokens).  Whatever the arrays hold, rows stay inside the tensors and positions inside 31 bits.
+struct Sequence { int32_t index, first, count, before; };
+__device__ __forceinline__ int cache_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+__device__ __forceinline__ Sequence cache_sequence(const CacheShape& c, int s) {
+  Sequence q;
+  q.index = s;
+  q.first = cache_clamp(c.starts[s], 0, c.tokens);
+  q.count = cache_clamp(c.starts[s + 1], q.first, c.tokens) - q.first;
+  q.before = cache_clamp(c.lengths[s], 0, 1 << 30) - q.count;
+  return q;
+}
+// Work is dealt out without the host knowing the lengths: with `units` pieces a token and `per` of them to a block, sequence s has the blocks from
+// starts[s] * units / per + s * extra on, which leaves each sequence room for ceil(count * units / per) + extra - 1 at least.  This finds the sequence of a block:
+// 64 of them are tried at a time, one a lane, so up to 64 sequences are one load.
+__device__ __forceinline__ int64_t cache_block_of(const CacheShape& c, int s, int units, int per_bits, int extra) {
+  return (((int64_t)cache_clamp(c.starts[s], 0, c.tokens) * units) >> per_bits) + (int64_t)s * extra;
+}
+__device__ __forceinline__ int cache_find(const CacheShape& c, int64_t block, int units, int per_bits, int extra) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = c.seqs;
+  while (n > 1) {
+    const int step = (n + 63) >> 6, at = lane * step;
+    const bool here = at < n && cache_block_of(c, lo + (at < n ? at : 0), units, per_bits, extra) <= block;
+    const uint64_t mask = __ballot(here);
+    const int k = mask ? 63 - __builtin_clzll(mask) : 0;
+    lo += k * step;
+    n = n - k * step < step ? n - k * step : step;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+// The page of a position, or -1.
+__device__ __forceinline__ int cache_page(const CacheShape& c, int s, int position) {
+  const int at = position >> c.page_bits;
+  if (at >= c.table_pages) return -1;
+  const int id = c.table[s * c.ld_table + at];
+  return (uint32_t)id < (uint64_t)c.pages ? id : -1;
+}
+
+// What both calls refuse; fills `c`.
+inline int cache_shape(CacheShape& c, const int32_t* table, int64_t ld_table, int64_t table_pages, const int32_t* starts, const int32_t* lengths, int64_t seqs,
+                       int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d, int64_t page, int64_t pages) {
+  if (seqs < 0 || seqs > (1 << 20) || tokens < 0 || tokens > (1 << 24) || heads <= 0 || kv_heads <= 0 || heads > 4096 || heads % kv_heads || tokens * heads > (1 << 30) || pages < 0 ||
+      pages > (1 << 30) || table_pages < 0 || ld_table < table_pages || (((uintptr_t)table | (uintptr_t)starts | (uintptr_t)lengths) & 3))
+    return GPTAQ_EDIM;
+  if (page < 16 || page > 256 || (page & (page - 1))) return GPTAQ_EUNSUPPORTED;
+  if (table_pages > (((int64_t)1 << 30) / page)) return GPTAQ_EDIM;
+  c.table = table; c.ld_table = ld_table; c.table_pages = (int32_t)table_pages;
+  c.starts = starts; c.lengths = lengths;
+  c.seqs = (int32_t)seqs; c.tokens = (int32_t)tokens; c.heads = (int32_t)heads; c.kv_heads = (int32_t)kv_heads; c.group = (int32_t)(heads / kv_heads);
+  c.d = (int32_t)d; c.page_bits = __builtin_ctzll(page); c.pages = pages;
+  return GPTAQ_OK;
+}
+
+// Whether the heads of an output's rows lie apart, in either order.
+inline bool cache_rows_apart(int64_t tokens, int64_t ld, int64_t heads, int64_t h, int64_t d) {
+  constexpr int64_t kMost = (int64_t)1 << 40;                        // (no stride of a real tensor)
+  return ld >= 0 && h >= 0 && ld <= kMost && h <= kMost && (heads == 1 || h >= d) && (tokens <= 1 || ld >= d) &&
+         (tokens <= 1 || heads == 1 || ld >= (heads - 1) * h + d || h >= (tokens - 1) * ld + d);
+}
+
+}  // namespace gptaq

@@ -1,0 +1,266 @@
+// y = x W^T + bias for layers whose weights the solve has quantised to 5 .. 8 bits with one scale and zero a row, and 8-bit activations:
+// y[t][r] = xs[t] scale[r] sum_j (code[r][j] - zero[r]) x[t][j] + bias[r].  The sum is exact (linear8.h); it is converted to fp32 once, multiplied by the product of
+// the two scales, and the bias is added with the same rounding.
+#include "linear8.h"
+
+namespace gptaq {
+
+// ---- laying out the weights
+
+// inverse[perm[j]] = j, and -1 where no j goes: what is missing or met twice shows as a column without a source.
+__global__ __launch_bounds__(256) void linear8_clear_kernel(int32_t* inverse, int n, const int32_t* perm, int32_t* info, uint8_t* tail, int count) {
+  const int at = blockIdx.x * 256 + threadIdx.x;
+  if (at < n) inverse[at] = perm ? -1 : at;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *info = 0;
+  if (blockIdx.x == 0 && (int)threadIdx.x < count) tail[threadIdx.x] = 0;
+}
+__global__ __launch_bounds__(256) void linear8_invert_kernel(int32_t* inverse, int n, const int32_t* perm) {
+  const int at = blockIdx.x * 256 + threadIdx.x;
+  if (at < n && (uint32_t)perm[at] < (uint32_t)n) atomicMax(inverse + perm[at], at);
+}
+// 16 columns of a row per thread.
+__global__ __launch_bounds__(256) void linear8_pack_kernel(const uint8_t* codes, int64_t ldc, const float* scales, const float* zeros, int m, int n, int64_t pieces,
+                                                           int kt, const int32_t* inverse, uint8_t* out, float* out_scales, int32_t* out_shifts, int32_t* info) {
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= pieces) return;
+  const int64_t tile = at / 64;
+  const int lane = (int)(at % 64), row = (int)(tile / (2 * kt)) * 16 + (lane & 15), col = (int)(tile % (2 * kt)) * 64 + (lane >> 4) * 16;
+  u32x4 w = {0u, 0u, 0u, 0u};
+  if (row < m) {
+    const uint8_t* c = codes + row * ldc;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (col + j >= n) continue;
+      const int from = inverse[col + j];
+      if (from < 0) { atomicMin(info, -1 - (col + j)); continue; }
+      w[j >> 2] |= (uint32_t)(c[from] ^ 0x80u) << (8 * (j & 3));
+    }
+  }
+  *reinterpret_cast<u32x4*>(out + at * 16) = w;
+  if (col == 0) {
+    float s = 0.f, z = 128.f;
+    if (row < m) { s = scales[row]; z = zeros[row]; }
+    if (!(z >= 0.f && z <= 255.f && z == rintf(z))) { atomicMax(info, row + 1); z = 128.f; }
+    out_scales[row] = s;
+    out_shifts[row] = 128 - (int)z;
+  }
+}
+
+// ---- activations whose rows do not start at 16 bytes or end inside 128 columns: to rows of `ldo` columns, zeros behind the n-th.  Bound by memory.
+typedef u32x4 __attribute__((aligned(1))) u32x4_at1;
+__global__ __launch_bounds__(256) void linear8_align_kernel(const int8_t* x, int64_t ldx, int n, int8_t* out, int ldo, int64_t pieces) {
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < pieces; at += (int64_t)gridDim.x * 256) {
+    const int64_t t = at / (ldo / 16);
+    const int c = (int)(at % (ldo / 16)) * 16;
+    const int8_t* from = x + t * ldx + c;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (c + 16 <= n) {
+      v = *reinterpret_cast<const u32x4_at1*>(from);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (c + j < n) v[j >> 2] |= (uint32_t)(uint8_t)from[j] << (8 * (j & 3));
+    }
+    *reinterpret_cast<u32x4*>(out + t * ldo + c) = v;
+  }
+}
+
+__device__ __forceinline__ i32x4 linear8_mfma(u32x4 a, u32x4 b, i32x4 c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+
+// ---- few tokens: TT tiles of v_mfma 16x16x64, 16 tokens each.  A workgroup takes RT tiles of 16 rows, its wavefronts share the runs of 128 columns out
+// among themselves.  Weights go straight from memory to the lanes that feed the matrix unit, two runs ahead; activations through LDS in runs of a token's 128
+// columns, to a place of the wavefront's own.  The activations' sum comes from one more matrix instruction, with ones.
+// The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W, the result has the row in l % 16 and tokens 4 (l / 16) .. + 3.
+constexpr int kFew8Waves = 16;
+template <int RT, int TT>
+__global__ __launch_bounds__(64 * kFew8Waves) void linear8_few_kernel(Linear8Args p) {
+  extern __shared__ __attribute__((aligned(256))) int32_t lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int l16 = lane & 15, q = lane >> 4;
+  const int rt0 = blockIdx.x * RT, tok0 = blockIdx.y * TT * 16, tokens = min(p.tokens - tok0, TT * 16);
+
+  const uint8_t* codes[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int64_t tr = rt0 + r < p.mt ? rt0 + r : p.mt - 1;      // (past the last tile of rows: that one again; nothing of it is stored)
+    codes[r] = p.codes + tr * p.kt * 2048 + lane * 16;
+  }
+  // The 16-byte chunks of a token's 128 columns are permuted so that 16 tokens' same chunk lies in 16 different places of 256 bytes.  Places of
+  // tokens that there are not hold anything: their results are not stored.
+  constexpr int XSTAGE = TT * 2048, NL = TT * 2;
+  auto swizzle = [](int row) { return (row >> 1) & 7; };
+  unsigned char* const xlds = reinterpret_cast<unsigned char*>(lds) + wave * 2 * XSTAGE;
+  const LdsLoader xfrom((const unsigned char*)p.x + (int64_t)tok0 * p.ldx);
+  int xsrc[NL];
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    const int row = j * 8 + lane / 8;
+    xsrc[j] = min(row, tokens - 1) * (int)p.ldx + ((lane % 8 ^ swizzle(row)) << 4);
+  }
+  struct Stage { u32x4 w[RT][2]; };
+  auto load = [&](Stage& s, int k, int place) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);          // lgkmcnt == 0: the place's last reads are over
+#pragma unroll
+    for (int j = 0; j < NL; ++j)
+      if (j == 0 || j * 8 < tokens) xfrom.load(xlds + place * XSTAGE + j * 1024, xsrc[j], __builtin_amdgcn_readfirstlane(k * 128));
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s.w[r][i] = *reinterpret_cast<const u32x4*>(codes[r] + (int64_t)k * 2048 + i * 1024);
+  };
+  i32x4 acc[TT][RT], accx[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    accx[t] = i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[t][r] = i32x4{0, 0, 0, 0};
+  }
+  const u32x4 ones = {0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u};
+  auto multiply = [&](const Stage& s, int place) {
+    asm volatile("" :: "v"(s.w[RT - 1][1]) : "memory");     // (where the weights are there, so are the activations, which were asked for before)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(xlds + place * XSTAGE + (t * 16 + l16) * 128 + (((4 * i + q) ^ swizzle(l16)) << 4));
+        accx[t] = linear8_mfma(x, ones, accx[t]);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[t][r] = linear8_mfma(x, s.w[r][i], acc[t][r]);
+      }
+  };
+  Stage a, b, c;
+  int k = wave;                        // (a workgroup has no more wavefronts than there are runs)
+  load(a, k, 0);
+  if (k + waves < p.kt) load(b, k + waves, 1);
+  for (; k + 3 * waves < p.kt; k += 2 * waves) {
+    multiply(a, 0);
+    load(a, k + 2 * waves, 0);
+    multiply(b, 1);
+    load(b, k + 3 * waves, 1);
+  }
+  multiply(a, 0);
+  if (k + 2 * waves < p.kt) load(c, k + 2 * waves, 0);
+  if (k + waves < p.kt) multiply(b, 1);
+  if (k + 2 * waves < p.kt) multiply(c, 0);
+  __syncthreads();                     // (the sums go where other wavefronts' activations are)
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int shift = p.shifts[(rt0 + r < p.mt ? rt0 + r : p.mt - 1) * 16 + l16];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      i32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (int)((uint32_t)acc[t][r][e] + (uint32_t)shift * (uint32_t)accx[t][e]);
+      *reinterpret_cast<i32x4*>(&lds[(((wave * TT + t) * RT + r) * 64 + lane) * 4]) = v;
+    }
+  }
+  __syncthreads();
+  for (int at = threadIdx.x; at < TT * RT * 256; at += blockDim.x) {
+    // 16 RT rows of W in a run of threads, so that a token's outputs are written together
+    const int r = at % (16 * RT), tok = at / (16 * RT), row = rt0 * 16 + r;
+    if (row >= p.out.m || tok >= tokens) continue;
+    const int slot = (((tok >> 4) * RT + (r >> 4)) * 64 + (tok & 15) / 4 * 16 + (r & 15)) * 4 + (tok & 3);
+    uint32_t sum = 0;
+    for (int w = 0; w < waves; ++w) sum += (uint32_t)lds[w * TT * RT * 256 + slot];
+    const float v = fmaf((float)(int)sum, p.xs[tok0 + tok] * p.scales[row], p.out.bias ? p.out.bias[row] : 0.f);
+    const int64_t o = (int64_t)(tok0 + tok) * p.out.ldy + row;
+    if (p.out.y_f32) ((float*)p.out.y)[o] = v;
+    else ((uint16_t*)p.out.y)[o] = __builtin_bit_cast(uint16_t, (__bf16)v);
+  }
+}
+
+template <int RT, int TT>
+static hipError_t launch_few8_as(const Linear8Args& p, int waves, hipStream_t s) {
+  while (waves > 1 && waves > p.kt) waves /= 2;
+  constexpr int kPerWave = TT * 4096 > TT * RT * 1024 ? TT * 4096 : TT * RT * 1024;
+  static LdsLimitOnce once;
+  if (const hipError_t e = once.ensure((const void*)&linear8_few_kernel<RT, TT>, kFew8Waves * kPerWave); e != hipSuccess) return e;
+  hipLaunchKernelGGL((linear8_few_kernel<RT, TT>), dim3((unsigned)((p.mt + RT - 1) / RT), (unsigned)((p.tokens + TT * 16 - 1) / (TT * 16))), dim3(64 * waves),
+                     (size_t)(waves * kPerWave), s, p);
+  return hipGetLastError();
+}
+static hipError_t launch_linear8(const Linear8Args& p, hipStream_t s) {
+  const int waves = p.mt < 512 && p.kt >= 64 ? 16 : 8;
+  return p.tokens <= 16 ? launch_few8_as<1, 1>(p, waves, s) : launch_few8_as<1, 2>(p, waves, s);
+}
+
+// ---- argument checks
+
+constexpr int64_t kMaxRows8 = (int64_t)1 << 20, kMaxColumns8 = (int64_t)1 << 16, kMaxTokens8 = (int64_t)1 << 23, kMaxTiles8 = (int64_t)1 << 23;
+static bool good_size8(int64_t m, int64_t n) {
+  return m > 0 && n > 0 && m <= kMaxRows8 && n <= kMaxColumns8 && ((m + 15) / 16) * ((n + 127) / 128) <= kMaxTiles8;
+}
+static size_t aligned_bytes(int64_t tokens, int64_t n) { return ((size_t)tokens * ((n + 127) / 128 * 128) + 255) / 256 * 256; }
+
+}  // namespace gptaq
+
+using namespace gptaq;
+
+extern "C" size_t gptaq_linear8_weights_bytes(int64_t m, int64_t n) { return good_size8(m, n) ? linear8_layout(m, n).bytes : 0; }
+
+extern "C" int gptaq_linear8_pack(const uint8_t* codes, int64_t ldc, const float* scales, const float* zeros, int64_t m, int64_t n, const int32_t* perm,
+                                  void* weights, size_t weights_bytes, int32_t* info, void* stream) {
+  if (!codes || !scales || !zeros || !weights || !info) return GPTAQ_ENULL;
+  if (!good_size8(m, n) || ldc < n || (((uintptr_t)scales | (uintptr_t)zeros | (uintptr_t)perm | (uintptr_t)info) & 3)) return GPTAQ_EDIM;
+  const Linear8Layout l = linear8_layout(m, n);
+  if (((uintptr_t)weights & 255) || weights_bytes < l.bytes) return GPTAQ_EWORKSPACE;
+  const hipStream_t s = (hipStream_t)stream;
+  uint8_t* const to = (uint8_t*)weights;
+  int32_t* const inverse = (int32_t*)(to + l.inverse);
+  const size_t end = l.inverse + (size_t)n * 4;
+  const unsigned columns = (unsigned)((n + 255) / 256);
+  hipLaunchKernelGGL(linear8_clear_kernel, dim3(columns), dim3(256), 0, s, inverse, (int)n, perm, info, to + end, (int)(l.bytes - end));
+  if (perm) hipLaunchKernelGGL(linear8_invert_kernel, dim3(columns), dim3(256), 0, s, inverse, (int)n, perm);
+  const int64_t pieces = l.mt * l.kt * 128;
+  hipLaunchKernelGGL(linear8_pack_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, s, codes, ldc, scales, zeros, (int)m, (int)n, pieces, (int)l.kt,
+                     inverse, to, (float*)(to + l.scales), (int32_t*)(to + l.shifts), info);
+  GPTAQ_LAUNCH_CHECK();
+  return GPTAQ_OK;
+}
+
+extern "C" size_t gptaq_linear8_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
+  if (tokens <= 0 || tokens > kMaxTokens8 || !good_size8(m, n)) return 0;
+  return aligned_bytes(tokens, n);
+}
+
+extern "C" int gptaq_linear8_i8(const int8_t* X, const float* x_scales, int64_t tokens, int64_t ldx, const void* weights, size_t weights_bytes, int64_t m, int64_t n,
+                                const float* bias, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes, void* stream) {
+  if (!weights || (tokens != 0 && (!X || !x_scales || !Y || !ws))) return GPTAQ_ENULL;      // (no tokens: nothing to point to)
+  if (tokens < 0 || tokens > kMaxTokens8 || !good_size8(m, n) || ldx < n || ldy < m || ((uintptr_t)weights & 255) || ((uintptr_t)Y & (y_f32 ? 3 : 1)) ||
+      (((uintptr_t)x_scales | (uintptr_t)bias) & 3))
+    return GPTAQ_EDIM;
+  const Linear8Layout l = linear8_layout(m, n);
+  if (weights_bytes < l.bytes) return GPTAQ_EWORKSPACE;
+  if (tokens == 0) return GPTAQ_OK;
+  if (((uintptr_t)ws & 255) || ws_bytes < gptaq_linear8_workspace_bytes(tokens, m, n)) return GPTAQ_EWORKSPACE;
+  const hipStream_t s = (hipStream_t)stream;
+  const uint8_t* const from = (const uint8_t*)weights;
+  Linear8Args p{};
+  p.out.bias = bias; p.out.y = Y; p.out.ldy = ldy; p.out.y_f32 = y_f32 ? 1 : 0; p.out.m = (int32_t)m;
+  p.x = X; p.xs = x_scales; p.ldx = ldx;
+  p.codes = from; p.scales = (const float*)(from + l.scales); p.shifts = (const int32_t*)(from + l.shifts);
+  p.mt = (int32_t)l.mt; p.kt = (int32_t)l.kt;
+  if (n % 128 || ldx % 16 || ((uintptr_t)X & 15) || ldx > kManyMaxRow) {
+    const int64_t ld = l.kt * 128, pieces = tokens * (ld / 16), blocks = (pieces + 255) / 256;
+    hipLaunchKernelGGL(linear8_align_kernel, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, X, ldx, (int)n, (int8_t*)ws, (int)ld, pieces);
+    GPTAQ_LAUNCH_CHECK();
+    p.x = (const int8_t*)ws;
+    p.ldx = ld;
+  }
+  // A grid has less than 2^32 threads, and 2^16 blocks along its second axis: more tokens than that takes are several launches.
+  int64_t most = (((int64_t)1 << 22) / l.mt) * 16;
+  if (most > 65535 * 16) most = 65535 * 16;
+  for (int64_t first = 0; first < tokens; first += most) {
+    Linear8Args part = p;
+    part.tokens = (int32_t)(tokens - first < most ? tokens - first : most);
+    part.x = p.x + first * p.ldx;
+    part.xs = p.xs + first;
+    part.out.y = (uint8_t*)Y + first * ldy * (y_f32 ? 4 : 2);
+    if (const hipError_t e = launch_linear8(part, s); e != hipSuccess) { set_last_hip_error(e); return GPTAQ_ELAUNCH; }
+  }
+  return GPTAQ_OK;
+}

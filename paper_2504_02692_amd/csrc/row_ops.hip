@@ -1,5 +1,5 @@
 // What lies between the products of a quantised layer set: the root-mean-square norm with the residual's addition, and the gated
-// activation, each with its output in bfloat16 or as 8-bit codes with one scale per token.
+// activation, each with its output in bfloat16 or as 8-bit codes with one scale per token; and rows that are in bfloat16 already as such codes.
 #include "common.h"
 
 namespace gptaq {
@@ -106,7 +106,7 @@ __device__ __forceinline__ float ro_silu(float g) {
 }
 
 struct RowArgs {
-  const uint16_t *a, *b, *weight;      // norm: x, residual (or NULL), weight (or NULL); gated: gate, up
+  const uint16_t *a, *b, *weight;      // norm: x, residual (or NULL), weight (or NULL); gated: gate, up; plain: x
   int64_t lda, ldb;
   uint16_t* sum; int64_t lds;          // norm with a residual: bf16(x + residual)
   uint16_t* y; int8_t* codes; int64_t ldy;
@@ -122,8 +122,13 @@ struct RowArgs {
 // the inputs' own memory: a thread writes only columns that it has read, and reads no others.  (Codes take half the bytes: not where other threads' columns were.)
 // 8 bits: scale = clip * max|y| / 127, code = rint(y / scale); the maximum is taken of |h w| and multiplied by the positive 1 / rms
 // afterwards, so one pass and one reduction give both.
-template <bool NORM, bool CODES>
+// Plain rows take the nearest code to the quotient itself: their values have eight bits, so quotients between two codes are common where
+// the scale has few bits, and a product with the reciprocal would break those ties at random.  The product is within 2 ulp of the quotient: it is
+// divided only where a tie is as near as that, which few wavefronts meet.
+enum RowKind { kGated = 0, kNorm = 1, kPlain = 2 };
+template <int KIND, bool CODES>
 __global__ __launch_bounds__(1024) void row_kernel(RowArgs p) {
+  constexpr bool NORM = KIND == kNorm;
   __shared__ float part[128];
   constexpr int KEEP = 4;
   const int T = blockDim.x, waves = T >> 6;
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(1024) void row_kernel(RowArgs p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += u[i];
       }
-    } else {
+    } else if (KIND == kGated) {
       ro_load(b, c, n, u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = ro_silu(v[i]) * u[i];
@@ -210,7 +215,8 @@ __global__ __launch_bounds__(1024) void row_kernel(RowArgs p) {
       int q[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float f = divide ? v[i] / scale : v[i] * inv;
+        float f = divide ? v[i] / scale : v[i] * inv;
+        if (KIND == kPlain && !divide && fabsf(f - rintf(f)) > 0.4999f) f = v[i] / scale;
         q[i] = (int)rintf(fminf(fmaxf(f, -127.f), 127.f));     // (a row that is not finite: inv is 0, NaN becomes -127)
       }
       ro_store_codes(p.codes + t * p.ldy, c, n, q);
@@ -233,19 +239,19 @@ __global__ __launch_bounds__(1024) void row_kernel(RowArgs p) {
   }
 }
 
-static int launch_rows(RowArgs p, bool norm, void* stream) {
+static int launch_rows(RowArgs p, RowKind kind, void* stream) {
   const int pieces = (p.n + 7) / 8;
   // Threads of a row.  With few rows, or nothing to reduce, one piece each: a row takes the least time.  With many rows two to four pieces, and 512
   // threads as far as these hold a row, so that three rows share a CU (76 to 79 registers: six wavefronts a SIMD) and one reads while another waits in its reduction.
   // 16384 x 8192, norm / 8 bits, 1024, 512, 256 threads: 237 / 254, 194 / 197, 203 / 191 us; 16384 x 11008, 1024, 704, 512: 338 / 388, 277 / 307, 265 / 268.
-  const bool reduces = norm || p.codes;
+  const bool reduces = kind == kNorm || p.codes;
   int T = p.tokens < 512 || !reduces ? pieces : pieces <= 2048 ? (pieces + 1) / 2 : (pieces + 3) / 4;
   if (p.tokens >= 512 && reduces && pieces <= 2048 && T > 512) T = 512;
   T = (T + 63) / 64 * 64;
   if (T > 1024) T = 1024;
   const int rows = T == 64 ? 4 : 1;
-  const auto kernel = norm ? (p.codes ? &row_kernel<true, true> : &row_kernel<true, false>)
-                           : (p.codes ? &row_kernel<false, true> : &row_kernel<false, false>);
+  const auto kernel = kind == kNorm ? (p.codes ? &row_kernel<kNorm, true> : &row_kernel<kNorm, false>)
+                      : kind == kGated ? (p.codes ? &row_kernel<kGated, true> : &row_kernel<kGated, false>) : &row_kernel<kPlain, true>;
   constexpr int kRowsPerLaunch = 1 << 21;              // (a grid has less than 2^32 threads)
   const int tokens = p.tokens;
   for (int64_t first = 0; first < tokens; first += kRowsPerLaunch) {
@@ -295,7 +301,7 @@ extern "C" int gptaq_rms_norm(const uint16_t* X, const uint16_t* residual, const
   if (const int rc = norm_args(p, X, residual, weight, tokens, n, ldx, ldr, eps, sum, lds, ldy)) return rc;
   if (odd(Y)) return GPTAQ_EDIM;
   p.y = Y;
-  return launch_rows(p, true, stream);
+  return launch_rows(p, kNorm, stream);
 }
 
 extern "C" int gptaq_rms_norm_i8(const uint16_t* X, const uint16_t* residual, const uint16_t* weight, int64_t tokens, int64_t n, int64_t ldx,
@@ -307,7 +313,7 @@ extern "C" int gptaq_rms_norm_i8(const uint16_t* X, const uint16_t* residual, co
   if (!(clip > 0.f && clip <= 1.f)) return GPTAQ_EUNSUPPORTED;
   if (tokens != 0 && (same(codes, X) || same(codes, residual) || same(codes, sum))) return GPTAQ_EUNSUPPORTED;
   p.codes = codes; p.scales = scales; p.clip = clip;
-  return launch_rows(p, true, stream);
+  return launch_rows(p, kNorm, stream);
 }
 
 extern "C" int gptaq_silu_mul(const uint16_t* gate, const uint16_t* up, int64_t tokens, int64_t n, int64_t ldg, int64_t ldu, uint16_t* Y,
@@ -317,7 +323,7 @@ extern "C" int gptaq_silu_mul(const uint16_t* gate, const uint16_t* up, int64_t 
   if (const int rc = gated_args(p, gate, up, tokens, n, ldg, ldu, ldy)) return rc;
   if (odd(Y)) return GPTAQ_EDIM;
   p.y = Y;
-  return launch_rows(p, false, stream);
+  return launch_rows(p, kGated, stream);
 }
 
 extern "C" int gptaq_silu_mul_i8(const uint16_t* gate, const uint16_t* up, int64_t tokens, int64_t n, int64_t ldg, int64_t ldu, float clip,
@@ -328,5 +334,18 @@ extern "C" int gptaq_silu_mul_i8(const uint16_t* gate, const uint16_t* up, int64
   if (!(clip > 0.f && clip <= 1.f)) return GPTAQ_EUNSUPPORTED;
   if (tokens != 0 && (same(codes, gate) || same(codes, up))) return GPTAQ_EUNSUPPORTED;
   p.codes = codes; p.scales = scales; p.clip = clip;
-  return launch_rows(p, false, stream);
+  return launch_rows(p, kGated, stream);
+}
+
+extern "C" int gptaq_quant_activations_i8(const uint16_t* X, int64_t tokens, int64_t n, int64_t ldx, float clip, int8_t* codes, int64_t ldc, float* scales,
+                                          void* stream) {
+  if (tokens != 0 && (!X || !codes || !scales)) return GPTAQ_ENULL;
+  if (tokens < 0 || tokens > kMaxTokens || n <= 0 || n > kMaxColumns || ldx < n || ldc < n || odd(X) || ((uintptr_t)scales & 3)) return GPTAQ_EDIM;
+  if (!(clip > 0.f && clip <= 1.f)) return GPTAQ_EUNSUPPORTED;
+  if (tokens != 0 && same(codes, X)) return GPTAQ_EUNSUPPORTED;
+  RowArgs p{};
+  p.a = X; p.lda = ldx; p.ldy = ldc;
+  p.tokens = (int)tokens; p.n = (int)n;
+  p.codes = codes; p.scales = scales; p.clip = clip;
+  return launch_rows(p, kPlain, stream);
 }
