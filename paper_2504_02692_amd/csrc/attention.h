@@ -87,12 +87,16 @@ __device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2
 // The running maximum is raised only when a score passes it by 2^8: a softmax does not depend on what is taken off its exponents, and weights up to 256 times
 // larger change no rounding of bf16 or fp32, so most tiles scale nothing.
 constexpr float kSlack = 8.f;
+// The score of a key that is not seen.  (One that is, with a score of minus infinity, has the same weight: none.)
+constexpr float kUnseen = -__builtin_inff();
 // A maximum to take off: rows that have seen nothing have none.
 __device__ __forceinline__ float at_origin(float m) { return m == -__builtin_inff() ? 0.f : m; }
 
 // What sums taken with the maximum `was` are multiplied by when it is `now`.  (Sums without a maximum are zero, or NaN.)
 __device__ __forceinline__ float at_factor(float was, float now) { return was == -__builtin_inff() ? 1.f : at_exp2(was - now); }
 
-hipError_t launch_attention_many(const AttentionArgs& a, hipStream_t s);
+// attention_many.hip: blocks of 32 kManyWaves rows, `blocks` of them (a.rows_bits is set).
+constexpr int kManyWaves = 8, kManyBits = 8;
+hipError_t launch_attention_many(const AttentionArgs& a, int64_t blocks, hipStream_t s);
 
 }  // namespace gptaq

@@ -70,19 +70,13 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
       for (int i = 0; i < KS; ++i) sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, g.k[t][i]), qf[i], sc[t], 0, 0, 0);
     const bool whole = g.ok == 3 && g.j0 + 31 <= pmin && (a.window == 0 || g.j0 > pmax - a.window || g.j0 + 31 < a.sinks);
     float v[8];
-    uint32_t seen = 255;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = sc[e >> 2][e & 3] * a.scale;
     if (!whole) {
-      seen = 0;
-      const int j = g.j0 + quad * 8;
-      const bool have = quad < 2 ? (g.ok & 1) : (g.ok & 2);
+      const int j = g.j0 + quad * 8, after = a.window ? p_row - a.window - j : -1 << 30, sinks = a.sinks - j;
+      const int until = (quad < 2 ? (g.ok & 1) : (g.ok & 2)) ? p_row - j : -1;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool here = have && attention_sees(a, p_row, j + e);
-        seen |= (here ? 1u : 0u) << e;
-        v[e] = here ? v[e] : -__builtin_inff();
-      }
+      for (int e = 0; e < 8; ++e) v[e] = e <= until && (e > after || e < sinks) ? v[e] : kUnseen;
     }
     float most = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
     if (__ballot(most > top + kSlack)) {
@@ -106,7 +100,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
       if (__ballot(any)) {
         u32x4 ones;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ones[i] = (seen >> (2 * i) & 1 ? 0x3f80u : 0u) | (seen >> (2 * i + 1) & 1 ? 0x3f800000u : 0u);
+        for (int i = 0; i < 4; ++i) ones[i] = (v[2 * i] != kUnseen ? 0x3f80u : 0u) | (v[2 * i + 1] != kUnseen ? 0x3f800000u : 0u);
 #pragma unroll
         for (int i = 0; i < VT; ++i) {
           u32x4 marks;
@@ -220,24 +214,28 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 }
 
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
-constexpr int64_t kMostParts = 64, kFewBits = 4, kPartialRows = 32768;
+constexpr int64_t kMostParts = 64, kFewBits = 4, kPartialRows = 65536;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
-// Parts of the keys: blocks for eight workgroups a CU, if the keys last.
-static int64_t attention_part_count(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads) {
-  const int64_t group = heads / kv_heads, blocks = ((tokens * group + 15) / 16 > seqs ? (tokens * group + 15) / 16 : seqs) * kv_heads;
-  const int64_t parts = 2048 / blocks;
-  return parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts;
+struct Plan { int bits; int64_t parts; };
+// Rows of a block, and parts of the keys: blocks of few rows for eight workgroups a CU, of many rows for one a CU, if the keys last.
+static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads) {
+  const int64_t group = heads / kv_heads;
+  const bool many = tokens * group > 32 * seqs;
+  const int bits = many ? kManyBits : kFewBits;
+  const int64_t full = ((tokens * group - 1) >> bits) + 1, blocks = (full > seqs ? full : seqs) * kv_heads, parts = (many ? 256 : 2048) / blocks;
+  return Plan{bits, parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts};
 }
-// Room for the parts' sums: parts times blocks is 2048 at most, so parts times rows 32768.  (More tokens never take less, so a workspace serves all smaller calls.)
+// Room for the parts' sums: parts times blocks times their rows is 65536 at most.  (More tokens never take less, so a workspace serves all smaller calls.)
 static int64_t partial_rows(int64_t tokens, int64_t heads) { return kMostParts * tokens * heads < kPartialRows ? kMostParts * tokens * heads : kPartialRows; }
 
 template <int D>
 static hipError_t launch_attention(const AttentionArgs& all, hipStream_t s) {
   AttentionArgs a = all;
-  a.rows_bits = kFewBits;
-  const int64_t blocks = attention_blocks(a.c.tokens, a.c.seqs, a.c.group, kFewBits), each = (int64_t)a.parts * a.c.kv_heads;
+  const int64_t blocks = attention_blocks(a.c.tokens, a.c.seqs, a.c.group, a.rows_bits), each = (int64_t)a.parts * a.c.kv_heads;
+  if (a.rows_bits == kManyBits)
+    if (const hipError_t e = launch_attention_many(a, blocks, s); e != hipSuccess) return e;
   const int64_t most = ((int64_t)1 << 23) / each;                    // (a grid has less than 2^32 threads)
-  for (int64_t first = 0; first < blocks; first += most) {
+  for (int64_t first = a.rows_bits == kManyBits ? blocks : 0; first < blocks; first += most) {
     a.first_block = first;
     const int64_t n = blocks - first < most ? blocks - first : most;
     hipLaunchKernelGGL(attention_few_kernel<D>, dim3((unsigned)(n * each)), dim3(256), 0, s, a);
@@ -284,11 +282,13 @@ extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const
   constexpr int64_t kFar = (int64_t)1 << 30;                          // (positions are below this)
   a.q = q; a.keys = keys; a.values = values; a.ldq = ldq; a.hq = hq;
   a.out = out; a.ldo = ldo; a.ho = ho;
-  a.scale = scale * 1.4426950408889634f;
+  a.scale = scale == 0.f ? 0x1p-126f : scale * 1.4426950408889634f;  // (0 times the minus infinity of a key that is not seen is NaN; 2^-126 gives the same weights)
   a.window = (int32_t)(window < kFar ? window : 0);
   a.sinks = (int32_t)(sinks < kFar ? sinks : kFar);
-  a.parts = (int32_t)attention_part_count(tokens, seqs, heads, kv_heads);
-  a.min_tiles = 2;
+  const Plan plan = attention_plan(tokens, seqs, heads, kv_heads);
+  a.rows_bits = plan.bits;
+  a.parts = (int32_t)plan.parts;
+  a.min_tiles = plan.bits == kManyBits ? 8 : 2;
   a.partial = (float*)ws;
   a.stats = a.partial + (int64_t)a.parts * tokens * heads * d;
   if (pages == 0) a.c.table_pages = 0;                                // no key anywhere: zeros
