@@ -43,6 +43,8 @@ __device__ __forceinline__ Tiles attention_tiles(const AttentionArgs& a, int pmi
 __device__ __forceinline__ bool attention_sees(const AttentionArgs& a, int p, int j) {
   return j <= p && (a.window == 0 || j > p - a.window || j < a.sinks);
 }
+// The token of a row that is the same in all lanes (a division is vector work).
+__device__ __forceinline__ int at_token(int row, int group) { return __builtin_amdgcn_readfirstlane(row / group); }
 // Tiles a part has, and how many parts there are.
 struct Parts { int32_t each, count; };
 __device__ __forceinline__ Parts attention_parts(const AttentionArgs& a, int tiles) {
@@ -50,15 +52,10 @@ __device__ __forceinline__ Parts attention_parts(const AttentionArgs& a, int til
   return Parts{each, (tiles + each - 1) / each};
 }
 
-// A tile that some row of the block does not see whole may hold anything where it is not seen: what other sequences left in a page, what lies behind the last
-// token, NaN.  A product with a weight of zero would let an infinity or NaN through, so there the values' entries that are not finite are taken out, and added
-// to the rows that do see them from a second product, of marks: 1 for infinity, 2^7 for minus infinity, 2^14 for NaN, summed over at most 64 keys (exact).
-__device__ __forceinline__ bool attention_strange(u32x4 v) {
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) any |= (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
-  return any;
-}
+// A tile that some row does not see whole may hold anything where it is not seen, and a weight of zero lets an infinity or NaN through.  What lies behind the
+// last position that a row sees, which nobody may have written, is taken for zeros.  Elsewhere such values are rare, so a block whose sums
+// are not all finite takes them again with care: the values' entries that are not finite are taken out, and added to the rows that do see them from a second
+// product, of marks: 1 for infinity, 2^7 for minus infinity, 2^14 for NaN, summed over at most 64 keys (exact).
 __device__ __forceinline__ void attention_marks(u32x4& v, u32x4& marks) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

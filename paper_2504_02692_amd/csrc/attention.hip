@@ -1,6 +1,7 @@
 // Attention of new tokens over a paged cache: y_i = sum_j softmax_j(scale q_i k_j) v_j over the keys that token i sees, with an optional window and first
 // tokens that stay visible.  In one pass over the keys, with the running maximum and sum of the softmax in fp32.
 #include "attention.h"
+#include <type_traits>
 
 namespace gptaq {
 
@@ -25,7 +26,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
   const int rows = seq.count * c.group;
   if (in_seq < 0 || in_seq * 16 >= rows) return;
   const int row0 = (int)in_seq * 16, last = min(row0 + 15, rows - 1);
-  const int pmin = seq.before + row0 / c.group, pmax = seq.before + last / c.group;
+  const int pmin = seq.before + at_token(row0, c.group), pmax = seq.before + at_token(last, c.group);
   const Tiles tiles = attention_tiles(a, pmin, pmax);
   const Parts parts = attention_parts(a, tiles.count);
   if (part > 0 && part >= parts.count) return;                       // (part 0 writes the zeros of rows that see nothing)
@@ -59,10 +60,9 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
   };
 
   f32x4 acc[VT];
-#pragma unroll
-  for (int i = 0; i < VT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float top = -__builtin_inff(), total = 0.f;                        // total: this lane's keys alone
-  auto work = [&](Stage& g) {
+  float top, total;                                                  // total: this lane's keys alone
+  auto work = [&](auto careful, Stage& g) {
+    constexpr bool CAREFUL = decltype(careful)::value;
     f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -93,38 +93,63 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) { w[e] = at_exp2(v[e] - from); total += w[e]; }
     const u32x4 wp = {at_bf16x2(w[0], w[1]), at_bf16x2(w[2], w[3]), at_bf16x2(w[4], w[5]), at_bf16x2(w[6], w[7])};
-    if (!whole) {
-      bool any = false;
+    if (CAREFUL) {
+      u32x4 ones;
 #pragma unroll
-      for (int i = 0; i < VT; ++i) any |= attention_strange(g.v[i]);
-      if (__ballot(any)) {
-        u32x4 ones;
+      for (int i = 0; i < 4; ++i) ones[i] = (v[2 * i] != kUnseen ? 0x3f80u : 0u) | (v[2 * i + 1] != kUnseen ? 0x3f800000u : 0u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ones[i] = (v[2 * i] != kUnseen ? 0x3f80u : 0u) | (v[2 * i + 1] != kUnseen ? 0x3f800000u : 0u);
+      for (int i = 0; i < VT; ++i) {
+        u32x4 marks;
+        attention_marks(g.v[i], marks);
+        const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < VT; ++i) {
-          u32x4 marks;
-          attention_marks(g.v[i], marks);
-          const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][e] += attention_strange_sum(n[e]);
-        }
+        for (int e = 0; e < 4; ++e) acc[i][e] += attention_strange_sum(n[e]);
       }
+    } else if (g.j0 + 31 > pmax) {                                   // behind the last position that some row sees: zeros
+      u32x4 ends;
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const int left = pmax - g.j0 - quad * 8 - 2 * h;
+        ends[h] = left >= 1 ? ~0u : left == 0 ? 0xffffu : 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < VT; ++i) g.v[i] &= ends;
     }
 #pragma unroll
     for (int i = 0; i < VT; ++i)
       acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, g.v[i]), __builtin_bit_cast(bf16x8, wp), acc[i], 0, 0, 0);
   };
   const int steps = 2 * max(0, end - begin);
-  Stage x, y;
-  int step = wave;
-  if (step < steps) load(x, step);
-  for (; step < steps; step += 8) {
-    if (step + 4 < steps) load(y, step + 4);
-    work(x);
-    if (step + 8 < steps) load(x, step + 8);
-    if (step + 4 < steps) work(y);
-  }
+  auto pass = [&](auto careful) {
+#pragma unroll
+    for (int i = 0; i < VT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    top = -__builtin_inff();
+    total = 0.f;
+    Stage x, y;
+    int step = wave;
+    if (step < steps) load(x, step);
+    if (decltype(careful)::value) {
+#pragma unroll 1
+      for (; step < steps; step += 4) {
+        work(careful, x);
+        if (step + 4 < steps) load(x, step + 4);
+      }
+      return;
+    }
+    for (; step < steps; step += 8) {
+      if (step + 4 < steps) load(y, step + 4);
+      work(careful, x);
+      if (step + 8 < steps) load(x, step + 8);
+      if (step + 4 < steps) work(careful, y);
+    }
+  };
+  pass(std::false_type{});
+  float bad = 0.f;                                                   // NaN if a sum is not finite
+#pragma unroll
+  for (int i = 0; i < VT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad = fmaf(acc[i][e], 0.f, bad);
+  if (__ballot(bad != 0.f)) pass(std::true_type{});
 
   // ---- the wavefronts' sums: a lane has row l % 16, entries 16 i + 4 quad + e
   total += __shfl_xor(total, 16);

@@ -1,6 +1,7 @@
 // Attention over a paged cache for many rows: prompts, and pieces of prompts behind what the cache has of them.
 #include "attention.h"
 #include "linear.h"
+#include <type_traits>
 
 namespace gptaq {
 
@@ -46,7 +47,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   const int rows = seq.count * c.group;
   if (in_seq < 0 || (in_seq << a.rows_bits) >= rows) return;
   const int row0 = (int)in_seq << a.rows_bits, last = min(row0 + 32 * NW - 1, rows - 1);
-  const Tiles tiles = attention_tiles(a, seq.before + row0 / c.group, seq.before + last / c.group);
+  const Tiles tiles = attention_tiles(a, seq.before + at_token(row0, c.group), seq.before + at_token(last, c.group));
   const Parts parts = attention_parts(a, tiles.count);
   if (part > 0 && part >= parts.count) return;                       // (part 0 writes the zeros of rows that see nothing)
   const int begin = part * parts.each, end = min(begin + parts.each, tiles.count);
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   const int wave0 = row0 + wave * 32, wave1 = min(wave0 + 31, last);
   const bool idle = wave0 > last;
   const int row = min(wave0 + l32, last), token = row / c.group, p_row = seq.before + token;
-  const int pmin = seq.before + min(wave0, last) / c.group, pmax = idle ? -1 : seq.before + wave1 / c.group;
+  const int pmin = seq.before + at_token(min(wave0, last), c.group), pmax = idle ? -1 : seq.before + at_token(wave1, c.group);
   const uint16_t* const qrow = a.q + (int64_t)(seq.first + token) * a.ldq + (int64_t)(head * c.group + row % c.group) * a.hq;
   typedef u32x4 __attribute__((aligned(2))) u32x4_at2;
   // (A negative scale goes to the queries' signs, so that the largest score is that of the largest product.)
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
 
   // ---- loads: a tile of keys, then of values, 1 KB each
   const int64_t head_bytes = (int64_t)(D * 2) << c.page_bits;        // of a page, of one head
-  const int32_t* const table = c.table + (int64_t)s * c.ld_table;
+  const ConstantInts table = cache_constant(c.table + (int64_t)s * c.ld_table);
   struct Ids { int id[1 << (6 - PB)]; };
   auto pages_of = [&](Ids& g, int i) {                               // of the i-th tile of this part (behind the last: that again)
     const int at = (tiles.at(min(i, end - 1)) * kTile) >> c.page_bits;
@@ -116,109 +117,207 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   }
   const int vread = (half * D + l32) * 16;
 
-  auto work = [&](auto whole_tile, int i, int j0, int ok) {
-    constexpr bool WHOLE = decltype(whole_tile)::value;
+  // Raises the maximum to that of `most` where some row needs it; returns whether sums have to be scaled by `factor`.
+  float factor = 1.f;
+  auto raise = [&](float most) {
+    if (!__ballot(most > top + kSlack)) return false;
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const float now = fmaxf(top, most);
+    factor = at_factor(top, now);
+    top = now;
+    total *= factor;
+    return true;
+  };
+  auto scale_sums = [&]() {
+#pragma unroll
+    for (int t = 0; t < VT; ++t) acc[t] *= factor;
+  };
+  // The weights of 16 keys and a row for the second product, from the scores of the tile.
+  auto weights = [&](const f32x16& sc, int k, float from) {
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = at_exp2(fmaf(sc[8 * k + e], scale, -from));
+      total += w[e];
+    }
+    return __builtin_bit_cast(bf16x8, u32x4{at_bf16x2(w[0], w[1]), at_bf16x2(w[2], w[3]), at_bf16x2(w[4], w[5]), at_bf16x2(w[6], w[7])});
+  };
+  auto values_at = [&](const unsigned char* vt, int step, int t) { return *reinterpret_cast<const u32x4*>(vt + vread + (step * 2 * D + t * 32) * 16); };
+  f32x16 sc[2];                                                      // scores of 32 keys; element e: key 16 (e / 8) + 8 half + e % 8
+  bf16x8 weight[2][2];                                               // [step & 1][16 keys]
+  // A tile of which some row sees a part, 32 keys after the other; what is behind the last position that some row sees is taken for zeros.  CAREFUL (see
+  // attention_marks) takes any tile, and every sum in the same order as where it is not needed.
+  auto work = [&](auto careful, int i, int j0, int ok) {
+    constexpr bool CAREFUL = decltype(careful)::value;
     const unsigned char* const kt = smem + (i % kRing) * 2 * TILE;
     const unsigned char* const vt = kt + TILE;
-    f32x16 sc[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
+      f32x16& s32 = sc[0];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sc[b][e] = 0.f;
+      for (int e = 0; e < 16; ++e) s32[e] = 0.f;
 #pragma unroll
       for (int k = 0; k < KS; ++k)
-        sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + kread[b] + k * (2 * P * 16)), qf[k], sc[b], 0, 0, 0);
-    }
-    // element e of block b: key 32 b + 16 (e / 8) + 8 half + e % 8
-    if (!WHOLE) {
-      const int j = j0 + 8 * half, until = p_row - j, after = a.window ? p_row - a.window - j : -1 << 30, sinks = a.sinks - j;
+        s32 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + kread[b] + k * (2 * P * 16)), qf[k], s32, 0, 0, 0);
+      const int j = j0 + 32 * b + 8 * half, until = p_row - j, after = a.window ? p_row - a.window - j : -1 << 30, sinks = a.sinks - j;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int e = 0; e < 16; ++e) {
+        const int at = 16 * (e >> 3) + (e & 7);
+        const bool here = (ok >> (2 * b + (e >> 3)) & 1) && at <= until && (at > after || at < sinks);
+        s32[e] = here ? s32[e] : kUnseen;
+      }
+      float most = s32[0];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int at = 32 * b + 16 * (e >> 3) + (e & 7);
-          const bool here = (ok >> (at >> 4) & 1) && at <= until && (at > after || at < sinks);
-          sc[b][e] = here ? sc[b][e] : kUnseen;
+      for (int e = 1; e < 16; ++e) most = fmaxf(most, s32[e]);
+      if (raise(most * scale)) scale_sums();
+      const float from = at_origin(top);
+#pragma unroll
+      for (int h16 = 0; h16 < 2; ++h16) {
+        weight[1][h16] = weights(s32, h16, from);
+        u32x4 ones, ends;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const int at = 8 * h16 + 2 * h, left = pmax - j - 16 * h16 - 2 * h;      // keys of the lane's pair that are not behind the last
+          ones[h] = (s32[at] != kUnseen ? 0x3f80u : 0u) | (s32[at + 1] != kUnseen ? 0x3f800000u : 0u);
+          ends[h] = left >= 1 ? ~0u : left == 0 ? 0xffffu : 0u;
         }
-    }
-    float most = sc[0][0];
 #pragma unroll
-    for (int e = 1; e < 32; ++e) most = fmaxf(most, sc[e >> 4][e & 15]);
-    most *= scale;
-    if (__ballot(most > top + kSlack)) {
-      most = fmaxf(most, __shfl_xor(most, 32));
-      const float now = fmaxf(top, most), factor = at_factor(top, now);
-      top = now;
-      total *= factor;
+        for (int t = 0; t < VT; ++t) {
+          u32x4 v = values_at(vt, 2 * b + h16, t);
+          if (CAREFUL) {
+            u32x4 marks;
+            attention_marks(v, marks);
+            f32x16 n;
 #pragma unroll
-      for (int t = 0; t < VT; ++t) acc[t] *= factor;
-    }
-    const float from = at_origin(top);
+            for (int e = 0; e < 16; ++e) n[e] = 0.f;
+            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), n, 0, 0, 0);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[e] = at_exp2(fmaf(sc[b][8 * k + e], scale, -from));
-          total += w[e];
-        }
-        const u32x4 wp = {at_bf16x2(w[0], w[1]), at_bf16x2(w[2], w[3]), at_bf16x2(w[4], w[5]), at_bf16x2(w[6], w[7])};
-        u32x4 v[VT];
-#pragma unroll
-        for (int t = 0; t < VT; ++t) v[t] = *reinterpret_cast<const u32x4*>(vt + vread + ((b * 4 + k * 2) * D + t * 32) * 16);
-        if (!WHOLE) {
-          bool any = false;
-#pragma unroll
-          for (int t = 0; t < VT; ++t) any |= attention_strange(v[t]);
-          if (__ballot(any)) {
-            u32x4 ones;
-#pragma unroll
-            for (int h = 0; h < 4; ++h) ones[h] = (sc[b][8 * k + 2 * h] != kUnseen ? 0x3f80u : 0u) | (sc[b][8 * k + 2 * h + 1] != kUnseen ? 0x3f800000u : 0u);
-#pragma unroll
-            for (int t = 0; t < VT; ++t) {
-              u32x4 marks;
-              attention_marks(v[t], marks);
-              f32x16 n;
-#pragma unroll
-              for (int e = 0; e < 16; ++e) n[e] = 0.f;
-              n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), n, 0, 0, 0);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) acc[t][e] += attention_strange_sum(n[e]);
-            }
+            for (int e = 0; e < 16; ++e) acc[t][e] += attention_strange_sum(n[e]);
+          } else {
+            v &= ends;
           }
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), weight[1][h16], acc[t], 0, 0, 0);
         }
-#pragma unroll
-        for (int t = 0; t < VT; ++t)
-          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[t]), __builtin_bit_cast(bf16x8, wp), acc[t], 0, 0, 0);
       }
     }
   };
 
-  if (begin < end) {
-    Ids ids[kRing];                                                  // of the tiles in flight: ids[k] of tile i + k
+  // Tiles that all the wavefront's rows see whole go through in steps of 32 keys, each with three parts that do not wait for each other: the next step's scores, this one's
+  // weights, and the product of the last one's weights with its values.  So the matrix unit works while the vector unit takes exponentials.  Groups of one
+  // instruction of either product, the reads of the group after the next, and the group's share of the weights; the barriers keep the compiler to this order.
+  auto scores_alone = [&](f32x16& next, const unsigned char* kt, int from) {
 #pragma unroll
-    for (int k = 0; k < kRing - 1; ++k) {
-      pages_of(ids[k], begin + k);
-      load_tile(ids[k], begin + k);
+    for (int e = 0; e < 16; ++e) next[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + from + k * (2 * P * 16)), qf[k], next, 0, 0, 0);
+  };
+  auto product_alone = [&](const bf16x8 (&w)[2], const unsigned char* vt, int step) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+      acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values_at(vt, step + k / VT, k % VT)), w[k / VT], acc[k % VT], 0, 0, 0);
+  };
+  auto step = [&](auto with_product, const f32x16& now, f32x16& next, const unsigned char* kt, int kfrom, const bf16x8 (&before)[2], const unsigned char* vt, int vstep,
+                  bf16x8 (&w)[2]) {
+    constexpr bool PRODUCT = decltype(with_product)::value;
+    constexpr int AHEAD = 2;
+    u32x4 kf[AHEAD + 1], vf[AHEAD + 1];
+    auto read = [&](int k) {
+      kf[k % (AHEAD + 1)] = *reinterpret_cast<const u32x4*>(kt + kfrom + k * (2 * P * 16));
+      if (PRODUCT) vf[k % (AHEAD + 1)] = values_at(vt, vstep + k / VT, k % VT);
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) read(k);
+    float most = now[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) most = fmaxf(most, now[e]);
+    const bool raised = raise(most * scale);
+    const float from = at_origin(top);
+    float x[16];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      if (k + AHEAD < KS) read(k + AHEAD);
+      const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[k % (AHEAD + 1)]), qf[k], k == 0 ? zero : next, 0, 0, 0);
+#pragma unroll
+      for (int e = k * 16 / KS; e < (k + 1) * 16 / KS; ++e) {
+        x[e] = at_exp2(fmaf(now[e], scale, -from));
+        asm volatile("" : "+v"(x[e]));                               // (here, not behind the products)
+        total += x[e];
+      }
+      if (PRODUCT) acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k % (AHEAD + 1)]), before[k / VT], acc[k % VT], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    pages_of(ids[kRing - 1], begin + kRing - 1);
-    for (int i = begin; i < end; ++i) {
-      am_wait<(kRing - 2) * Shape::kPerWave>();                      // the wavefront's loads of tile i are there ..
-      am_barrier();                                                  // .. and everyone's; and tile i - 1 is no longer read
-      load_tile(ids[kRing - 1], i + kRing - 1);
-      const int ok = valid(ids[0]);
 #pragma unroll
-      for (int k = 0; k < kRing - 1; ++k) ids[k] = ids[k + 1];
-      pages_of(ids[kRing - 1], i + kRing);
-      const int j0 = tiles.at(i) * kTile;
-      if (j0 > pmax || (a.window && j0 + kTile - 1 <= pmin - a.window && j0 >= a.sinks)) continue;
-      if (ok == 15 && j0 + kTile - 1 <= pmin && (a.window == 0 || j0 > pmax - a.window || j0 + kTile - 1 < a.sinks)) work(std::true_type{}, i, j0, ok);
-      else work(std::false_type{}, i, j0, ok);
+    for (int h = 0; h < 2; ++h)
+      w[h] = __builtin_bit_cast(bf16x8, u32x4{at_bf16x2(x[8 * h], x[8 * h + 1]), at_bf16x2(x[8 * h + 2], x[8 * h + 3]), at_bf16x2(x[8 * h + 4], x[8 * h + 5]),
+                                              at_bf16x2(x[8 * h + 6], x[8 * h + 7])});
+    if (raised) scale_sums();
+  };
+
+  // what the wavefront does with a tile: 0 nothing (none of its rows sees any of it), 1 rows see parts of it, 2 all rows see it whole (3: the one before it, too, so that
+  // sc[0] has the scores of its first step, and weight[1] the weights of the step before that)
+  auto kind_of = [&](const Ids& g, int i) {
+    const int j0 = tiles.at(min(i, end - 1)) * kTile;
+    if (i >= end || j0 > pmax || (a.window && j0 + kTile - 1 <= pmin - a.window && j0 >= a.sinks)) return 0;
+    return valid(g) == 15 && j0 + kTile - 1 <= pmin && (a.window == 0 || j0 > pmax - a.window || j0 + kTile - 1 < a.sinks) ? 2 : 1;
+  };
+  auto keys_at = [&](int i) { return smem + (i % kRing) * 2 * TILE; };
+  auto pass = [&](auto careful) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    Ids now, next, after;                                            // pages of tiles i, i + 1, i + 2
+    pages_of(now, begin);
+    load_tile(now, begin);
+    pages_of(next, begin + 1);
+    load_tile(next, begin + 1);
+    pages_of(after, begin + 2);
+    int kind = __builtin_amdgcn_readfirstlane(kind_of(now, begin));
+    for (int i = begin; i < end; ++i) {
+      am_wait<0>();                                                  // the wavefront's loads of tile i + 1 are there ..
+      am_barrier();                                                  // .. and everyone's; and tile i - 2 is no longer read
+      load_tile(after, i + 2);
+#pragma unroll
+      for (int t = 0; t < VT; ++t) asm volatile("" : "+v"(acc[t]));  // (sums stay in their registers whichever way a tile goes,
+      kind = __builtin_amdgcn_readfirstlane(kind);
+      asm volatile("" : "+s"(kind));                                 // and no way has a loop of its own)
+      const int ok = valid(now), then = __builtin_amdgcn_readfirstlane(kind_of(next, i + 1));
+      now = next;
+      next = after;
+      pages_of(after, i + 3);
+      if (!CAREFUL && kind >= 2) {
+        const unsigned char* const kt = keys_at(i);
+        if (kind == 3) {
+          step(std::true_type{}, sc[0], sc[1], kt, kread[1], weight[1], keys_at(i - 1) + TILE, 2, weight[0]);
+        } else {
+          scores_alone(sc[0], kt, kread[0]);
+          step(std::false_type{}, sc[0], sc[1], kt, kread[1], weight[1], kt, 0, weight[0]);
+        }
+        step(std::true_type{}, sc[1], sc[0], keys_at(i + 1), kread[0], weight[0], kt + TILE, 0, weight[1]);
+        if (then != 2) product_alone(weight[1], kt + TILE, 2);
+      } else if (kind != 0) {
+        work(careful, i, tiles.at(i) * kTile, ok);
+      }
+      kind = kind >= 2 && then == 2 ? 3 : then;
     }
     am_wait<0>();                                                    // (no load writes to LDS from here on)
-    am_barrier();
+  };
+  if (begin < end) {
+    pass(std::false_type{});
+    float bad = 0.f;                                                 // NaN if a sum is not finite
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) bad = fmaf(acc[t][e], 0.f, bad);
+    if (__syncthreads_or(bad != 0.f)) {
+#pragma unroll
+      for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+      top = -__builtin_inff();
+      total = 0.f;
+      pass(std::true_type{});
+      __syncthreads();
+    }
   }
   if (idle) return;
 

@@ -16,13 +16,16 @@ struct CacheShape {
 // A sequence's new tokens: rows first .. first + count - 1, positions before .. before + count - 1 (before may be negative where `lengths` says less than
 // `starts`; positions below 0 are no tokens).  Whatever the arrays hold, rows stay inside the tensors and positions inside 31 bits.
 struct Sequence { int32_t index, first, count, before; };
+// What one address serves all lanes is read through the scalar cache (nothing of it changes while a kernel runs), and waited for apart from loads to LDS.
+typedef const __attribute__((address_space(4))) int32_t* ConstantInts;
+__device__ __forceinline__ ConstantInts cache_constant(const int32_t* p) { return (ConstantInts)(uintptr_t)p; }
 __device__ __forceinline__ int cache_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 __device__ __forceinline__ Sequence cache_sequence(const CacheShape& c, int s) {
   Sequence q;
   q.index = s;
-  q.first = cache_clamp(c.starts[s], 0, c.tokens);
-  q.count = cache_clamp(c.starts[s + 1], q.first, c.tokens) - q.first;
-  q.before = cache_clamp(c.lengths[s], 0, 1 << 30) - q.count;
+  q.first = cache_clamp(cache_constant(c.starts)[s], 0, c.tokens);
+  q.count = cache_clamp(cache_constant(c.starts)[s + 1], q.first, c.tokens) - q.first;
+  q.before = cache_clamp(cache_constant(c.lengths)[s], 0, 1 << 30) - q.count;
   return q;
 }
 // Work is dealt out without the host knowing the lengths: with `units` pieces a token and `per` of them to a block, sequence s has the blocks from
@@ -48,7 +51,7 @@ __device__ __forceinline__ int cache_find(const CacheShape& c, int64_t block, in
 __device__ __forceinline__ int cache_page(const CacheShape& c, int s, int position) {
   const int at = position >> c.page_bits;
   if (at >= c.table_pages) return -1;
-  const int id = c.table[s * c.ld_table + at];
+  const int id = cache_constant(c.table + s * c.ld_table)[at];
   return (uint32_t)id < (uint64_t)c.pages ? id : -1;
 }
 
