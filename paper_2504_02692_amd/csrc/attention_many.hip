@@ -66,33 +66,41 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
 #pragma unroll
   for (int i = 0; i < KS; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4_at2*>(qrow + i * 16 + half * 8) ^ flip);
 
-  // ---- loads: a tile of keys, then of values, 1 KB each
+  // ---- loads: a tile of keys, then of values, 1 KB each; a wavefront's are neighbours.  Of a page of up to 64 positions they are one run, of a larger one the keys'
+  // are a row of 64 positions each.
+  constexpr int PAGES = 1 << (6 - PB), PER = Shape::kLoads >> (6 - PB);      // pages of a tile, loads of a page
   const int64_t head_bytes = (int64_t)(D * 2) << c.page_bits;        // of a page, of one head
+  const int64_t page_bytes = head_bytes * c.kv_heads;
+  const unsigned char* const keys_base = (const unsigned char*)a.keys + head * head_bytes;
+  const unsigned char* const values_base = (const unsigned char*)a.values + head * head_bytes;
   const ConstantInts table = cache_constant(c.table + (int64_t)s * c.ld_table);
-  struct Ids { int id[1 << (6 - PB)]; };
-  auto pages_of = [&](Ids& g, int i) {                               // of the i-th tile of this part (behind the last: that again)
-    const int at = (tiles.at(min(i, end - 1)) * kTile) >> c.page_bits;
+  const int last_tile = tiles.at(max(end - 1, 0));
+  struct Ids { int id[PAGES]; };
+  auto tile_of = [&](int i) { return i < end ? tiles.at(i) : last_tile; };      // (behind the last that again)
+  auto pages_of = [&](Ids& g, int tile) {
+    const int at = (tile * kTile) >> c.page_bits;
 #pragma unroll
-    for (int k = 0; k < (1 << (6 - PB)); ++k) {
+    for (int k = 0; k < PAGES; ++k) {
       const int id = at + k < c.table_pages ? table[at + k] : -1;
-      g.id[k] = __builtin_amdgcn_readfirstlane((uint32_t)id < (uint64_t)c.pages ? id : -1);
+      g.id[k] = (uint32_t)id < (uint32_t)c.pages ? id : -1;
     }
   };
-  auto load_tile = [&](const Ids& g, int i) {
-    const int off = (tiles.at(min(i, end - 1)) * kTile) & ((1 << c.page_bits) - 1);      // (in a page of more than 64)
-    constexpr int PER = Shape::kLoads >> (6 - PB);                   // loads of a page
+  const int off_mask = (1 << c.page_bits) - 1;
+  const int key_step = PB < 6 ? 1024 : 16 << c.page_bits;            // from one load of keys of a page to the next
+  auto load_tile = [&](const Ids& g, int tile, int slot) {
+    const int off = PB < 6 ? 0 : (tile * kTile) & off_mask;
+    unsigned char* const to = smem + slot * 2 * TILE;
 #pragma unroll
     for (int n = 0; n < Shape::kPerWave; ++n) {
-      const int at = wave * Shape::kPerWave + n, load = at % Shape::kLoads;
+      const int at = wave * Shape::kPerWave + n;
       const bool value = at >= Shape::kLoads;
-      const int which = load / PER, in_page = load % PER;
+      const int load = value ? at - Shape::kLoads : at, which = load / PER, in_page = load - which * PER;
       int id = g.id[0];
 #pragma unroll
-      for (int k = 1; k < (1 << (6 - PB)); ++k) id = which == k ? g.id[k] : id;
-      const int64_t from = ((int64_t)max(id, 0) * c.kv_heads + head) * head_bytes +
-                           (PB < 6 ? in_page * 1024 : value ? off * (D * 2) + in_page * 1024 : ((in_page << c.page_bits) + off) * 16);
-      const LdsLoader loader((const unsigned char*)(value ? a.values : a.keys) + from);
-      loader.load(smem + ((i % kRing) * 2 + (value ? 1 : 0)) * TILE + load * 1024, lane * 16, 0);
+      for (int k = 1; k < PAGES; ++k) id = which == k ? g.id[k] : id;
+      const int inside = value ? off * (D * 2) + in_page * 1024 : off * 16 + in_page * key_step;
+      const LdsLoader loader((value ? values_base : keys_base) + max(id, 0) * page_bytes);
+      loader.load(to + at * 1024, lane * 16, inside);
     }
   };
   auto valid = [&](const Ids& g) {                                   // a bit for each 16 keys
@@ -147,9 +155,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   bf16x8 weight[2][2];                                               // [step & 1][16 keys]
   // A tile of which some row sees a part, 32 keys after the other; what is behind the last position that some row sees is taken for zeros.  CAREFUL (see
   // attention_marks) takes any tile, and every sum in the same order as where it is not needed.
-  auto work = [&](auto careful, int i, int j0, int ok) {
+  auto work = [&](auto careful, const unsigned char* kt, int j0, int ok) {
     constexpr bool CAREFUL = decltype(careful)::value;
-    const unsigned char* const kt = smem + (i % kRing) * 2 * TILE;
     const unsigned char* const vt = kt + TILE;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -216,14 +223,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
     for (int k = 0; k < KS; ++k)
       acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values_at(vt, step + k / VT, k % VT)), w[k / VT], acc[k % VT], 0, 0, 0);
   };
-  auto step = [&](auto with_product, const f32x16& now, f32x16& next, const unsigned char* kt, int kfrom, const bf16x8 (&before)[2], const unsigned char* vt, int vstep,
+  auto step = [&](const f32x16& now, f32x16& next, const unsigned char* kt, int kfrom, const bf16x8 (&before)[2], const unsigned char* vt, int vstep,
                   bf16x8 (&w)[2]) {
-    constexpr bool PRODUCT = decltype(with_product)::value;
     constexpr int AHEAD = 2;
     u32x4 kf[AHEAD + 1], vf[AHEAD + 1];
     auto read = [&](int k) {
       kf[k % (AHEAD + 1)] = *reinterpret_cast<const u32x4*>(kt + kfrom + k * (2 * P * 16));
-      if (PRODUCT) vf[k % (AHEAD + 1)] = values_at(vt, vstep + k / VT, k % VT);
+      vf[k % (AHEAD + 1)] = values_at(vt, vstep + k / VT, k % VT);
     };
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) read(k);
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
         asm volatile("" : "+v"(x[e]));                               // (here, not behind the products)
         total += x[e];
       }
-      if (PRODUCT) acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k % (AHEAD + 1)]), before[k / VT], acc[k % VT], 0, 0, 0);
+      acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k % (AHEAD + 1)]), before[k / VT], acc[k % VT], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -255,49 +261,62 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
     if (raised) scale_sums();
   };
 
-  // what the wavefront does with a tile: 0 nothing (none of its rows sees any of it), 1 rows see parts of it, 2 all rows see it whole (3: the one before it, too, so that
-  // sc[0] has the scores of its first step, and weight[1] the weights of the step before that)
-  auto kind_of = [&](const Ids& g, int i) {
-    const int j0 = tiles.at(min(i, end - 1)) * kTile;
-    if (i >= end || j0 > pmax || (a.window && j0 + kTile - 1 <= pmin - a.window && j0 >= a.sinks)) return 0;
-    return valid(g) == 15 && j0 + kTile - 1 <= pmin && (a.window == 0 || j0 > pmax - a.window || j0 + kTile - 1 < a.sinks) ? 2 : 1;
+  // Tiles of which the wavefront's rows see something are seen_from .. seen_to and those below seen_sinks; tiles that all of them see whole likewise.
+  const int seen_to = pmax >> 6, seen_from = a.window ? max(pmin - a.window + 1, 0) >> 6 : 0, seen_sinks = a.window ? (a.sinks + kTile - 1) / kTile : 0;
+  const int whole_to = ((pmin + 1) >> 6) - 1, whole_from = a.window ? (max(pmax - a.window + 1, 0) + kTile - 1) >> 6 : 0, whole_sinks = a.window ? a.sinks / kTile : 0;
+  enum { kNothing, kParts, kWhole };
+  auto kind_of = [&](const Ids& g, int tile) {
+    const bool some = tile <= seen_to && (tile >= seen_from || tile < seen_sinks);
+    const bool all = tile <= whole_to && (tile >= whole_from || tile < whole_sinks) && valid(g) == 15;
+    return idle ? kNothing : all ? kWhole : some ? kParts : kNothing;
   };
-  auto keys_at = [&](int i) { return smem + (i % kRing) * 2 * TILE; };
   auto pass = [&](auto careful) {
     constexpr bool CAREFUL = decltype(careful)::value;
     Ids now, next, after;                                            // pages of tiles i, i + 1, i + 2
-    pages_of(now, begin);
-    load_tile(now, begin);
-    pages_of(next, begin + 1);
-    load_tile(next, begin + 1);
-    pages_of(after, begin + 2);
-    int kind = __builtin_amdgcn_readfirstlane(kind_of(now, begin));
-    for (int i = begin; i < end; ++i) {
+    int i = begin, tile = tile_of(i), tile1 = tile_of(i + 1), tile2 = tile_of(i + 2);
+    pages_of(now, tile);
+    load_tile(now, tile, i % kRing);
+    pages_of(next, tile1);
+    load_tile(next, tile1, (i + 1) % kRing);
+    pages_of(after, tile2);
+    auto top_of = [&]() {
       am_wait<0>();                                                  // the wavefront's loads of tile i + 1 are there ..
       am_barrier();                                                  // .. and everyone's; and tile i - 2 is no longer read
-      load_tile(after, i + 2);
-#pragma unroll
-      for (int t = 0; t < VT; ++t) asm volatile("" : "+v"(acc[t]));  // (sums stay in their registers whichever way a tile goes,
-      kind = __builtin_amdgcn_readfirstlane(kind);
-      asm volatile("" : "+s"(kind));                                 // and no way has a loop of its own)
-      const int ok = valid(now), then = __builtin_amdgcn_readfirstlane(kind_of(next, i + 1));
+      load_tile(after, tile2, (i + 2) % kRing);
+    };
+    auto advance = [&]() {
+      ++i;
       now = next;
       next = after;
-      pages_of(after, i + 3);
-      if (!CAREFUL && kind >= 2) {
-        const unsigned char* const kt = keys_at(i);
-        if (kind == 3) {
-          step(std::true_type{}, sc[0], sc[1], kt, kread[1], weight[1], keys_at(i - 1) + TILE, 2, weight[0]);
-        } else {
-          scores_alone(sc[0], kt, kread[0]);
-          step(std::false_type{}, sc[0], sc[1], kt, kread[1], weight[1], kt, 0, weight[0]);
+      tile = tile1;
+      tile1 = tile2;
+      tile2 = tile_of(i + 2);
+      pages_of(after, tile2);
+      if (i < end) top_of();
+    };
+    auto keys_at = [&](int i) { return smem + (i % kRing) * 2 * TILE; };
+    top_of();
+    while (i < end) {
+      const int kind = __builtin_amdgcn_readfirstlane(kind_of(now, tile));
+      if (!CAREFUL && kind == kWhole) {
+        const unsigned char* kt = keys_at(i);
+        const unsigned char* vt = kt + TILE;                         // (the first product is with weights of zero)
+        scores_alone(sc[0], kt, kread[0]);
+        weight[1][0] = weight[1][1] = bf16x8{};
+        for (;;) {
+          step(sc[0], sc[1], kt, kread[1], weight[1], vt, 2, weight[0]);
+          vt = kt + TILE;
+          kt = keys_at(i + 1);
+          step(sc[1], sc[0], kt, kread[0], weight[0], vt, 0, weight[1]);
+          const bool more = i + 1 < end && __builtin_amdgcn_readfirstlane(kind_of(next, tile1)) == kWhole;
+          if (!more) break;
+          advance();
         }
-        step(std::true_type{}, sc[1], sc[0], keys_at(i + 1), kread[0], weight[0], kt + TILE, 0, weight[1]);
-        if (then != 2) product_alone(weight[1], kt + TILE, 2);
-      } else if (kind != 0) {
-        work(careful, i, tiles.at(i) * kTile, ok);
+        product_alone(weight[1], vt, 2);
+      } else if (kind != kNothing) {
+        work(careful, keys_at(i), tile * kTile, valid(now));
       }
-      kind = kind >= 2 && then == 2 ? 3 : then;
+      advance();
     }
     am_wait<0>();                                                    // (no load writes to LDS from here on)
   };
