@@ -30,6 +30,10 @@ template <int N> __device__ __forceinline__ void am_wait() {        // vmcnt <= 
   asm volatile("" ::: "memory");
 }
 
+// No score is this low; with it as the origin every weight is infinite.  A step's 16 weights of a lane may sum up to 2^12: a softmax does not depend on its origin,
+// and weights that much larger change no rounding of bf16 or fp32.
+constexpr float kNoOrigin = -1e30f, kMostSum = 4096.f;
+
 template <int D, int PB, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArgs a, int64_t blocks) {
   using Shape = ManyShape<D, NW>;
@@ -115,7 +119,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   for (int i = 0; i < VT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-  float top = -__builtin_inff(), total = 0.f;                        // top: of scaled scores; total: this lane's keys alone
+  float origin = kNoOrigin, total = 0.f;                             // what is taken off scaled scores; total: this lane's keys alone
   const int key = (l32 & 0x13) | (l32 & 4) << 1 | (l32 & 8) >> 1;    // of 32 that the lane reads
   int kread[2];
 #pragma unroll
@@ -125,35 +129,45 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   }
   const int vread = (half * D + l32) * 16;
 
-  // Raises the maximum to that of `most` where some row needs it; returns whether sums have to be scaled by `factor`.
+  // The weights of a step's scores are taken with the origin as it is.  Where their sum says that some score is far above it (or that there is none yet, which
+  // makes every weight infinite), the origin becomes the largest score so far, sums are to be scaled by `factor`, and the weights are taken again.
+  // `seen`: a bit for each of the lane's 16 keys, at the key's place in 24.
+  auto place = [](int e) { return 16 * (e >> 3) + (e & 7); };
+  auto only = [&](float w, uint32_t seen, int e) { return __uint_as_float(__float_as_uint(w) & (uint32_t)((int32_t)(seen << (31 - place(e))) >> 31)); };
+  auto seen_of = [&](int j) {                                        // j: the first of the lane's keys
+    auto first = [](int n) { return (1u << cache_clamp(n, 0, 24)) - 1u; };
+    const int p = p_row - j;
+    return first(p + 1) & (a.window ? ~first(p - a.window + 1) | first(a.sinks - j) : ~0u);
+  };
   float factor = 1.f;
-  auto raise = [&](float most) {
-    if (!__ballot(most > top + kSlack)) return false;
+  auto raise = [&](const f32x16& now, float (&w)[16], float& sum, uint32_t seen) {
+    if (!__ballot(sum > kMostSum)) return false;
+    float most = kUnseen;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) most = fmaxf(most, seen >> place(e) & 1 ? now[e] : kUnseen);
+    most *= scale;
     most = fmaxf(most, __shfl_xor(most, 32));
-    const float now = fmaxf(top, most);
-    factor = at_factor(top, now);
-    top = now;
+    if (most == kUnseen) most = kNoOrigin;
+    const float to = fmaxf(origin, most);
+    factor = origin == kNoOrigin ? 1.f : at_exp2(origin - to);       // (sums without an origin are zero, or NaN)
+    origin = to;
     total *= factor;
+    sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { w[e] = only(at_exp2(fmaf(now[e], scale, -origin)), seen, e); sum += w[e]; }
     return true;
   };
   auto scale_sums = [&]() {
 #pragma unroll
     for (int t = 0; t < VT; ++t) acc[t] *= factor;
   };
-  // The weights of 16 keys and a row for the second product, from the scores of the tile.
-  auto weights = [&](const f32x16& sc, int k, float from) {
-    float w[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      w[e] = at_exp2(fmaf(sc[8 * k + e], scale, -from));
-      total += w[e];
-    }
+  auto pack = [&](const float* w) {
     return __builtin_bit_cast(bf16x8, u32x4{at_bf16x2(w[0], w[1]), at_bf16x2(w[2], w[3]), at_bf16x2(w[4], w[5]), at_bf16x2(w[6], w[7])});
   };
   auto values_at = [&](const unsigned char* vt, int step, int t) { return *reinterpret_cast<const u32x4*>(vt + vread + (step * 2 * D + t * 32) * 16); };
   f32x16 sc[2];                                                      // scores of 32 keys; element e: key 16 (e / 8) + 8 half + e % 8
   bf16x8 weight[2][2];                                               // [step & 1][16 keys]
-  // A tile of which some row sees a part, 32 keys after the other; what is behind the last position that some row sees is taken for zeros.  CAREFUL (see
+  // A tile of which parts are not there, 32 keys after the other; what is behind the last position that some row sees is taken for zeros.  CAREFUL (see
   // attention_marks) takes any tile, and every sum in the same order as where it is not needed.
   auto work = [&](auto careful, const unsigned char* kt, int j0, int ok) {
     constexpr bool CAREFUL = decltype(careful)::value;
@@ -166,26 +180,21 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
 #pragma unroll
       for (int k = 0; k < KS; ++k)
         s32 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + kread[b] + k * (2 * P * 16)), qf[k], s32, 0, 0, 0);
-      const int j = j0 + 32 * b + 8 * half, until = p_row - j, after = a.window ? p_row - a.window - j : -1 << 30, sinks = a.sinks - j;
+      const int j = j0 + 32 * b + 8 * half;
+      const uint32_t seen = seen_of(j) & ((ok >> (2 * b) & 1 ? 0xffu : 0u) | (ok >> (2 * b + 1) & 1 ? 0xff0000u : 0u));
+      float w[16], sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int at = 16 * (e >> 3) + (e & 7);
-        const bool here = (ok >> (2 * b + (e >> 3)) & 1) && at <= until && (at > after || at < sinks);
-        s32[e] = here ? s32[e] : kUnseen;
-      }
-      float most = s32[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) most = fmaxf(most, s32[e]);
-      if (raise(most * scale)) scale_sums();
-      const float from = at_origin(top);
+      for (int e = 0; e < 16; ++e) { w[e] = only(at_exp2(fmaf(s32[e], scale, -origin)), seen, e); sum += w[e]; }
+      if (raise(s32, w, sum, seen)) scale_sums();
+      total += sum;
 #pragma unroll
       for (int h16 = 0; h16 < 2; ++h16) {
-        weight[1][h16] = weights(s32, h16, from);
+        weight[1][h16] = pack(w + 8 * h16);
         u32x4 ones, ends;
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           const int at = 8 * h16 + 2 * h, left = pmax - j - 16 * h16 - 2 * h;      // keys of the lane's pair that are not behind the last
-          ones[h] = (s32[at] != kUnseen ? 0x3f80u : 0u) | (s32[at + 1] != kUnseen ? 0x3f800000u : 0u);
+          if (CAREFUL) ones[h] = (seen >> place(at) & 1 ? 0x3f80u : 0u) | (seen >> place(at + 1) & 1 ? 0x3f800000u : 0u);
           ends[h] = left >= 1 ? ~0u : left == 0 ? 0xffffu : 0u;
         }
 #pragma unroll
@@ -200,7 +209,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
             n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), n, 0, 0, 0);
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[t][e] += attention_strange_sum(n[e]);
-          } else {
+          } else if (j0 + kTile > pmax) {
             v &= ends;
           }
           acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), weight[1][h16], acc[t], 0, 0, 0);
@@ -209,7 +218,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
     }
   };
 
-  // Tiles that all the wavefront's rows see whole go through in steps of 32 keys, each with three parts that do not wait for each other: the next step's scores, this one's
+  // All other tiles go through in steps of 32 keys, each with three parts that do not wait for each other: the next step's scores, this one's
   // weights, and the product of the last one's weights with its values.  So the matrix unit works while the vector unit takes exponentials.  Groups of one
   // instruction of either product, the reads of the group after the next, and the group's share of the weights; the barriers keep the compiler to this order.
   auto scores_alone = [&](f32x16& next, const unsigned char* kt, int from) {
@@ -224,7 +233,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
       acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values_at(vt, step + k / VT, k % VT)), w[k / VT], acc[k % VT], 0, 0, 0);
   };
   auto step = [&](const f32x16& now, f32x16& next, const unsigned char* kt, int kfrom, const bf16x8 (&before)[2], const unsigned char* vt, int vstep,
-                  bf16x8 (&w)[2]) {
+                  bf16x8 (&packed)[2], bool parts_seen, int j) {
     constexpr int AHEAD = 2;
     u32x4 kf[AHEAD + 1], vf[AHEAD + 1];
     auto read = [&](int k) {
@@ -233,12 +242,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
     };
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) read(k);
-    float most = now[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) most = fmaxf(most, now[e]);
-    const bool raised = raise(most * scale);
-    const float from = at_origin(top);
-    float x[16];
+    float w[16], sum = 0.f;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
@@ -247,28 +251,35 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
       next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[k % (AHEAD + 1)]), qf[k], k == 0 ? zero : next, 0, 0, 0);
 #pragma unroll
       for (int e = k * 16 / KS; e < (k + 1) * 16 / KS; ++e) {
-        x[e] = at_exp2(fmaf(now[e], scale, -from));
-        asm volatile("" : "+v"(x[e]));                               // (here, not behind the products)
-        total += x[e];
+        w[e] = at_exp2(fmaf(now[e], scale, -origin));
+        sum += w[e];
+        asm volatile("" : "+v"(w[e]), "+v"(sum));                    // (here, not behind the products)
       }
       acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k % (AHEAD + 1)]), before[k / VT], acc[k % VT], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
+    uint32_t seen = ~0u;
+    if (parts_seen) {
+      seen = seen_of(j);
+      sum = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      w[h] = __builtin_bit_cast(bf16x8, u32x4{at_bf16x2(x[8 * h], x[8 * h + 1]), at_bf16x2(x[8 * h + 2], x[8 * h + 3]), at_bf16x2(x[8 * h + 4], x[8 * h + 5]),
-                                              at_bf16x2(x[8 * h + 6], x[8 * h + 7])});
-    if (raised) scale_sums();
+      for (int e = 0; e < 16; ++e) { w[e] = only(w[e], seen, e); sum += w[e]; }
+    }
+    if (raise(now, w, sum, seen)) scale_sums();
+    total += sum;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) packed[h] = pack(w + 8 * h);
   };
 
   // Tiles of which the wavefront's rows see something are seen_from .. seen_to and those below seen_sinks; tiles that all of them see whole likewise.
   const int seen_to = pmax >> 6, seen_from = a.window ? max(pmin - a.window + 1, 0) >> 6 : 0, seen_sinks = a.window ? (a.sinks + kTile - 1) / kTile : 0;
   const int whole_to = ((pmin + 1) >> 6) - 1, whole_from = a.window ? (max(pmax - a.window + 1, 0) + kTile - 1) >> 6 : 0, whole_sinks = a.window ? a.sinks / kTile : 0;
-  enum { kNothing, kParts, kWhole };
+  enum { kNothing, kOdd, kParts, kWhole };                           // kOdd: some of it is not there, or behind the sequence's end
+  const int end_tile = (seq.before + seq.count) >> 6;
   auto kind_of = [&](const Ids& g, int tile) {
     const bool some = tile <= seen_to && (tile >= seen_from || tile < seen_sinks);
-    const bool all = tile <= whole_to && (tile >= whole_from || tile < whole_sinks) && valid(g) == 15;
-    return idle ? kNothing : all ? kWhole : some ? kParts : kNothing;
+    const bool all = tile <= whole_to && (tile >= whole_from || tile < whole_sinks);
+    return idle || !some ? kNothing : valid(g) != 15 || tile >= end_tile ? kOdd : all ? kWhole : kParts;
   };
   auto pass = [&](auto careful) {
     constexpr bool CAREFUL = decltype(careful)::value;
@@ -297,19 +308,20 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
     auto keys_at = [&](int i) { return smem + (i % kRing) * 2 * TILE; };
     top_of();
     while (i < end) {
-      const int kind = __builtin_amdgcn_readfirstlane(kind_of(now, tile));
-      if (!CAREFUL && kind == kWhole) {
+      int kind = __builtin_amdgcn_readfirstlane(kind_of(now, tile));
+      if (!CAREFUL && kind >= kParts) {
         const unsigned char* kt = keys_at(i);
         const unsigned char* vt = kt + TILE;                         // (the first product is with weights of zero)
         scores_alone(sc[0], kt, kread[0]);
         weight[1][0] = weight[1][1] = bf16x8{};
         for (;;) {
-          step(sc[0], sc[1], kt, kread[1], weight[1], vt, 2, weight[0]);
+          const int j = tile * kTile + 8 * half;
+          step(sc[0], sc[1], kt, kread[1], weight[1], vt, 2, weight[0], kind == kParts, j);
           vt = kt + TILE;
           kt = keys_at(i + 1);
-          step(sc[1], sc[0], kt, kread[0], weight[0], vt, 0, weight[1]);
-          const bool more = i + 1 < end && __builtin_amdgcn_readfirstlane(kind_of(next, tile1)) == kWhole;
-          if (!more) break;
+          step(sc[1], sc[0], kt, kread[0], weight[0], vt, 0, weight[1], kind == kParts, j + 32);
+          kind = i + 1 < end ? __builtin_amdgcn_readfirstlane(kind_of(next, tile1)) : kNothing;
+          if (kind < kParts) break;
           advance();
         }
         product_alone(weight[1], vt, 2);
@@ -332,7 +344,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
       for (int t = 0; t < VT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
-      top = -__builtin_inff();
+      origin = kNoOrigin;
       total = 0.f;
       pass(std::true_type{});
       __syncthreads();
@@ -352,7 +364,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
 #pragma unroll
       for (int e = 0; e < 16; e += 4)
         *reinterpret_cast<f32x4*>(to + 32 * t + 2 * e + 4 * half) = f32x4{acc[t][e], acc[t][e + 1], acc[t][e + 2], acc[t][e + 3]};
-    if (half == 0) { a.stats[call_row * 2] = top; a.stats[call_row * 2 + 1] = total; }
+    if (half == 0) { a.stats[call_row * 2] = origin == kNoOrigin ? -__builtin_inff() : origin; a.stats[call_row * 2 + 1] = total; }
     return;
   }
   // through the wavefront's own rows of LDS, so that a row leaves in one run
