@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgptaq.so")
 SOURCES = ["status.hip", "gemm_bf16.hip", "accumulate.hip", "prepare.hip", "factor_sweep.hip", "quantize.hip", "quantize_sb.hip", "act_order.hip", "upstream.hip", "peaks.hip",
-           "row_ops.hip", "linear.hip", "linear_many.hip", "linear8.hip", "cache.hip", "attention.hip",
+           "row_ops.hip", "linear.hip", "linear_many.hip", "linear8.hip", "linear8_many.hip", "cache.hip", "attention.hip",
            "attention_many.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

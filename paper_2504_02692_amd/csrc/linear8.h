@@ -35,6 +35,12 @@ struct Linear8Args {
   const int8_t* x; const float* xs; int64_t ldx;
   const uint8_t* codes; const float* scales; const int32_t* shifts;
   int32_t tokens, mt, kt;
+  int32_t parts;                       // linear8_many.hip: the columns in so many parts, whose sums (more than one) go to
+  int32_t* partial; int64_t ld_partial;                             // partial[part][token][row]
 };
+
+// linear8_many.hip
+hipError_t launch_linear8_many(Linear8Args p, int32_t* partial, hipStream_t s);
+size_t linear8_partial_bytes(int64_t tokens, int64_t m, int64_t n);
 
 }  // namespace gptaq

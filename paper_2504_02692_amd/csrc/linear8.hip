@@ -183,13 +183,15 @@ static hipError_t launch_few8_as(const Linear8Args& p, int waves, hipStream_t s)
                      (size_t)(waves * kPerWave), s, p);
   return hipGetLastError();
 }
-static hipError_t launch_linear8(const Linear8Args& p, hipStream_t s) {
+static hipError_t launch_linear8(const Linear8Args& p, int32_t* partial, hipStream_t s) {
+  if (p.tokens > 32) return launch_linear8_many(p, partial, s);
   const int waves = p.mt < 512 && p.kt >= 64 ? 16 : 8;
   return p.tokens <= 16 ? launch_few8_as<1, 1>(p, waves, s) : launch_few8_as<1, 2>(p, waves, s);
 }
 
 // ---- argument checks
 
+constexpr int64_t kMaxRow8 = (int64_t)1 << 22;          // bytes between rows: 256 of them take 31 bits of offset
 constexpr int64_t kMaxRows8 = (int64_t)1 << 20, kMaxColumns8 = (int64_t)1 << 16, kMaxTokens8 = (int64_t)1 << 23, kMaxTiles8 = (int64_t)1 << 23;
 static bool good_size8(int64_t m, int64_t n) {
   return m > 0 && n > 0 && m <= kMaxRows8 && n <= kMaxColumns8 && ((m + 15) / 16) * ((n + 127) / 128) <= kMaxTiles8;
@@ -224,7 +226,7 @@ extern "C" int gptaq_linear8_pack(const uint8_t* codes, int64_t ldc, const float
 
 extern "C" size_t gptaq_linear8_workspace_bytes(int64_t tokens, int64_t m, int64_t n) {
   if (tokens <= 0 || tokens > kMaxTokens8 || !good_size8(m, n)) return 0;
-  return aligned_bytes(tokens, n);
+  return aligned_bytes(tokens, n) + (linear8_partial_bytes(tokens, m, n) + 255) / 256 * 256;
 }
 
 extern "C" int gptaq_linear8_i8(const int8_t* X, const float* x_scales, int64_t tokens, int64_t ldx, const void* weights, size_t weights_bytes, int64_t m, int64_t n,
@@ -244,13 +246,14 @@ extern "C" int gptaq_linear8_i8(const int8_t* X, const float* x_scales, int64_t 
   p.x = X; p.xs = x_scales; p.ldx = ldx;
   p.codes = from; p.scales = (const float*)(from + l.scales); p.shifts = (const int32_t*)(from + l.shifts);
   p.mt = (int32_t)l.mt; p.kt = (int32_t)l.kt;
-  if (n % 128 || ldx % 16 || ((uintptr_t)X & 15) || ldx > kManyMaxRow) {
+  if (n % 128 || ldx % 16 || ((uintptr_t)X & 15) || ldx > kMaxRow8) {
     const int64_t ld = l.kt * 128, pieces = tokens * (ld / 16), blocks = (pieces + 255) / 256;
     hipLaunchKernelGGL(linear8_align_kernel, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, s, X, ldx, (int)n, (int8_t*)ws, (int)ld, pieces);
     GPTAQ_LAUNCH_CHECK();
     p.x = (const int8_t*)ws;
     p.ldx = ld;
   }
+  int32_t* const partial = (int32_t*)((uint8_t*)ws + aligned_bytes(tokens, n));
   // A grid has less than 2^32 threads, and 2^16 blocks along its second axis: more tokens than that takes are several launches.
   int64_t most = (((int64_t)1 << 22) / l.mt) * 16;
   if (most > 65535 * 16) most = 65535 * 16;
@@ -260,7 +263,7 @@ extern "C" int gptaq_linear8_i8(const int8_t* X, const float* x_scales, int64_t 
     part.x = p.x + first * p.ldx;
     part.xs = p.xs + first;
     part.out.y = (uint8_t*)Y + first * ldy * (y_f32 ? 4 : 2);
-    if (const hipError_t e = launch_linear8(part, s); e != hipSuccess) { set_last_hip_error(e); return GPTAQ_ELAUNCH; }
+    if (const hipError_t e = launch_linear8(part, partial, s); e != hipSuccess) { set_last_hip_error(e); return GPTAQ_ELAUNCH; }
   }
   return GPTAQ_OK;
 }
