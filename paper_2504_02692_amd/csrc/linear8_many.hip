@@ -61,24 +61,28 @@ __global__ __launch_bounds__(64 * WT * WR, 2) void linear8_many_kernel(Linear8Ar
 #pragma unroll
     for (int j = 0; j < NL; ++j) xfrom.load(smem + k % kX8Ring * Tile::kStage + (wave * NL + j) * 1024, xsrc[j], from);
   };
-  const int foff = (wt * TT * 32 + l32) * 128 + ((half ^ swizzle(l32)) << 4);
+  int foff[4];                                            // of the steps
+#pragma unroll
+  for (int s = 0; s < 4; ++s) foff[s] = (wt * TT * 32 + l32) * 128 + ((((half ^ swizzle(l32)) << 4)) ^ (s << 5));
   u32x4 xf[2][TT];                                        // [step & 1][tile of 32 tokens]
   auto read_x = [&](int stage, int s, int i) {
-    xf[s & 1][i] = *reinterpret_cast<const u32x4*>(smem + ((stage % kX8Ring * Tile::kStage + foff) ^ (s << 5)) + i * 32 * 128);
+    xf[s & 1][i] = *reinterpret_cast<const u32x4*>(smem + stage % kX8Ring * Tile::kStage + foff[s] + i * 32 * 128);
   };
   // ---- weights: lane l has row l % 32 of 32; step s has chunks 2 s and 2 s + 1 of the stage's eight
-  const uint8_t* codes[RT];
+  // (Buffer loads: the place in the row is a scalar.)
+  const int tr0 = row0 / 16;
+  const __amdgpu_buffer_rsrc_t codes = __builtin_amdgcn_make_buffer_rsrc((void*)(p.codes + (int64_t)tr0 * p.kt * 2048), 0, 0x7fffffff, 0x00020000);
+  int wsrc[RT];
 #pragma unroll
   for (int j = 0; j < RT; ++j) {
-    int tr = row0 / 16 + (wr * RT + j) * 2 + (l32 >> 4);
-    tr = tr < p.mt ? tr : p.mt - 1;
-    codes[j] = p.codes + (int64_t)tr * p.kt * 2048 + half * 256 + l16 * 16;
+    const int tr = (wr * RT + j) * 2 + (l32 >> 4);
+    wsrc[j] = (tr0 + tr < p.mt ? tr : p.mt - 1 - tr0) * p.kt * 2048 + half * 256 + l16 * 16;
   }
   struct Codes { u32x4 w[4][RT]; };
   auto load_w = [&](Codes& c, int k, int s) {
-    k = k < k_end ? k : k_end - 1;
+    const int from = (k < k_end ? k : k_end - 1) * 2048 + s * 512;
 #pragma unroll
-    for (int j = 0; j < RT; ++j) c.w[s][j] = *reinterpret_cast<const u32x4*>(codes[j] + (int64_t)k * 2048 + s * 512);
+    for (int j = 0; j < RT; ++j) c.w[s][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(codes, wsrc[j], from, 0));
   };
 
   i32x16 acc[RT][TT];
@@ -91,7 +95,7 @@ __global__ __launch_bounds__(64 * WT * WR, 2) void linear8_many_kernel(Linear8Ar
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[j][i][e] = 0;
   }
-  // Behind each fragment's matrix instructions: the same fragment of the next step; behind a step's, its weights of the stage after the next.
+  // (The dot products are written out: the compiler would take all, and keep one of WR.)  Behind each fragment's matrix instructions: the same fragment of the next step; behind a step's, its weights of the stage after the next.
   auto stage = [&](Codes& c, int k) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -102,7 +106,7 @@ __global__ __launch_bounds__(64 * WT * WR, 2) void linear8_many_kernel(Linear8Ar
           acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, c.w[s][j]), __builtin_bit_cast(i32x4, xf[s & 1][i]), acc[j][i], 0, 0, 0);
         if (s % WR == wr) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sums[i] = __builtin_amdgcn_sdot4((int)xf[s & 1][i][e], 0x01010101, sums[i], false);
+          for (int e = 0; e < 4; ++e) asm volatile("v_dot4_i32_i8 %0, %1, %2, %0" : "+v"(sums[i]) : "v"(xf[s & 1][i][e]), "s"(0x01010101));
         }
         __builtin_amdgcn_sched_barrier(0);
         if (s < 3) read_x(k, s + 1, i);
