@@ -183,10 +183,18 @@ static hipError_t launch_few8_as(const Linear8Args& p, int waves, hipStream_t s)
                      (size_t)(waves * kPerWave), s, p);
   return hipGetLastError();
 }
+// Two tiles of rows a workgroup, which read the activations half as often, where enough workgroups are left: us a call, one / two, 32 tokens a block: 28672 x 8192, 17 tokens 56.7 /
+// 53.6; 4096 x 4096, 64 8.3 / 7.2, 128 13.4 / 10.1; 4096 x 11008, 64 19.8 / 13.0, 128 36.2 / 20.3; 4096 x 1024, 128 5.7 / 4.9; but 1024 x 8192, 128 7.6 / 9.1 and 11008 x 4096, 32 11.3 /
+// 12.0 (344 workgroups).
+// Blocks of 32 tokens as far as they are few and small; more go to the tiles of linear8_many.hip: us a call, this / that: 4096 x 4096, 128 tokens 10.1 / 16.5, 257 24.4 / 17.1;
+// 4096 x 11008, 64 13.0 / 16.6, 96 19.7 / 19.9, 128 20.3 / 21.3; 28672 x 8192, 33 84 / 54; 11008 x 4096, 64 16.1 / 16.4, 96 22.7 / 17.1; 4096 x 1024, 128 4.9 / 7.6; 1024 x 8192, 257
+// 15.8 / 16.4.
 static hipError_t launch_linear8(const Linear8Args& p, int32_t* partial, hipStream_t s) {
-  if (p.tokens > 32) return launch_linear8_many(p, partial, s);
+  const int64_t blocks = (p.tokens + 31) / 32, workgroups = blocks * p.mt;
+  if (blocks > 1 && (workgroups > 2048 || workgroups * p.kt > 57344)) return launch_linear8_many(p, partial, s);
   const int waves = p.mt < 512 && p.kt >= 64 ? 16 : 8;
-  return p.tokens <= 16 ? launch_few8_as<1, 1>(p, waves, s) : launch_few8_as<1, 2>(p, waves, s);
+  if (p.tokens <= 16) return launch_few8_as<1, 1>(p, waves, s);
+  return workgroups >= 512 && (blocks > 1 || p.mt >= 1024) ? launch_few8_as<2, 2>(p, 8, s) : launch_few8_as<1, 2>(p, waves, s);
 }
 
 // ---- argument checks

@@ -235,29 +235,39 @@ template <int TT, int RT, int WT, int WR> static hipError_t launch_many8_as(cons
   return hipGetLastError();
 }
 
-// Tile of a call: 0: 64 x 128, 1: 128 x 128, 2: 256 x 256; and the parts that its columns are taken in.
+// Tile of a call, 64 x 128, 128 x 128 or 256 x 256, and the parts that the columns of the smallest are taken in.  The rule is the least of what the calls were measured to
+// take, us: a stage of the smaller tiles takes 0.5 and 0.7 while every CU has one at most, and 0.37 and 0.69 for each 256 tiles from there on, more where a few CUs
+// have one more than the others; one of the largest 1.6 while half of the CUs have one, and 1.9 for each round of 256; parts save stages, and cost a launch and their sums' way through memory; and the weights are read at
+// 5 TB/s at best.  us a call, 64 x 128 / 128 x 128 / 256 x 256, one part: 4096 x 4096, 512 tokens 18.5 / 24.7 / 51.9, 2048 46.7 / 42.9 / 56.2, 4096 91.6 / 82.4 / 70.0;
+// 28672 x 8192, 257 122 / 121 / 121, 512 179 / 168 / 132, 2048 615 / 545 / 465; 11008 x 4096, 257 22.9 / 33.5 / 52.3, 1500 94 / 95 / 112, 4096 255 / 225 / 193.  One part /
+// parts: 4096 x 11008, 33 tokens 34.0 / 16.3 (5), 257 35.6 / 29.7 (3), 512 38.7 / 41.7 (2); 1024 x 8192, 257 27.1 / 16.4 (4), 2048 29.8 / 34.5 (2); 4096 x 4096, 257 17.1 / 23.2 (3).
 struct Many8Plan { int tile; int64_t parts; };
-static constexpr int64_t kTileTokens[3] = {64, 128, 256}, kTileRows[3] = {128, 128, 256}, kRoom[3] = {512, 512, 256};
+static constexpr int64_t kTileTokens[3] = {64, 128, 256}, kTileRows[3] = {128, 128, 256}, kRoom = 512;
 static int64_t tiles_of(int tile, int64_t tokens, int64_t m) {
   return (tokens + kTileTokens[tile] - 1) / kTileTokens[tile] * ((m + kTileRows[tile] - 1) / kTileRows[tile]);
 }
 static int64_t most_parts8(int64_t n) { return (n + 127) / 128 / 4; }       // of at least four stages each
 static Many8Plan many8_plan(int64_t tokens, int64_t m, int64_t n) {
-  const int tile = tokens <= 64 || tiles_of(1, tokens, m) < 256 ? 0 : tiles_of(2, tokens, m) < 256 ? 1 : 2;
-  const int64_t most = most_parts8(n), want = kRoom[tile] / tiles_of(tile, tokens, m), parts = want < most ? want : most;
-  return Many8Plan{tile, parts < 1 ? 1 : parts};
-}
-// Room for the partial sums of every call with at most so many tokens: parts times tiles of tokens is at most room / tiles of rows, and parts at most so many.
-size_t linear8_partial_bytes(int64_t tokens, int64_t m, int64_t n) {
-  const int64_t ld = (m + 7) / 8 * 8;
-  if (most_parts8(n) < 2) return 0;
-  int64_t rows = 0;                                       // of ld values
-  for (int tile = 0; tile < 3; ++tile) {
-    const int64_t each = kRoom[tile] / ((m + kTileRows[tile] - 1) / kTileRows[tile]);
-    if (each < 2) continue;
-    const int64_t need = each * kTileTokens[tile] < most_parts8(n) * tokens ? each * kTileTokens[tile] : most_parts8(n) * tokens;
-    rows = need > rows ? need : rows;
+  const double kt = (double)((n + 127) / 128), t0 = (double)tiles_of(0, tokens, m) / 256, t1 = (double)tiles_of(1, tokens, m) / 256;
+  const int64_t t2 = tiles_of(2, tokens, m);
+  auto greater = [](double a, double b) { return a > b ? a : b; };
+  Many8Plan plan{0, 1};
+  double least = kt * (t0 <= 2 ? greater(0.5, 0.38 * t0) : greater(1.0, 0.37 * t0));
+  if (const double us = kt * (t1 <= 1 ? 0.7 : greater(1.15, 0.69 * t1)); us < least) { least = us; plan.tile = 1; }
+  if (const double us = kt * (t2 <= 128 ? 1.6 : 1.9 * (double)((t2 + 255) / 256)); us < least) { least = us; plan.tile = 2; }
+  const double read = (double)m * (double)n / 5e6;
+  least = greater(least, read);
+  for (int64_t parts = 2; parts <= most_parts8(n) && parts * tiles_of(0, tokens, m) <= kRoom; ++parts) {
+    const double us = greater(read, kt / (double)parts * greater(0.5, 0.36 * t0 * (double)parts)) + 4 + (double)(parts * tokens * m) * 8 / 2.5e6;
+    if (us < least) { least = us; plan = Many8Plan{0, parts}; }
   }
+  return plan;
+}
+// Room for the partial sums of every call with at most so many tokens: parts times tiles is at most kRoom, and parts at most so many.
+size_t linear8_partial_bytes(int64_t tokens, int64_t m, int64_t n) {
+  const int64_t ld = (m + 7) / 8 * 8, each = kRoom / ((m + kTileRows[0] - 1) / kTileRows[0]);
+  if (most_parts8(n) < 2 || each < 2) return 0;
+  const int64_t rows = each * kTileTokens[0] < most_parts8(n) * tokens ? each * kTileTokens[0] : most_parts8(n) * tokens;      // of ld values
   return (size_t)(rows * ld) * 4;
 }
 hipError_t launch_linear8_many(Linear8Args p, int32_t* partial, hipStream_t s) {
