@@ -216,20 +216,35 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
   const int last = min(row0 + (1 << a.rows_bits) - 1, rows_seq - 1);
   const Parts parts = attention_parts(a, attention_tiles(a, seq.before + row0 / c.group, seq.before + last / c.group).count);
   if (parts.count <= 1) return;
-  float m = -__builtin_inff();
-  for (int i = 0; i < parts.count; ++i) m = fmaxf(m, a.stats[(i * rows + row) * 2]);
-  float sum = 0.f, o[D / 64 + 1];
+  // a lane has the statistics of a part (there are 64 at most), and all lanes a share of every part's sums, eight parts at a time
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  f32x2 st = {-__builtin_inff(), 0.f};
+  if (lane < parts.count) st = *reinterpret_cast<const f32x2*>(a.stats + (lane * rows + row) * 2);
+  float m = st[0];
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
+  const float mine = lane < parts.count ? at_factor(st[0], m) : 0.f;
+  float sum = mine * st[1];
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
   constexpr int N = (D + 63) / 64;
+  float o[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) o[k] = 0.f;
-  for (int i = 0; i < parts.count; ++i) {
-    const float* st = a.stats + (i * rows + row) * 2;
-    const float factor = at_factor(st[0], m);
-    sum += factor * st[1];
-    const float* from = a.partial + (i * rows + row) * D;
+  const float* const from = a.partial + row * D + lane;
+  for (int i0 = 0; i0 < parts.count; i0 += 8) {
+    float v[8][N];
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (D % 64 == 0 || k * 64 + lane < D) o[k] += factor * from[k * 64 + lane];
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[i][k] = i0 + i < parts.count && (D % 64 == 0 || k * 64 + lane < D) ? from[(i0 + i) * rows * D + k * 64] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float factor = __shfl(mine, i0 + i);
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (i0 + i < parts.count) o[k] += factor * v[i][k];
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   uint16_t* const to = a.out + (int64_t)token * a.ldo + (int64_t)h * a.ho;
@@ -241,14 +256,21 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
 constexpr int64_t kMostParts = 64, kFewBits = 4, kPartialRows = 65536;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
-struct Plan { int bits; int64_t parts; };
-// Rows of a block, and parts of the keys: blocks of few rows for eight workgroups a CU, of many rows for one a CU, if the keys last.
-static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads) {
+struct Plan { int bits; int64_t parts; int min_tiles; };
+// Rows of a block, and parts of the keys.  Blocks of many rows: for a workgroup a CU, of 8 tiles at least.  Blocks of few rows: for two a CU, of 4 tiles at least, or, which
+// evens sequences of different lengths out, for eight a CU of 32 tiles at least.  us a call, room for 512 / 1024 / 2048 workgroups of 4 tiles: 64 heads over 8 of 128, 64
+// sequences of up to 1000 positions 30.0 / 35.5 / 43.7 (those that find nothing to do take a microsecond, too), of up to 8191 245 / 241 / 234; 8 heads, 8 of up to 16000
+// 70.8 / 73.7 / 73.4.  Tiles at least, 2 / 4 / 9: 32 heads, one sequence of 200 8.1 / 5.8 / 7.5, a window of 1024 11.4 / 10.7 / 12.9; 64 over 8, 8000 18.4 / 16.0 / 15.4.
+static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t most_tiles) {
   const int64_t group = heads / kv_heads;
   const bool many = tokens * group > 32 * seqs;
   const int bits = many ? kManyBits : kFewBits;
-  const int64_t full = ((tokens * group - 1) >> bits) + 1, blocks = (full > seqs ? full : seqs) * kv_heads, parts = (many ? 256 : 2048) / blocks;
-  return Plan{bits, parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts};
+  const int64_t full = ((tokens * group - 1) >> bits) + 1, blocks = (full > seqs ? full : seqs) * kv_heads, min_tiles = many ? 8 : 4;
+  int64_t parts = (many ? 256 : 512) / blocks, even = 2048 / blocks;
+  if (parts > (most_tiles + min_tiles - 1) / min_tiles) parts = (most_tiles + min_tiles - 1) / min_tiles;
+  if (even > most_tiles / 32) even = most_tiles / 32;
+  if (!many && parts < even) parts = even;
+  return Plan{bits, parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts, (int)min_tiles};
 }
 // Room for the parts' sums: parts times blocks times their rows is 65536 at most.  (More tokens never take less, so a workspace serves all smaller calls.)
 static int64_t partial_rows(int64_t tokens, int64_t heads) { return kMostParts * tokens * heads < kPartialRows ? kMostParts * tokens * heads : kPartialRows; }
@@ -310,10 +332,13 @@ extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const
   a.scale = scale == 0.f ? 0x1p-126f : scale * 1.4426950408889634f;  // (0 times the minus infinity of a key that is not seen is NaN; 2^-126 gives the same weights)
   a.window = (int32_t)(window < kFar ? window : 0);
   a.sinks = (int32_t)(sinks < kFar ? sinks : kFar);
-  const Plan plan = attention_plan(tokens, seqs, heads, kv_heads);
+  // Tiles that a row can see: those of the table, or of the window (which begins and ends inside a tile, as the block's other rows have theirs) and the sinks.
+  int64_t most_tiles = (table_pages * page + kTile - 1) / kTile;
+  if (a.window && a.window / kTile + a.sinks / kTile + 4 < most_tiles) most_tiles = a.window / kTile + a.sinks / kTile + 4;
+  const Plan plan = attention_plan(tokens, seqs, heads, kv_heads, most_tiles);
   a.rows_bits = plan.bits;
   a.parts = (int32_t)plan.parts;
-  a.min_tiles = plan.bits == kManyBits ? 8 : 2;
+  a.min_tiles = plan.min_tiles;
   a.partial = (float*)ws;
   a.stats = a.partial + (int64_t)a.parts * tokens * heads * d;
   if (pages == 0) a.c.table_pages = 0;                                // no key anywhere: zeros
