@@ -724,39 +724,39 @@ def gptaq_quant_activations_i8(X: torch.Tensor, clip: float = 1.0):
 
 # ---- the cache and attention
 
-def _need_heads(t: torch.Tensor, name: str):
-    """(address, stride of tokens, stride of heads) of a (tokens x heads x d) bf16 tensor."""
-    if t.dtype is not torch.bfloat16 or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
-        raise GptaqError(f"{name}: expected a (tokens, heads, d) bfloat16 CUDA tensor with adjacent entries")
-    tokens, heads, d = t.shape
-    return t.data_ptr(), t.stride(0) if tokens > 1 else heads * t.stride(1) if heads > 1 else d, t.stride(1) if heads > 1 else d
+def _need_heads(t: torch.Tensor, shape, name: str):
+    """(address, stride of tokens, stride of heads) of a (tokens x heads x d) bf16 tensor of that shape."""
+    stride = t.stride()
+    if t.dtype is not torch.bfloat16 or len(stride) != 3 or t.shape != shape or (stride[2] != 1 and shape[2] != 1):
+        raise GptaqError(f"{name}: expected bfloat16 ({', '.join(map(str, shape))}) with adjacent entries")
+    tokens, heads, d = shape                             # (of one token or head alone torch may give any stride)
+    head = stride[1] if heads > 1 else d
+    return t.data_ptr(), stride[0] if tokens > 1 else heads * head, head
 
 
 def _cache_args(keys: torch.Tensor, values: torch.Tensor, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, d: int, name: str):
     """The cache's arguments as the C calls take them: (keys, values, pages, page, table, ld_table, table_pages, starts, lengths, seqs), and kv_heads."""
-    if keys.dtype is not torch.bfloat16 or keys.dim() != 5 or not keys.is_contiguous() or keys.shape[2] * 8 != d or keys.shape[4] != 8:
+    shape, seqs, width, bf16, int32 = keys.shape, lengths.numel(), table.shape[-1], torch.bfloat16, torch.int32
+    if keys.dtype is not bf16 or len(shape) != 5 or shape[2] * 8 != d or shape[4] != 8 or not keys.is_contiguous():
         raise GptaqError(f"{name}: keys: expected contiguous bfloat16 (pages, kv_heads, {d} / 8, page, 8)")
-    pages, kv_heads, _, page, _ = keys.shape
-    if values.dtype is not torch.bfloat16 or values.shape != (pages, kv_heads, page // 8, d, 8) or not values.is_contiguous():
+    pages, kv_heads, _, page, _ = shape
+    if values.dtype is not bf16 or values.shape != (pages, kv_heads, page // 8, d, 8) or not values.is_contiguous():
         raise GptaqError(f"{name}: values: expected contiguous bfloat16 ({pages}, {kv_heads}, {page} / 8, {d}, 8)")
-    if lengths.dtype is not torch.int32 or lengths.dim() != 1 or not lengths.is_contiguous():
+    if lengths.dtype is not int32 or lengths.dim() != 1 or not lengths.is_contiguous():
         raise GptaqError(f"{name}: lengths: expected a contiguous int32 vector")
-    seqs = lengths.shape[0]
-    if starts.dtype is not torch.int32 or starts.shape != (seqs + 1,) or not starts.is_contiguous():
+    if starts.dtype is not int32 or starts.dim() != 1 or starts.numel() != seqs + 1 or not starts.is_contiguous():
         raise GptaqError(f"{name}: starts: expected {seqs + 1} contiguous int32")
-    if table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != seqs or (table.shape[1] > 1 and table.stride(1) != 1):
+    if table.dtype is not int32 or table.shape != (seqs, width) or (width > 1 and table.stride(1) != 1):
         raise GptaqError(f"{name}: table: expected a row-major int32 tensor with a row for each of {seqs} sequences")
-    width = table.shape[1]
     return (keys.data_ptr(), values.data_ptr(), pages, page, table.data_ptr(), table.stride(0) if seqs > 1 else width, width, starts.data_ptr(),
             lengths.data_ptr(), seqs), kv_heads
 
 
-def _heads_out(q: torch.Tensor, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
-    if out is None:
-        return torch.empty_like(q, memory_format=torch.contiguous_format)
-    if out.shape != q.shape:
-        raise GptaqError(f"{name}: out: shape mismatch")
-    return out
+def _heads_of(q: torch.Tensor, name: str):
+    shape = q.shape
+    if len(shape) != 3:
+        raise GptaqError(f"{name}: q: expected (tokens, heads, d)")
+    return shape
 
 
 def gptaq_cache_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, table: torch.Tensor,
@@ -766,19 +766,19 @@ def gptaq_cache_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, keys: 
     itself).  q, k, v: (tokens, heads, d), for instance parts of one product's rows; sequence s has rows starts[s] .. starts[s + 1] - 1, its
     lengths[s] count them.  freqs: float64, the angle per position of each rotated pair (None: no rotation)."""
     device = _here(q, k, v, keys, values, table, starts, lengths, freqs, out)
-    qp, kp, vp = _need_heads(q, "q"), _need_heads(k, "k"), _need_heads(v, "v")
-    tokens, heads, d = q.shape
+    shape = _heads_of(q, "gptaq_cache_append")
+    tokens, heads, d = shape
     cache, kv_heads = _cache_args(keys, values, table, starts, lengths, d, "gptaq_cache_append")
-    if k.shape != (tokens, kv_heads, d) or v.shape != (tokens, kv_heads, d):
-        raise GptaqError(f"gptaq_cache_append: k, v: expected ({tokens}, {kv_heads}, {d})")
+    kv_shape = (tokens, kv_heads, d)
     pairs = 0
     if freqs is not None:
         if freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
             raise GptaqError("gptaq_cache_append: freqs: expected a contiguous float64 vector")
-        pairs = freqs.shape[0]
-    out = _heads_out(q, out, "gptaq_cache_append")
-    _check(load().gptaq_cache_append(*qp, *kp, *vp, *cache, tokens, heads, kv_heads, d, _ptr(freqs), pairs, bool(interleaved), *_need_heads(out, "out"),
-                                     _stream(device)), "gptaq_cache_append")
+        pairs = freqs.numel()
+    if out is None:
+        out = q.new_empty(shape)
+    _check(load().gptaq_cache_append(*_need_heads(q, shape, "q"), *_need_heads(k, kv_shape, "k"), *_need_heads(v, kv_shape, "v"), *cache, tokens, heads, kv_heads, d,
+                                     _ptr(freqs), pairs, bool(interleaved), *_need_heads(out, shape, "out"), _stream(device)), "gptaq_cache_append")
     return out
 
 
@@ -791,10 +791,12 @@ def gptaq_attention(q: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, t
     """Causal attention of new tokens' queries (tokens, heads, d) over the cache, which holds their own keys and values already.  window: positions a
     token sees, itself among them (0: all); sinks: first positions that stay visible.  scale: 1 / sqrt(d) if not given."""
     device = _here(q, keys, values, table, starts, lengths, out)
-    qp = _need_heads(q, "q")
-    tokens, heads, d = q.shape
+    shape = _heads_of(q, "gptaq_attention")
+    tokens, heads, d = shape
     cache, kv_heads = _cache_args(keys, values, table, starts, lengths, d, "gptaq_attention")
-    out = _heads_out(q, out, "gptaq_attention")
-    _check(load().gptaq_attention(*qp, *cache, tokens, heads, kv_heads, d, int(window), int(sinks), d ** -0.5 if scale is None else float(scale),
-                                  *_need_heads(out, "out"), _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_attention")
+    if out is None:
+        out = q.new_empty(shape)
+    _check(load().gptaq_attention(*_need_heads(q, shape, "q"), *cache, tokens, heads, kv_heads, d, int(window), int(sinks),
+                                  d ** -0.5 if scale is None else float(scale), *_need_heads(out, shape, "out"), _ws(ws, device), ws.nbytes, _stream(device)),
+           "gptaq_attention")
     return out

@@ -32,28 +32,40 @@ def solve(W: torch.Tensor, X: torch.Tensor, Xtilde: torch.Tensor, bits: int, gro
     Q = B.gptaq_permute_columns_f32(W, perm) if act_order else W.clone()
     dead, info = B.gptaq_prepare(H, A, damp, B.workspace(B.gptaq_prepare_workspace_bytes(n)))
     codes, scales, zeros = B.gptaq_quantize_layer(Q, H, A, bits, group, False, 128, B.workspace(B.gptaq_quantize_workspace_bytes(m, n)), dead=dead)
-    weights = B.gptaq_linear_pack(codes, scales, zeros, group, perm=perm)
+    if bits > 4:                                         # (one scale and zero a row)
+        weights = B.gptaq_linear8_pack(codes, scales, zeros, perm=perm)
+    else:
+        weights = B.gptaq_linear_pack(codes, scales, zeros, group, perm=perm)
     if info[0].item() != 0 or weights.info.item() != 0:
         raise RuntimeError(f"solve failed: info {info.tolist()}, {weights.info.tolist()}")
     return weights, B.gptaq_permute_columns_f32(Q, perm, inverse=True) if act_order else Q
 
 
+def product(codes: torch.Tensor, scales: torch.Tensor, weights, ws: torch.Tensor) -> torch.Tensor:
+    """The product of 8-bit activations with a layer of either kind."""
+    return (B.gptaq_linear8_i8 if isinstance(weights, B.Linear8Weights) else B.gptaq_linear_i8)(codes, scales, weights, ws)
+
+
+def product_workspace_bytes(tokens: int, weights) -> int:
+    return (B.gptaq_linear8_workspace_bytes if isinstance(weights, B.Linear8Weights) else B.gptaq_linear_workspace_bytes)(tokens, weights.m, weights.n)
+
+
 class QuantizedMLP(NamedTuple):
     norm: torch.Tensor                           # bf16
-    gate_up: B.LinearWeights                     # gate's rows, then up's
-    down: B.LinearWeights
+    gate_up: "B.LinearWeights | B.Linear8Weights"      # gate's rows, then up's
+    down: "B.LinearWeights | B.Linear8Weights"
 
     def workspace(self, tokens: int) -> torch.Tensor:
-        return B.workspace(max(B.gptaq_linear_workspace_bytes(tokens, w.m, w.n) for w in (self.gate_up, self.down)))
+        return B.workspace(max(product_workspace_bytes(tokens, w) for w in (self.gate_up, self.down)))
 
     def __call__(self, x: torch.Tensor, residual: torch.Tensor, ws: torch.Tensor, eight_bits: bool = True):
-        """(the MLP's output, x + residual) for bf16 tokens; the caller adds them at its next norm."""
+        """(the MLP's output, x + residual) for bf16 tokens; the caller adds them at its next norm.  Layers of more than 4 bits take 8-bit activations."""
         inner = self.down.n
         if eight_bits:
             codes, scales, total = B.gptaq_rms_norm_i8(x, self.norm, EPS, residual=residual)
-            both = B.gptaq_linear_i8(codes, scales, self.gate_up, ws)
+            both = product(codes, scales, self.gate_up, ws)
             codes, scales = B.gptaq_silu_mul_i8(both[:, :inner], both[:, inner:])
-            return B.gptaq_linear_i8(codes, scales, self.down, ws), total
+            return product(codes, scales, self.down, ws), total
         h, total = B.gptaq_rms_norm(x, self.norm, EPS, residual=residual)
         both = B.gptaq_linear(h, self.gate_up, ws)
         return B.gptaq_linear(B.gptaq_silu_mul(both[:, :inner], both[:, inner:]), self.down, ws), total
@@ -81,7 +93,8 @@ def calibrate(hidden: int, inner: int, tokens: int, bits: int = 4, group: int = 
     # second input: of the full model, and of the one whose gate and up are quantised
     gate, up = torch.matmul(h.float(), gate_up.t()).to(torch.bfloat16).chunk(2, 1)
     full_input = B.gptaq_silu_mul(gate, up)
-    both = B.gptaq_linear(h, packed, B.workspace(B.gptaq_linear_workspace_bytes(tokens, packed.m, packed.n)))
+    ws = B.workspace(product_workspace_bytes(tokens, packed))
+    both = product(*B.gptaq_quant_activations_i8(h), packed, ws) if bits > 4 else B.gptaq_linear(h, packed, ws)
     here = B.gptaq_silu_mul(both[:, :inner], both[:, inner:])
     packed_down, down_q = solve(down, here, full_input, bits, group, act_order)
     return QuantizedMLP(norm, packed, packed_down), (gate_up, down), (gate_up_q, down_q)
@@ -92,16 +105,18 @@ def main() -> None:
     ap.add_argument("--hidden", type=int, default=4096)
     ap.add_argument("--inner", type=int, default=11008)
     ap.add_argument("--tokens", type=int, default=32768, help="calibration tokens")
-    ap.add_argument("--bits", type=int, default=4, choices=(2, 3, 4))
-    ap.add_argument("--group", type=int, default=128, choices=(0, 32, 64, 128))
+    ap.add_argument("--bits", type=int, default=4, choices=(2, 3, 4, 5, 6, 7, 8))
+    ap.add_argument("--group", type=int, default=128, choices=(0, 32, 64, 128), help="columns per scale (0: one a row, as layers of more than 4 bits have)")
     ap.add_argument("--act-order", action="store_true")
     a = ap.parse_args()
+    if a.bits > 4:
+        a.group = 0
     mlp, (gate_up, down), _ = calibrate(a.hidden, a.inner, a.tokens, a.bits, a.group, a.act_order)
     for tokens in (1, 16, 512, 2048):
         x, residual = (torch.randn((tokens, a.hidden), device="cuda").to(torch.bfloat16) for _ in range(2))
         ws = mlp.workspace(tokens)
         want = full_precision(x, residual, mlp.norm, gate_up, down)
-        for eight_bits in (True, False):
+        for eight_bits in (True,) if a.bits > 4 else (True, False):
             y, _ = mlp(x, residual, ws, eight_bits)
             torch.cuda.synchronize()
             began = time.perf_counter()
