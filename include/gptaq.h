@@ -366,7 +366,7 @@ int gptaq_quant_activations_i8(const uint16_t* X, int64_t tokens, int64_t n, int
  *   values[id][head][p % page / 8][e][p % 8], with id = table[s][p / page].
  *   table  : (seqs x table_pages) int32, leading dimension ld_table: the pages of each sequence in order; those behind its length are not looked at.  An entry
  *            outside 0 .. pages - 1 stands for a page that is not there (given back, for instance): nothing is written to it, and no token sees its positions.
- *   starts : seqs + 1 int32, ascending: the new tokens of sequence s are rows starts[s] .. starts[s + 1] - 1 of q, k, v and out.  A sequence may have none.
+ *   starts : seqs + 1 int32 (seqs at most 65536), ascending: the new tokens of sequence s are rows starts[s] .. starts[s + 1] - 1 of q, k, v and out.  A sequence may have none.
  *            Rows of no sequence are neither read nor written.
  *   lengths: seqs int32: tokens of each sequence with the new ones; token i of count new ones has position lengths[s] - count + i.  Tokens with a
  *            position below 0 or beyond the table are not written to the cache, and those below 0 see nothing.

@@ -11,7 +11,7 @@ namespace gptaq {
 // 4 a + i of the first product's tile T has key 8 a + 4 T + i.  The four wavefronts of a block take 32 keys each in turn and join through LDS.
 // Weights are rounded to bf16 for the second product (2^-9 each, as the output is once more); their sum is taken of the fp32 values.
 template <int D>
-__global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) {
   constexpr int KS = D / 32, VT = D / 16, PAD = D + 4;
   __shared__ __attribute__((aligned(16))) float joined[4][16][PAD];
   __shared__ float maxima[4][16], sums[4][16];
@@ -256,6 +256,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
 constexpr int64_t kMostParts = 64, kFewBits = 4, kPartialRows = 65536;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
+// Rows of a sequence, on average, up to which blocks are of few: us a call of few / many, 32 heads over 2000 positions, 32 rows 13.6 / 21.8, 64 16.2 / 23.1, 128 22.1 /
+// 27.4, 512 50.8 / 47.2; 64 heads over 8, four sequences over 4000, 64 21.8 / 25.2, 128 31.8 / 30.2, 512 93 / 59; 32 over 8, sixteen over 2000, 64 29.3 / 37.5, 128 49.7 / 45.5, 512 162 / 79.
+constexpr int64_t kFewRows = 96;
 struct Plan { int bits; int64_t parts; int min_tiles; };
 // Rows of a block, and parts of the keys.  Blocks of many rows: for a workgroup a CU, of 8 tiles at least.  Blocks of few rows: for two a CU, of 4 tiles at least, or, which
 // evens sequences of different lengths out, for eight a CU of 32 tiles at least.  us a call, room for 512 / 1024 / 2048 workgroups of 4 tiles: 64 heads over 8 of 128, 64
@@ -263,7 +266,7 @@ struct Plan { int bits; int64_t parts; int min_tiles; };
 // 70.8 / 73.7 / 73.4.  Tiles at least, 2 / 4 / 9: 32 heads, one sequence of 200 8.1 / 5.8 / 7.5, a window of 1024 11.4 / 10.7 / 12.9; 64 over 8, 8000 18.4 / 16.0 / 15.4.
 static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t most_tiles) {
   const int64_t group = heads / kv_heads;
-  const bool many = tokens * group > 32 * seqs;
+  const bool many = tokens * group > kFewRows * seqs;
   const int bits = many ? kManyBits : kFewBits;
   const int64_t full = ((tokens * group - 1) >> bits) + 1, blocks = (full > seqs ? full : seqs) * kv_heads, min_tiles = many ? 8 : 4;
   int64_t parts = (many ? 256 : 512) / blocks, even = 2048 / blocks;
@@ -299,7 +302,7 @@ static hipError_t launch_attention(const AttentionArgs& all, hipStream_t s) {
 }
 
 static bool attention_size(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t d) {
-  return tokens >= 0 && tokens <= (1 << 24) && seqs >= 0 && seqs <= (1 << 20) && heads > 0 && heads <= 4096 && tokens * heads <= (1 << 30) && kv_heads > 0 && heads % kv_heads == 0 &&
+  return tokens >= 0 && tokens <= (1 << 24) && seqs >= 0 && seqs <= kMostSequences && heads > 0 && heads <= 4096 && tokens * heads <= (1 << 30) && kv_heads > 0 && heads % kv_heads == 0 &&
          (d == 64 || d == 96 || d == 128);
 }
 

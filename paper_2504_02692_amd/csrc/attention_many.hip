@@ -10,7 +10,7 @@ namespace gptaq {
 // takes the weights from there without an exchange, if the first product's row 16 s + 8 b + 4 a + i has key 16 s + 8 a + 4 b + i (bits 2 and 3 change places).
 // Reads of either from LDS are runs of 512 bytes: no bank is met twice.
 // PB: bits of a page as far as they matter to a tile's layout (4, 5, 6: pages of 16, 32, and more).
-constexpr int kRing = 4;
+constexpr int kRing = 5;
 template <int D, int NW> struct ManyShape {
   static constexpr int kTileBytes = kTile * D * 2, kLoads = kTileBytes / 1024;      // of keys, or of values
   static constexpr int kPerWave = 2 * kLoads / NW;
@@ -35,22 +35,23 @@ template <int N> __device__ __forceinline__ void am_wait() {        // vmcnt <= 
 constexpr float kNoOrigin = -1e30f, kMostSum = 4096.f;
 
 template <int D, int PB, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArgs a, int64_t blocks) {
+__global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArgs a, int blocks) {
   using Shape = ManyShape<D, NW>;
   extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
   constexpr int KS = D / 16, VT = D / 32, P = 1 << PB, TILE = Shape::kTileBytes;
   const CacheShape& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
-  // The heads of a block side by side, so that with eight key heads each XCD has one; late blocks first, which see the most.
+  // The heads of a block side by side, so that with eight key heads each XCD has one; late blocks first, which see the most, all of their first parts before any second
+  // one: workgroups that find nothing to do come last (they go to the shader engines in turn, and between others they would leave CUs idle).
   const int head = (int)(blockIdx.x % (unsigned)c.kv_heads), rest = (int)(blockIdx.x / (unsigned)c.kv_heads);
-  const int part = rest % a.parts;
-  const int64_t block = blocks - 1 - (a.first_block + rest / a.parts);
-  const int s = cache_find(c, block, c.group, a.rows_bits, 1);
+  const int part = rest / blocks;
+  const Dealt dealt = cache_deal(c, a.first_block + rest % blocks, a.rows_bits, true);
+  if (dealt.block < 0) return;
+  const int s = dealt.sequence;
   const Sequence seq = cache_sequence(c, s);
-  const int64_t in_seq = block - cache_block_of(c, s, c.group, a.rows_bits, 1);
   const int rows = seq.count * c.group;
-  if (in_seq < 0 || (in_seq << a.rows_bits) >= rows) return;
-  const int row0 = (int)in_seq << a.rows_bits, last = min(row0 + 32 * NW - 1, rows - 1);
+  if (((int64_t)dealt.block << a.rows_bits) >= rows) return;         // (starts that do not ascend)
+  const int row0 = dealt.block << a.rows_bits, last = min(row0 + 32 * NW - 1, rows - 1);
   const Tiles tiles = attention_tiles(a, seq.before + at_token(row0, c.group), seq.before + at_token(last, c.group));
   const Parts parts = attention_parts(a, tiles.count);
   if (part > 0 && part >= parts.count) return;                       // (part 0 writes the zeros of rows that see nothing)
@@ -77,41 +78,35 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   const int64_t page_bytes = head_bytes * c.kv_heads;
   const unsigned char* const keys_base = (const unsigned char*)a.keys + head * head_bytes;
   const unsigned char* const values_base = (const unsigned char*)a.values + head * head_bytes;
-  const ConstantInts table = cache_constant(c.table + (int64_t)s * c.ld_table);
   const int last_tile = tiles.at(max(end - 1, 0));
-  struct Ids { int id[PAGES]; };
+  static_assert(PER % Shape::kPerWave == 0, "a wavefront's loads of a tile are of one page");
+  const int first_load = wave * Shape::kPerWave;                     // keys' loads, then values'
+  const bool loads_values = first_load >= Shape::kLoads;
+  const int load0 = loads_values ? first_load - Shape::kLoads : first_load, own_page = load0 / PER, in_page0 = load0 % PER;
+  struct Ids { int page, there; };                                   // of a tile: the wavefront's own page, a bit for each that there is
   auto tile_of = [&](int i) { return i < end ? tiles.at(i) : last_tile; };      // (behind the last that again)
-  auto pages_of = [&](Ids& g, int tile) {
-    const int at = (tile * kTile) >> c.page_bits;
-#pragma unroll
-    for (int k = 0; k < PAGES; ++k) {
-      const int id = at + k < c.table_pages ? table[at + k] : -1;
-      g.id[k] = (uint32_t)id < (uint32_t)c.pages ? id : -1;
-    }
+  // A tile's pages are asked for a tile before its loads, lane k for the k-th, by a vector load: what waits for it waits for what was asked for before it alone.
+  auto ask_pages = [&](int tile) {
+    const int at = ((tile * kTile) >> c.page_bits) + lane % PAGES;
+    return at < c.table_pages ? c.table[(int64_t)s * c.ld_table + at] : -1;
+  };
+  auto pages_of = [&](Ids& g, int asked) {
+    const bool there = (uint32_t)asked < (uint32_t)c.pages;
+    g.there = (int)(__ballot(there) & ((1 << PAGES) - 1));
+    g.page = __builtin_amdgcn_readlane(there ? asked : 0, own_page);
   };
   const int off_mask = (1 << c.page_bits) - 1;
   const int key_step = PB < 6 ? 1024 : 16 << c.page_bits;            // from one load of keys of a page to the next
   auto load_tile = [&](const Ids& g, int tile, int slot) {
     const int off = PB < 6 ? 0 : (tile * kTile) & off_mask;
     unsigned char* const to = smem + slot * 2 * TILE;
+    const LdsLoader loader((loads_values ? values_base : keys_base) + g.page * page_bytes);
+    const int step = loads_values ? 1024 : key_step, inside = loads_values ? off * (D * 2) + in_page0 * 1024 : off * 16 + in_page0 * key_step;
 #pragma unroll
-    for (int n = 0; n < Shape::kPerWave; ++n) {
-      const int at = wave * Shape::kPerWave + n;
-      const bool value = at >= Shape::kLoads;
-      const int load = value ? at - Shape::kLoads : at, which = load / PER, in_page = load - which * PER;
-      int id = g.id[0];
-#pragma unroll
-      for (int k = 1; k < PAGES; ++k) id = which == k ? g.id[k] : id;
-      const int inside = value ? off * (D * 2) + in_page * 1024 : off * 16 + in_page * key_step;
-      const LdsLoader loader((value ? values_base : keys_base) + max(id, 0) * page_bytes);
-      loader.load(to + at * 1024, lane * 16, inside);
-    }
+    for (int n = 0; n < Shape::kPerWave; ++n) loader.load(to + (first_load + n) * 1024, lane * 16, inside + n * step);
   };
   auto valid = [&](const Ids& g) {                                   // a bit for each 16 keys
-    int ok = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) ok |= (g.id[k >> (PB - 4)] >= 0 ? 1 : 0) << k;
-    return ok;
+    return PAGES == 4 ? g.there : PAGES == 2 ? (g.there & 1) * 3 | (g.there >> 1) * 12 : g.there * 15;
   };
 
   f32x16 acc[VT];
@@ -283,50 +278,60 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   };
   auto pass = [&](auto careful) {
     constexpr bool CAREFUL = decltype(careful)::value;
-    Ids now, next, after;                                            // pages of tiles i, i + 1, i + 2
-    int i = begin, tile = tile_of(i), tile1 = tile_of(i + 1), tile2 = tile_of(i + 2);
-    pages_of(now, tile);
-    load_tile(now, tile, i % kRing);
-    pages_of(next, tile1);
-    load_tile(next, tile1, (i + 1) % kRing);
-    pages_of(after, tile2);
+    Ids ids[4];                                                      // pages of tiles i .. i + 3
+    int i = begin, slot = 0, tile[4];
+    auto slot_of = [&](int ahead) { return slot + ahead < kRing ? slot + ahead : slot + ahead - kRing; };
+    int asked[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      tile[k] = tile_of(i + k);
+      asked[k] = ask_pages(tile[k]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      pages_of(ids[k], asked[k]);
+      load_tile(ids[k], tile[k], k);
+    }
     auto top_of = [&]() {
-      am_wait<0>();                                                  // the wavefront's loads of tile i + 1 are there ..
+      am_wait<Shape::kPerWave>();                                    // the wavefront's loads of tile i + 1 are there (those of i + 2 may not be) ..
       am_barrier();                                                  // .. and everyone's; and tile i - 2 is no longer read
-      load_tile(after, tile2, (i + 2) % kRing);
+      pages_of(ids[3], asked[3]);
+      asked[3] = ask_pages(tile_of(i + 4));
+      __builtin_amdgcn_sched_barrier(0);
+      load_tile(ids[3], tile[3], slot_of(3));
+      __builtin_amdgcn_sched_barrier(0);
     };
     auto advance = [&]() {
       ++i;
-      now = next;
-      next = after;
-      tile = tile1;
-      tile1 = tile2;
-      tile2 = tile_of(i + 2);
-      pages_of(after, tile2);
+      slot = slot_of(1);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) { ids[k] = ids[k + 1]; tile[k] = tile[k + 1]; }
+      tile[3] = tile_of(i + 3);
       if (i < end) top_of();
     };
-    auto keys_at = [&](int i) { return smem + (i % kRing) * 2 * TILE; };
+    auto keys_at = [&](int ahead) { return smem + slot_of(ahead) * 2 * TILE; };
     top_of();
     while (i < end) {
-      int kind = __builtin_amdgcn_readfirstlane(kind_of(now, tile));
+      int kind = __builtin_amdgcn_readfirstlane(kind_of(ids[0], tile[0]));
       if (!CAREFUL && kind >= kParts) {
-        const unsigned char* kt = keys_at(i);
+        const unsigned char* kt = keys_at(0);
         const unsigned char* vt = kt + TILE;                         // (the first product is with weights of zero)
         scores_alone(sc[0], kt, kread[0]);
         weight[1][0] = weight[1][1] = bf16x8{};
         for (;;) {
-          const int j = tile * kTile + 8 * half;
+          const int j = tile[0] * kTile + 8 * half;
           step(sc[0], sc[1], kt, kread[1], weight[1], vt, 2, weight[0], kind == kParts, j);
           vt = kt + TILE;
-          kt = keys_at(i + 1);
+          kt = keys_at(1);
           step(sc[1], sc[0], kt, kread[0], weight[0], vt, 0, weight[1], kind == kParts, j + 32);
-          kind = i + 1 < end ? __builtin_amdgcn_readfirstlane(kind_of(next, tile1)) : kNothing;
+          kind = i + 1 < end ? __builtin_amdgcn_readfirstlane(kind_of(ids[1], tile[1])) : kNothing;
           if (kind < kParts) break;
           advance();
         }
         product_alone(weight[1], vt, 2);
       } else if (kind != kNothing) {
-        work(careful, keys_at(i), tile * kTile, valid(now));
+        work(careful, keys_at(0), tile[0] * kTile, valid(ids[0]));
       }
       advance();
     }
@@ -339,7 +344,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
     for (int t = 0; t < VT; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) bad = fmaf(acc[t][e], 0.f, bad);
-    if (__syncthreads_or(bad != 0.f)) {
+    // (All of LDS is the ring's.)
+    int* const again = reinterpret_cast<int*>(smem);
+    __syncthreads();
+    if (threadIdx.x == 0) *again = 0;
+    __syncthreads();
+    if (bad != 0.f) *again = 1;
+    __syncthreads();
+    const bool careful = *again != 0;
+    __syncthreads();
+    if (careful) {
 #pragma unroll
       for (int t = 0; t < VT; ++t)
 #pragma unroll
@@ -395,7 +409,7 @@ template <int D, int PB, int NW> static hipError_t launch_many_as(const Attentio
   for (int64_t first = 0; first < blocks; first += most) {
     a.first_block = first;
     const int64_t n = blocks - first < most ? blocks - first : most;
-    hipLaunchKernelGGL((attention_many_kernel<D, PB, NW>), dim3((unsigned)(n * each)), dim3(64 * NW), (ManyShape<D, NW>::kLds), s, a, blocks);
+    hipLaunchKernelGGL((attention_many_kernel<D, PB, NW>), dim3((unsigned)(n * each)), dim3(64 * NW), (ManyShape<D, NW>::kLds), s, a, (int)n);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   return hipSuccess;

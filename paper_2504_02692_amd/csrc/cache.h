@@ -28,24 +28,68 @@ __device__ __forceinline__ Sequence cache_sequence(const CacheShape& c, int s) {
   q.before = cache_clamp(cache_constant(c.lengths)[s], 0, 1 << 30) - q.count;
   return q;
 }
-// Work is dealt out without the host knowing the lengths: with `units` pieces a token and `per` of them to a block, sequence s has the blocks from
-// starts[s] * units / per + s * extra on, which leaves each sequence room for ceil(count * units / per) + extra - 1 at least.  This finds the sequence of a block:
-// 64 of them are tried at a time, one a lane, so up to 64 sequences are one load.
-__device__ __forceinline__ int64_t cache_block_of(const CacheShape& c, int s, int units, int per_bits, int extra) {
-  return (((int64_t)cache_clamp(c.starts[s], 0, c.tokens) * units) >> per_bits) + (int64_t)s * extra;
+// Work is dealt out without the host knowing the lengths: with `units` pieces a token and 2^bits of them to a block, sequence s has the blocks from starts[s] units / 2^bits + s * extra
+// on, which leaves each sequence room for ceil(count units / 2^bits) + extra - 1 at least.  This finds the sequence of a block: 64 are tried at a time, one a lane, so up to 64
+// sequences are one load.
+__device__ __forceinline__ int64_t cache_block_of(const CacheShape& c, int s, int units, int bits, int extra) {
+  return (((int64_t)cache_clamp(c.starts[s], 0, c.tokens) * units) >> bits) + (int64_t)s * extra;
 }
-__device__ __forceinline__ int cache_find(const CacheShape& c, int64_t block, int units, int per_bits, int extra) {
+__device__ __forceinline__ int cache_find(const CacheShape& c, int64_t block, int units, int bits, int extra) {
   const int lane = threadIdx.x & 63;
   int lo = 0, n = c.seqs;
   while (n > 1) {
     const int step = (n + 63) >> 6, at = lane * step;
-    const bool here = at < n && cache_block_of(c, lo + (at < n ? at : 0), units, per_bits, extra) <= block;
+    const bool here = at < n && cache_block_of(c, lo + (at < n ? at : 0), units, bits, extra) <= block;
     const uint64_t mask = __ballot(here);
     const int k = mask ? 63 - __builtin_clzll(mask) : 0;
     lo += k * step;
     n = n - k * step < step ? n - k * step : step;
   }
   return __builtin_amdgcn_readfirstlane(lo);
+}
+// The same without gaps, for work that fills the GPU once or a few times: sequence s has ceil(rows / 2^bits) blocks of its count * group rows, and a block is found by
+// sums over the lanes, each of which has a run of sequences; then over that lane's sequences.  From the last block on where `from_end`.  block -1: there are not so many.
+struct Dealt { int32_t sequence, block; };
+__device__ __forceinline__ int64_t cache_blocks(const CacheShape& c, int s, int bits) {
+  const int first = cache_clamp(c.starts[s], 0, c.tokens), count = cache_clamp(c.starts[s + 1], first, c.tokens) - first;
+  return ((int64_t)count * c.group + (1 << bits) - 1) >> bits;
+}
+__device__ __forceinline__ int cache_prefix(int v) {                 // sums over this lane and those below
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int below = __shfl_up(v, d);
+    v += lane >= d ? below : 0;
+  }
+  return v;
+}
+__device__ __forceinline__ Dealt cache_deal(const CacheShape& c, int64_t at, int bits, bool from_end) {
+  const int lane = threadIdx.x & 63, per = (c.seqs + 63) >> 6, mine0 = lane * per, mine1 = mine0 + per < c.seqs ? mine0 + per : c.seqs;
+  int mine = 0;                                                      // (rows are 2^30 at most, and blocks fewer)
+  for (int s = mine0; s < mine1; ++s) mine += (int)cache_blocks(c, s, bits);
+  int sums = cache_prefix(mine);
+  const int all = __builtin_amdgcn_readlane(sums, 63);
+  if (at >= all) return Dealt{0, -1};
+  int block = from_end ? all - 1 - (int)at : (int)at;
+  uint64_t mask = __ballot(sums > block);
+  int k = __builtin_ctzll(mask);
+  block -= __builtin_amdgcn_readlane(sums, k) - __builtin_amdgcn_readlane(mine, k);
+  int s0 = k * per;
+  if (per > 1) {
+    const int end = s0 + per < c.seqs ? s0 + per : c.seqs;
+    for (;; s0 += 64) {                                              // (ends: the lane's sequences have the block among them)
+      mine = s0 + lane < end ? (int)cache_blocks(c, s0 + lane, bits) : 0;
+      sums = cache_prefix(mine);
+      const int here = __builtin_amdgcn_readlane(sums, 63);
+      if (block < here || s0 + 64 >= end) break;
+      block -= here;
+    }
+    mask = __ballot(sums > block);
+    k = mask ? __builtin_ctzll(mask) : 63;
+    block -= __builtin_amdgcn_readlane(sums, k) - __builtin_amdgcn_readlane(mine, k);
+    s0 = s0 + k < end ? s0 + k : end - 1;
+  }
+  return Dealt{__builtin_amdgcn_readfirstlane(s0), __builtin_amdgcn_readfirstlane(block)};
 }
 // The page of a position, or -1.
 __device__ __forceinline__ int cache_page(const CacheShape& c, int s, int position) {
@@ -56,9 +100,10 @@ __device__ __forceinline__ int cache_page(const CacheShape& c, int s, int positi
 }
 
 // What both calls refuse; fills `c`.
+constexpr int64_t kMostSequences = 65536;
 inline int cache_shape(CacheShape& c, const int32_t* table, int64_t ld_table, int64_t table_pages, const int32_t* starts, const int32_t* lengths, int64_t seqs,
                        int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d, int64_t page, int64_t pages) {
-  if (seqs < 0 || seqs > (1 << 20) || tokens < 0 || tokens > (1 << 24) || heads <= 0 || kv_heads <= 0 || heads > 4096 || heads % kv_heads || tokens * heads > (1 << 30) || pages < 0 ||
+  if (seqs < 0 || seqs > kMostSequences || tokens < 0 || tokens > (1 << 24) || heads <= 0 || kv_heads <= 0 || heads > 4096 || heads % kv_heads || tokens * heads > (1 << 30) || pages < 0 ||
       pages > (1 << 30) || table_pages < 0 || ld_table < table_pages || (((uintptr_t)table | (uintptr_t)starts | (uintptr_t)lengths) & 3))
     return GPTAQ_EDIM;
   if (page < 16 || page > 256 || (page & (page - 1))) return GPTAQ_EUNSUPPORTED;
