@@ -10,7 +10,7 @@ namespace gptaq {
 // takes the weights from there without an exchange, if the first product's row 16 s + 8 b + 4 a + i has key 16 s + 8 a + 4 b + i (bits 2 and 3 change places).
 // Reads of either from LDS are runs of 512 bytes: no bank is met twice.
 // PB: bits of a page as far as they matter to a tile's layout (4, 5, 6: pages of 16, 32, and more).
-constexpr int kRing = 5;
+constexpr int kRing = 4;                               // (five, with two tiles in flight: 1 % slower)
 template <int D, int NW> struct ManyShape {
   static constexpr int kTileBytes = kTile * D * 2, kLoads = kTileBytes / 1024;      // of keys, or of values
   static constexpr int kPerWave = 2 * kLoads / NW;
@@ -278,36 +278,35 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   };
   auto pass = [&](auto careful) {
     constexpr bool CAREFUL = decltype(careful)::value;
-    Ids ids[4];                                                      // pages of tiles i .. i + 3
-    int i = begin, slot = 0, tile[4];
-    auto slot_of = [&](int ahead) { return slot + ahead < kRing ? slot + ahead : slot + ahead - kRing; };
-    int asked[4];
+    Ids ids[3];                                                      // pages of tiles i .. i + 2
+    int i = begin, slot = 0, tile[3], asked[3];
+    auto slot_of = [&](int ahead) { return (slot + ahead) % kRing; };
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 3; ++k) {
       tile[k] = tile_of(i + k);
       asked[k] = ask_pages(tile[k]);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 2; ++k) {
       pages_of(ids[k], asked[k]);
       load_tile(ids[k], tile[k], k);
     }
     auto top_of = [&]() {
-      am_wait<Shape::kPerWave>();                                    // the wavefront's loads of tile i + 1 are there (those of i + 2 may not be) ..
+      am_wait<0>();                                                  // the wavefront's loads of tile i + 1 are there ..
       am_barrier();                                                  // .. and everyone's; and tile i - 2 is no longer read
-      pages_of(ids[3], asked[3]);
-      asked[3] = ask_pages(tile_of(i + 4));
+      pages_of(ids[2], asked[2]);
+      asked[2] = ask_pages(tile_of(i + 3));
       __builtin_amdgcn_sched_barrier(0);
-      load_tile(ids[3], tile[3], slot_of(3));
+      load_tile(ids[2], tile[2], slot_of(2));
       __builtin_amdgcn_sched_barrier(0);
     };
     auto advance = [&]() {
       ++i;
       slot = slot_of(1);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) { ids[k] = ids[k + 1]; tile[k] = tile[k + 1]; }
-      tile[3] = tile_of(i + 3);
+      for (int k = 0; k < 2; ++k) { ids[k] = ids[k + 1]; tile[k] = tile[k + 1]; }
+      tile[2] = tile_of(i + 2);
       if (i < end) top_of();
     };
     auto keys_at = [&](int ahead) { return smem + slot_of(ahead) * 2 * TILE; };
