@@ -30,9 +30,9 @@ template <int N> __device__ __forceinline__ void am_wait() {        // vmcnt <= 
   asm volatile("" ::: "memory");
 }
 
-// No score is this low; with it as the origin every weight is infinite.  A step's 16 weights of a lane may sum up to 2^12: a softmax does not depend on its origin,
+// No finite score is lower than this; with it as the origin every weight of one that is not as low is infinite.  A step's 16 weights of a lane may sum up to 2^12: a softmax does not depend on its origin,
 // and weights that much larger change no rounding of bf16 or fp32.
-constexpr float kNoOrigin = -1e30f, kMostSum = 4096.f;
+constexpr float kNoOrigin = -3.402823466e38f, kMostSum = 4096.f;
 
 template <int D, int PB, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArgs a, int blocks) {

@@ -297,6 +297,89 @@ def test_large_scores():
             check(got, c, q, 2, 0, 0)
 
 
+@pytest.mark.parametrize("pairs", [[(1, 300)], [(150, 150)]])
+def test_scores_near_the_ends_of_fp32(pairs):
+    """Scores of 1e33 and more, of either sign: one key that stands out has all the weight, and equal scores have equal weights."""
+    c = Cache(pairs, 1, 64, 16, seed=10)
+    n = len(c.k[0])
+    c.k[0][:] = -(2.0 ** 53)
+    for s in range(len(pairs)):
+        c.v[s] = 2.0 * c.r.integers(-8, 8, c.v[s].shape) + 1.0
+    q = bf16(np.full((c.tokens, 2, 64), 2.0 ** 53))
+    ws = workspace(c.tokens, 1, 2, 1, 64)
+    see = seen(c, 0, 0, 0).astype(np.float64)
+    got = f64(B.gptaq_attention(q, **c.device(), ws=ws))
+    want = see @ c.v[0][:, 0] / see.sum(1, keepdims=True)
+    assert np.all(np.abs(got[:, 0] - want) <= np.abs(want) * (HALF + 4 * U)) and np.array_equal(got[:, 0], got[:, 1])
+    c.k[0][37] = 2.0 ** 53
+    got = f64(B.gptaq_attention(q, **c.device(), ws=ws))
+    assert np.array_equal(got[see[:, 37] > 0], np.broadcast_to(c.v[0][37], got[see[:, 37] > 0].shape))
+
+
+@pytest.mark.parametrize("pairs", [[(1, 120), (1, 70)], [(120, 100), (100, 33)]])
+def test_shared_pages_and_tables_in_wider_arrays(pairs):
+    """Sequences with the same first pages, and a table whose rows are parts of longer ones."""
+    c = Cache(pairs, 2, 64, 16, seed=12)
+    shared = min(before for _, before in pairs) // 16                # (whole pages in front of the new tokens)
+    c.table[1, :shared] = c.table[0, :shared]
+    c.k[1][:shared * 16], c.v[1][:shared * 16] = c.k[0][:shared * 16], c.v[0][:shared * 16]
+    dev = c.device()
+    wide = torch.full((2, c.table.shape[1] + 9), -1, dtype=torch.int32, device="cuda")
+    dev["table"] = wide[:, 4:4 + c.table.shape[1]]
+    dev["table"].copy_(torch.from_numpy(c.table))
+    q = queries(c, 4, 64)
+    ws = workspace(c.tokens, 2, 4, 2, 64)
+    check(B.gptaq_attention(q, **dev, ws=ws), c, q, 4, 0, 0)
+    k = bf16(c.r.standard_normal((c.tokens, 2, 64)))
+    before = dev["keys"].clone()
+    B.gptaq_cache_append(q, k, k, **dev, freqs=None)                  # (new tokens are behind the shared pages)
+    for s, (count, first) in enumerate(c.pairs):
+        p = first + count - 1
+        id = int(c.table[s, p // 16])
+        assert torch.equal(dev["keys"][id, :, :, p % 16].reshape(2, 64), k[c.starts[s + 1] - 1])
+    for id in c.table[0, :shared]:
+        assert torch.equal(dev["keys"][id].view(torch.int16), before[id].view(torch.int16))
+
+
+@pytest.mark.parametrize("tokens", [1, 300])
+def test_no_pages_and_no_table(tokens):
+    empty = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+    one = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    q = bf16(np.ones((tokens, 4, 64)))
+    ws = workspace(tokens, 1, 4, 2, 64)
+    table = torch.zeros((1, 3), dtype=torch.int32, device="cuda")
+    for keys, values, t in ((empty(0, 2, 8, 16, 8), empty(0, 2, 2, 64, 8), table), (empty(5, 2, 8, 16, 8), empty(5, 2, 2, 64, 8), table[:, :0])):
+        y = B.gptaq_attention(q, keys, values, t, one(0, tokens), one(tokens), ws)
+        assert torch.all(y == 0)
+        assert torch.equal(B.gptaq_cache_append(q, q[:, :2], q[:, 2:], keys, values, t, one(0, tokens), one(tokens), None), q)
+    assert B.gptaq_attention(q, keys, values, table[:0], one(0), table[0, :0], ws).shape == q.shape
+
+
+def test_two_graphs_that_share_a_workspace():
+    """A prompt's and a step's attention, captured with one workspace and replayed in turn with eager calls between."""
+    cases = []
+    ws = workspace(300, 2, 8, 2, 128)
+    for pairs in ([(200, 700), (100, 5)], [(1, 900), (1, 77)]):
+        c = Cache(pairs, 2, 128, 16, seed=len(cases))
+        q, out = queries(c, 8, 128), torch.empty((c.tokens, 8, 128), dtype=torch.bfloat16, device="cuda")
+        dev = c.device()
+        B.gptaq_attention(q, **dev, ws=ws, out=out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.gptaq_attention(q, **dev, ws=ws, out=out)
+        cases.append((c, q, dev, out, graph))
+    for k in range(3):
+        for c, q, dev, out, graph in cases:
+            q.copy_(queries(c, 8, 128))
+            graph.replay()
+        torch.cuda.synchronize()
+        for c, q, dev, out, graph in cases:
+            got = out.clone()
+            assert torch.equal(B.gptaq_attention(q, **dev, ws=ws), got), k
+            check(got, c, q, 8, 0, 0)
+
+
 def test_many_sequences():
     """More than a wavefront tries at once, empty ones among them."""
     r = np.random.default_rng(11)
