@@ -361,8 +361,8 @@ int gptaq_quant_activations_i8(const uint16_t* X, int64_t tokens, int64_t n, int
 /* ---------------------------------------------------------------------------------------
  * What lies between the qkv product and o_proj of a decoder block: a paged cache of keys and values, and attention over it.
  *
- * The cache: keys (pages, kv_heads, d / 8, page, 8) and values (pages, kv_heads, page / 8, d, 8), bf16, contiguous, 16-byte aligned; `page` positions to a
- *   page, a power of two from 16 to 256.  Entry e of the key of position p lies in keys[id][head][e / 8][p % page][e % 8], that of its value in
+ * The cache (a gptaq_cache, in host memory, read during the call): keys (pages, kv_heads, d / 8, page, 8) and values (pages, kv_heads, page / 8, d, 8), bf16,
+ *   contiguous, 16-byte aligned; `page` positions to a page, a power of two from 16 to 256.  Entry e of the key of position p lies in keys[id][head][e / 8][p % page][e % 8], that of its value in
  *   values[id][head][p % page / 8][e][p % 8], with id = table[s][p / page].
  *   table  : (seqs x table_pages) int32, leading dimension ld_table: the pages of each sequence in order; those behind its length are not looked at.  An entry
  *            outside 0 .. pages - 1 stands for a page that is not there (given back, for instance): nothing is written to it, and no token sees its positions.
@@ -385,15 +385,19 @@ int gptaq_quant_activations_i8(const uint16_t* X, int64_t tokens, int64_t n, int
  *   ws     : >= gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d) bytes, 256-byte aligned; the size for more tokens serves fewer.
  * Scores, the softmax's maximum and sum, and the outputs' sums are fp32; weights w are rounded to bf16 for the product with the values.  The order of a sum depends on
  * the shapes and the lengths alone: no atomics, the same bits every time. */
+typedef struct gptaq_cache {
+  uint16_t *keys, *values;
+  int64_t pages, kv_heads, page, d;
+  const int32_t* table;
+  int64_t ld_table, table_pages;
+  const int32_t *starts, *lengths;
+  int64_t seqs;
+} gptaq_cache;
 int gptaq_cache_append(const uint16_t* q, int64_t ldq, int64_t hq, const uint16_t* k, int64_t ldk, int64_t hk, const uint16_t* v,
-                       int64_t ldv, int64_t hv, uint16_t* keys, uint16_t* values, int64_t pages, int64_t page, const int32_t* table,
-                       int64_t ld_table, int64_t table_pages, const int32_t* starts, const int32_t* lengths, int64_t seqs,
-                       int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d, const double* freqs, int64_t pairs,
-                       int interleaved, uint16_t* out, int64_t ldo, int64_t ho, void* stream);
+                       int64_t ldv, int64_t hv, const gptaq_cache* cache, int64_t tokens, int64_t heads, const double* freqs,
+                       int64_t pairs, int interleaved, uint16_t* out, int64_t ldo, int64_t ho, void* stream);
 size_t gptaq_attention_workspace_bytes(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t d);
-int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const uint16_t* keys, const uint16_t* values, int64_t pages,
-                    int64_t page, const int32_t* table, int64_t ld_table, int64_t table_pages, const int32_t* starts,
-                    const int32_t* lengths, int64_t seqs, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d,
+int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const gptaq_cache* cache, int64_t tokens, int64_t heads,
                     int64_t window, int64_t sinks, float scale, uint16_t* out, int64_t ldo, int64_t ho, void* ws, size_t ws_bytes,
                     void* stream);
 

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -91,13 +92,11 @@ _SIGS = {
                                     _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "gptaq_quant_activations_i8": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float, _c.c_void_p, _c.c_int64, _c.c_void_p,
                                               _c.c_void_p]),
-    "gptaq_cache_append": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64] * 3 + [_c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_int64,
-                                     _c.c_int64, _c.c_void_p, _c.c_void_p] + [_c.c_int64] * 5 + [_c.c_void_p, _c.c_int64, _c.c_int, _c.c_void_p, _c.c_int64,
-                                     _c.c_int64, _c.c_void_p]),
+    "gptaq_cache_append": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64] * 3 + [_c.c_char_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int,
+                                     _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p]),
     "gptaq_attention_workspace_bytes": (_c.c_size_t, [_c.c_int64] * 5),
-    "gptaq_attention": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_int64, _c.c_int64,
-                                   _c.c_void_p, _c.c_void_p] + [_c.c_int64] * 7 + [_c.c_float, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_size_t,
-                                   _c.c_void_p]),
+    "gptaq_attention": (_c.c_int, [_c.c_void_p, _c.c_int64, _c.c_int64, _c.c_char_p] + [_c.c_int64] * 4 + [_c.c_float, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p,
+                                   _c.c_size_t, _c.c_void_p]),
     "gptaq_profile_enable": (_c.c_int, [_c.c_int]),
     "gptaq_profile_read": (_c.c_int, [_c.c_int, _c.POINTER(_c.c_int64), _c.POINTER(_c.c_double)]),
     "gptaq_measure_mfma_peak": (_c.c_int, [_c.c_int, _c.c_int, _c.c_void_p, _c.c_size_t, _c.POINTER(_c.c_double),
@@ -724,6 +723,9 @@ def gptaq_quant_activations_i8(X: torch.Tensor, clip: float = 1.0):
 
 # ---- the cache and attention
 
+_cache = struct.Struct("12q").pack                       # a gptaq_cache
+
+
 def _need_heads(t: torch.Tensor, shape, name: str):
     """(address, stride of tokens, stride of heads) of a (tokens x heads x d) bf16 tensor of that shape."""
     stride = t.stride()
@@ -735,21 +737,22 @@ def _need_heads(t: torch.Tensor, shape, name: str):
 
 
 def _cache_args(keys: torch.Tensor, values: torch.Tensor, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, d: int, name: str):
-    """The cache's arguments as the C calls take them: (keys, values, pages, page, table, ld_table, table_pages, starts, lengths, seqs), and kv_heads."""
-    shape, seqs, width, bf16, int32 = keys.shape, lengths.numel(), table.shape[-1], torch.bfloat16, torch.int32
+    """The cache as the C calls take it, and kv_heads."""
+    bf16, int32, shape, size = torch.bfloat16, torch.int32, keys.shape, table.shape
     if keys.dtype is not bf16 or len(shape) != 5 or shape[2] * 8 != d or shape[4] != 8 or not keys.is_contiguous():
         raise GptaqError(f"{name}: keys: expected contiguous bfloat16 (pages, kv_heads, {d} / 8, page, 8)")
     pages, kv_heads, _, page, _ = shape
     if values.dtype is not bf16 or values.shape != (pages, kv_heads, page // 8, d, 8) or not values.is_contiguous():
         raise GptaqError(f"{name}: values: expected contiguous bfloat16 ({pages}, {kv_heads}, {page} / 8, {d}, 8)")
-    if lengths.dtype is not int32 or lengths.dim() != 1 or not lengths.is_contiguous():
-        raise GptaqError(f"{name}: lengths: expected a contiguous int32 vector")
-    if starts.dtype is not int32 or starts.dim() != 1 or starts.numel() != seqs + 1 or not starts.is_contiguous():
+    if table.dtype is not int32 or len(size) != 2 or (size[1] > 1 and table.stride(1) != 1):
+        raise GptaqError(f"{name}: table: expected a row-major int32 tensor with a row for each sequence")
+    seqs, width = size
+    if lengths.dtype is not int32 or lengths.shape != (seqs,) or not lengths.is_contiguous():
+        raise GptaqError(f"{name}: lengths: expected {seqs} contiguous int32, as many as the table has rows")
+    if starts.dtype is not int32 or starts.shape != (seqs + 1,) or not starts.is_contiguous():
         raise GptaqError(f"{name}: starts: expected {seqs + 1} contiguous int32")
-    if table.dtype is not int32 or table.shape != (seqs, width) or (width > 1 and table.stride(1) != 1):
-        raise GptaqError(f"{name}: table: expected a row-major int32 tensor with a row for each of {seqs} sequences")
-    return (keys.data_ptr(), values.data_ptr(), pages, page, table.data_ptr(), table.stride(0) if seqs > 1 else width, width, starts.data_ptr(),
-            lengths.data_ptr(), seqs), kv_heads
+    return _cache(keys.data_ptr(), values.data_ptr(), pages, kv_heads, page, d, table.data_ptr(), table.stride(0) if seqs > 1 else width, width, starts.data_ptr(),
+                  lengths.data_ptr(), seqs), kv_heads
 
 
 def _heads_of(q: torch.Tensor, name: str):
@@ -775,10 +778,14 @@ def gptaq_cache_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, keys: 
         if freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
             raise GptaqError("gptaq_cache_append: freqs: expected a contiguous float64 vector")
         pairs = freqs.numel()
+    qp = _need_heads(q, shape, "q")
     if out is None:
-        out = q.new_empty(shape)
-    _check(load().gptaq_cache_append(*_need_heads(q, shape, "q"), *_need_heads(k, kv_shape, "k"), *_need_heads(v, kv_shape, "v"), *cache, tokens, heads, kv_heads, d,
-                                     _ptr(freqs), pairs, bool(interleaved), *_need_heads(out, shape, "out"), _stream(device)), "gptaq_cache_append")
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        op = out.data_ptr(), heads * d, d
+    else:
+        op = _need_heads(out, shape, "out")
+    _check(load().gptaq_cache_append(*qp, *_need_heads(k, kv_shape, "k"), *_need_heads(v, kv_shape, "v"), cache, tokens, heads, _ptr(freqs), pairs, bool(interleaved),
+                                     *op, _stream(device)), "gptaq_cache_append")
     return out
 
 
@@ -793,10 +800,13 @@ def gptaq_attention(q: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, t
     device = _here(q, keys, values, table, starts, lengths, out)
     shape = _heads_of(q, "gptaq_attention")
     tokens, heads, d = shape
-    cache, kv_heads = _cache_args(keys, values, table, starts, lengths, d, "gptaq_attention")
+    cache, _ = _cache_args(keys, values, table, starts, lengths, d, "gptaq_attention")
+    qp = _need_heads(q, shape, "q")
     if out is None:
-        out = q.new_empty(shape)
-    _check(load().gptaq_attention(*_need_heads(q, shape, "q"), *cache, tokens, heads, kv_heads, d, int(window), int(sinks),
-                                  d ** -0.5 if scale is None else float(scale), *_need_heads(out, shape, "out"), _ws(ws, device), ws.nbytes, _stream(device)),
-           "gptaq_attention")
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        op = out.data_ptr(), heads * d, d
+    else:
+        op = _need_heads(out, shape, "out")
+    _check(load().gptaq_attention(*qp, cache, tokens, heads, int(window), int(sinks), d ** -0.5 if scale is None else float(scale), *op, _ws(ws, device), ws.nbytes,
+                                  _stream(device)), "gptaq_attention")
     return out

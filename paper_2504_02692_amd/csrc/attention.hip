@@ -315,28 +315,27 @@ extern "C" size_t gptaq_attention_workspace_bytes(int64_t tokens, int64_t seqs, 
   return ((size_t)partial_rows(tokens, heads) * (d + 2) * 4 + 255) / 256 * 256;
 }
 
-extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const uint16_t* keys, const uint16_t* values, int64_t pages, int64_t page,
-                               const int32_t* table, int64_t ld_table, int64_t table_pages, const int32_t* starts, const int32_t* lengths, int64_t seqs,
-                               int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d, int64_t window, int64_t sinks, float scale, uint16_t* out, int64_t ldo,
-                               int64_t ho, void* ws, size_t ws_bytes, void* stream) {
-  if (tokens != 0 && seqs != 0 && (!q || !out || !starts || !lengths || !ws || (table_pages != 0 && !table) || (pages != 0 && (!keys || !values)))) return GPTAQ_ENULL;
+extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const gptaq_cache* cache, int64_t tokens, int64_t heads, int64_t window, int64_t sinks,
+                               float scale, uint16_t* out, int64_t ldo, int64_t ho, void* ws, size_t ws_bytes, void* stream) {
   AttentionArgs a{};
-  if (const int rc = cache_shape(a.c, table, ld_table, table_pages, starts, lengths, seqs, tokens, heads, kv_heads, d, page, pages)) return rc;
+  if (const int rc = cache_shape(a.c, cache, tokens, heads)) return rc;
+  const int64_t d = cache->d, kv_heads = cache->kv_heads, seqs = cache->seqs;
+  if (tokens != 0 && seqs != 0 && (!q || !out || !ws)) return GPTAQ_ENULL;
   if (d != 64 && d != 96 && d != 128) return GPTAQ_EUNSUPPORTED;
-  if ((((uintptr_t)q | (uintptr_t)out) & 1) || (((uintptr_t)keys | (uintptr_t)values) & 15) || ldq < 0 || hq < 0 || window < 0 || sinks < 0 ||
+  if ((((uintptr_t)q | (uintptr_t)out) & 1) || ldq < 0 || hq < 0 || window < 0 || sinks < 0 ||
       !cache_rows_apart(tokens, ldo, heads, ho, d))
     return GPTAQ_EDIM;
   if (!(scale > -__builtin_inff() && scale < __builtin_inff())) return GPTAQ_EUNSUPPORTED;
   if (tokens == 0 || seqs == 0) return GPTAQ_OK;
   if (((uintptr_t)ws & 255) || ws_bytes < gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d)) return GPTAQ_EWORKSPACE;
   constexpr int64_t kFar = (int64_t)1 << 30;                          // (positions are below this)
-  a.q = q; a.keys = keys; a.values = values; a.ldq = ldq; a.hq = hq;
+  a.q = q; a.keys = cache->keys; a.values = cache->values; a.ldq = ldq; a.hq = hq;
   a.out = out; a.ldo = ldo; a.ho = ho;
   a.scale = scale == 0.f ? 0x1p-126f : scale * 1.4426950408889634f;  // (0 times the minus infinity of a key that is not seen is NaN; 2^-126 gives the same weights)
   a.window = (int32_t)(window < kFar ? window : 0);
   a.sinks = (int32_t)(sinks < kFar ? sinks : kFar);
   // Tiles that a row can see: those of the table, or of the window (which begins and ends inside a tile, as the block's other rows have theirs) and the sinks.
-  int64_t most_tiles = (table_pages * page + kTile - 1) / kTile;
+  int64_t most_tiles = (cache->table_pages * cache->page + kTile - 1) / kTile;
   if (a.window && a.window / kTile + a.sinks / kTile + 4 < most_tiles) most_tiles = a.window / kTile + a.sinks / kTile + 4;
   const Plan plan = attention_plan(tokens, seqs, heads, kv_heads, most_tiles);
   a.rows_bits = plan.bits;
@@ -344,7 +343,7 @@ extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const
   a.min_tiles = plan.min_tiles;
   a.partial = (float*)ws;
   a.stats = a.partial + (int64_t)a.parts * tokens * heads * d;
-  if (pages == 0) a.c.table_pages = 0;                                // no key anywhere: zeros
+  if (cache->pages == 0) a.c.table_pages = 0;                                // no key anywhere: zeros
   const hipError_t e = d == 64 ? launch_attention<64>(a, (hipStream_t)stream) : d == 96 ? launch_attention<96>(a, (hipStream_t)stream)
                                                                             : launch_attention<128>(a, (hipStream_t)stream);
   if (e != hipSuccess) { set_last_hip_error(e); return GPTAQ_ELAUNCH; }

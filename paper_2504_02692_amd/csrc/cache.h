@@ -101,8 +101,11 @@ __device__ __forceinline__ int cache_page(const CacheShape& c, int s, int positi
 
 // What both calls refuse; fills `c`.
 constexpr int64_t kMostSequences = 65536;
-inline int cache_shape(CacheShape& c, const int32_t* table, int64_t ld_table, int64_t table_pages, const int32_t* starts, const int32_t* lengths, int64_t seqs,
-                       int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d, int64_t page, int64_t pages) {
+inline int cache_shape(CacheShape& c, const gptaq_cache* cache, int64_t tokens, int64_t heads) {
+  if (!cache) return GPTAQ_ENULL;
+  const auto [keys, values, pages, kv_heads, page, d, table, ld_table, table_pages, starts, lengths, seqs] = *cache;
+  if (tokens != 0 && seqs != 0 && (!starts || !lengths || (table_pages != 0 && !table) || (pages != 0 && (!keys || !values)))) return GPTAQ_ENULL;
+  if (((uintptr_t)keys | (uintptr_t)values) & 15) return GPTAQ_EDIM;
   if (seqs < 0 || seqs > kMostSequences || tokens < 0 || tokens > (1 << 24) || heads <= 0 || kv_heads <= 0 || heads > 4096 || heads % kv_heads || tokens * heads > (1 << 30) || pages < 0 ||
       pages > (1 << 30) || table_pages < 0 || ld_table < table_pages || (((uintptr_t)table | (uintptr_t)starts | (uintptr_t)lengths) & 3))
     return GPTAQ_EDIM;

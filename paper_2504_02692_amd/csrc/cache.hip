@@ -132,22 +132,20 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs p) {
 using namespace gptaq;
 
 extern "C" int gptaq_cache_append(const uint16_t* q, int64_t ldq, int64_t hq, const uint16_t* k, int64_t ldk, int64_t hk, const uint16_t* v, int64_t ldv, int64_t hv,
-                                  uint16_t* keys, uint16_t* values, int64_t pages, int64_t page, const int32_t* table, int64_t ld_table, int64_t table_pages,
-                                  const int32_t* starts, const int32_t* lengths, int64_t seqs, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t d,
-                                  const double* freqs, int64_t pairs, int interleaved, uint16_t* out, int64_t ldo, int64_t ho, void* stream) {
-  if (tokens != 0 && seqs != 0 && (!q || !k || !v || !out || !starts || !lengths || (pairs != 0 && !freqs) || (table_pages != 0 && !table) ||
-                                   (pages != 0 && (!keys || !values))))
-    return GPTAQ_ENULL;
+                                  const gptaq_cache* cache, int64_t tokens, int64_t heads, const double* freqs, int64_t pairs, int interleaved, uint16_t* out,
+                                  int64_t ldo, int64_t ho, void* stream) {
   AppendArgs p{};
-  if (const int rc = cache_shape(p.c, table, ld_table, table_pages, starts, lengths, seqs, tokens, heads, kv_heads, d, page, pages)) return rc;
+  if (const int rc = cache_shape(p.c, cache, tokens, heads)) return rc;
+  const int64_t d = cache->d, kv_heads = cache->kv_heads, seqs = cache->seqs;
+  if (tokens != 0 && seqs != 0 && (!q || !k || !v || !out || (pairs != 0 && !freqs))) return GPTAQ_ENULL;
   if (d <= 0 || d % 16 || d > 256 || pairs < 0 || pairs % 8 || 2 * pairs > d) return GPTAQ_EUNSUPPORTED;
-  if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 1) || (((uintptr_t)keys | (uintptr_t)values) & 15) || ((uintptr_t)freqs & 7) ||
+  if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 1) || ((uintptr_t)freqs & 7) ||
       ldq < 0 || hq < 0 || ldk < 0 || hk < 0 || ldv < 0 || hv < 0 || !cache_rows_apart(tokens, ldo, heads, ho, d))
     return GPTAQ_EDIM;
   if (out == q && tokens != 0 && (ldo != ldq || ho != hq)) return GPTAQ_EUNSUPPORTED;
   if (tokens == 0 || seqs == 0) return GPTAQ_OK;
   p.q = q; p.k = k; p.v = v; p.ldq = ldq; p.hq = hq; p.ldk = ldk; p.hk = hk; p.ldv = ldv; p.hv = hv;
-  p.keys = keys; p.values = values; p.out = out; p.ldo = ldo; p.ho = ho;
+  p.keys = cache->keys; p.values = cache->values; p.out = out; p.ldo = ldo; p.ho = ho;
   p.freqs = freqs; p.half = (int32_t)pairs; p.interleaved = interleaved ? 1 : 0;
   const int64_t blocks = tokens / 8 + 2 * seqs;
   const int64_t items = (heads + kv_heads) * (d / 16);              // of a token

@@ -1,6 +1,7 @@
 """The cache's, attention's and the 8-bit layers' calls refuse what they cannot take, on the host, before anything is launched (no GPU needed)."""
 import ctypes
 import os
+import struct
 
 import pytest
 
@@ -91,14 +92,19 @@ def test_quant_activations_refusals(lib):
     run(0, tokens=0)
 
 
-def cache(want_append, want_attention, lib, pages=10, page=16, table=ONE, ld_table=5, table_pages=5, starts=ONE, lengths=ONE, seqs=2, tokens=3, heads=4,
-          kv_heads=2, d=64, keys=ONE, values=ONE):
+def packed(pages=10, page=16, table=ONE, ld_table=5, table_pages=5, starts=ONE, lengths=ONE, seqs=2, kv_heads=2, d=64, keys=ONE, values=ONE):
+    """A gptaq_cache."""
+    return struct.pack("12q", *(v if isinstance(v, int) else v.value or 0 for v in (keys, values, pages, kv_heads, page, d, table, ld_table, table_pages, starts, lengths, seqs)))
+
+
+def cache(want_append, want_attention, lib, tokens=3, heads=4, **more):
+    d, kv_heads = more.get("d", 64), more.get("kv_heads", 2)
+    far = ctypes.c_void_p(1 << 20)
     if want_append is not None:
-        assert lib.gptaq_cache_append(ONE, heads * d, d, ONE, kv_heads * d, d, ONE, kv_heads * d, d, keys, values, pages, page, table, ld_table, table_pages, starts,
-                                      lengths, seqs, tokens, heads, kv_heads, d, ONE, 32, 0, ctypes.c_void_p(1 << 20), heads * d, d, NULL) == want_append
+        assert lib.gptaq_cache_append(ONE, heads * d, d, ONE, kv_heads * d, d, ONE, kv_heads * d, d, packed(**more), tokens, heads, ONE, 32, 0, far, heads * d, d,
+                                      NULL) == want_append
     if want_attention is not None:
-        assert lib.gptaq_attention(ONE, heads * d, d, keys, values, pages, page, table, ld_table, table_pages, starts, lengths, seqs, tokens, heads, kv_heads,
-                                   d, 0, 0, 0.125, ctypes.c_void_p(1 << 20), heads * d, d, ONE, BIG, NULL) == want_attention
+        assert lib.gptaq_attention(ONE, heads * d, d, packed(**more), tokens, heads, 0, 0, 0.125, far, heads * d, d, ONE, BIG, NULL) == want_attention
 
 
 def test_cache_refusals(lib):
@@ -126,6 +132,8 @@ def test_cache_refusals(lib):
     cache(None, -3, lib, d=32)                            # (the cache takes it, attention has no kernel for it)
     cache(None, -3, lib, d=256)
     cache(-3, None, lib, d=272)
+    assert lib.gptaq_attention(ONE, 256, 64, None, 3, 4, 0, 0, 0.125, ONE, 256, 64, ONE, BIG, NULL) == -1
+    assert lib.gptaq_cache_append(ONE, 256, 64, ONE, 128, 64, ONE, 128, 64, None, 3, 4, ONE, 32, 0, ONE, 256, 64, NULL) == -1
     cache(0, 0, lib, tokens=0)
     cache(0, 0, lib, seqs=0)
     cache(0, 0, lib, tokens=0, table=NULL, starts=NULL, lengths=NULL, keys=NULL, values=NULL)
@@ -133,8 +141,7 @@ def test_cache_refusals(lib):
 
 def test_append_refusals(lib):
     def run(want, q=ONE, k=ONE, v=ONE, ldq=256, hq=64, ldk=128, hk=64, ldv=128, hv=64, d=64, freqs=ONE, pairs=32, out=ctypes.c_void_p(1 << 20), ldo=256, ho=64, tokens=3):
-        assert lib.gptaq_cache_append(q, ldq, hq, k, ldk, hk, v, ldv, hv, ONE, ONE, 10, 16, ONE, 5, 5, ONE, ONE, 2, tokens, 4, 2, d, freqs, pairs, 0, out, ldo, ho,
-                                      NULL) == want
+        assert lib.gptaq_cache_append(q, ldq, hq, k, ldk, hk, v, ldv, hv, packed(d=d), tokens, 4, freqs, pairs, 0, out, ldo, ho, NULL) == want
 
     for name in ("q", "k", "v", "out", "freqs"):
         run(-1, **{name: NULL})
@@ -153,7 +160,7 @@ def test_append_refusals(lib):
 
 def test_attention_refusals(lib):
     def run(want, q=ONE, ldq=256, hq=64, tokens=3, seqs=2, d=64, window=0, sinks=0, scale=0.125, out=ctypes.c_void_p(1 << 20), ldo=256, ho=64, ws=ONE, nb=BIG):
-        assert lib.gptaq_attention(q, ldq, hq, ONE, ONE, 10, 16, ONE, 5, 5, ONE, ONE, seqs, tokens, 4, 2, d, window, sinks, scale, out, ldo, ho, ws, nb, NULL) == want
+        assert lib.gptaq_attention(q, ldq, hq, packed(seqs=seqs, d=d), tokens, 4, window, sinks, scale, out, ldo, ho, ws, nb, NULL) == want
 
     for name in ("q", "out", "ws"):
         run(-1, **{name: NULL})
