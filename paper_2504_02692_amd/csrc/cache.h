@@ -65,8 +65,8 @@ __device__ __forceinline__ int cache_prefix(int v) {                 // sums ove
 }
 __device__ __forceinline__ Dealt cache_deal(const CacheShape& c, int64_t at, int bits, bool from_end) {
   const int lane = threadIdx.x & 63, per = (c.seqs + 63) >> 6, mine0 = lane * per, mine1 = mine0 + per < c.seqs ? mine0 + per : c.seqs;
-  int mine = 0;                                                      // (rows are 2^30 at most, and blocks fewer)
-  for (int s = mine0; s < mine1; ++s) mine += (int)cache_blocks(c, s, bits);
+  int mine = 0;                                                      // (blocks are 2^23 at most; starts that do not ascend could say more than 31 bits)
+  for (int s = mine0; s < mine1; ++s) mine = min(mine + (int)cache_blocks(c, s, bits), 1 << 24);
   int sums = cache_prefix(mine);
   const int all = __builtin_amdgcn_readlane(sums, 63);
   if (at >= all) return Dealt{0, -1};
