@@ -380,7 +380,7 @@ int gptaq_quant_activations_i8(const uint16_t* X, int64_t tokens, int64_t n, int
  *   (a, b) -> (a cos - b sin, b cos + a sin), taken in fp32 and rounded once.  Entries from 2 pairs on are copied.  d is a multiple of 16 up to 256, pairs one of 8
  *   up to d / 2.  out may be q itself (same strides); other overlaps are not allowed.  Queries of positions below 0 are not written.
  * gptaq_attention: out[i] = sum_j w_ij v_j / sum_j w_ij with w_ij = exp(scale q_i k_j) over the positions j that token i, at position p, sees: j <= p, and with
- *   window > 0 only j > p - window or j < sinks.  d is 64, 96 or 128.  A token that sees nothing gives zeros.  What lies where no token sees it (other sequences'
+ *   window > 0 only j > p - window or j < sinks.  d is 64, 96 or 128; scale log2(e) is finite in fp32.  A token that sees nothing gives zeros.  What lies where no token sees it (other sequences'
  *   remains, infinities, NaN) changes nothing.
  *   ws     : >= gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d) bytes, 256-byte aligned; the size for more tokens serves fewer.
  * Scores, the softmax's maximum and sum, and the outputs' sums are fp32; weights w are rounded to bf16 for the product with the values.  The order of a sum depends on

@@ -325,13 +325,14 @@ extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const
   if ((((uintptr_t)q | (uintptr_t)out) & 1) || ldq < 0 || hq < 0 || window < 0 || sinks < 0 ||
       !cache_rows_apart(tokens, ldo, heads, ho, d))
     return GPTAQ_EDIM;
-  if (!(scale > -__builtin_inff() && scale < __builtin_inff())) return GPTAQ_EUNSUPPORTED;
+  const float scale2 = scale * 1.4426950408889634f;
+  if (!(fabsf(scale2) < __builtin_inff())) return GPTAQ_EUNSUPPORTED;
   if (tokens == 0 || seqs == 0) return GPTAQ_OK;
   if (((uintptr_t)ws & 255) || ws_bytes < gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d)) return GPTAQ_EWORKSPACE;
   constexpr int64_t kFar = (int64_t)1 << 30;                          // (positions are below this)
   a.q = q; a.keys = cache->keys; a.values = cache->values; a.ldq = ldq; a.hq = hq;
   a.out = out; a.ldo = ldo; a.ho = ho;
-  a.scale = scale == 0.f ? 0x1p-126f : scale * 1.4426950408889634f;  // (0 times the minus infinity of a key that is not seen is NaN; 2^-126 gives the same weights)
+  a.scale = scale2;
   a.window = (int32_t)(window < kFar ? window : 0);
   a.sinks = (int32_t)(sinks < kFar ? sinks : kFar);
   // Tiles that a row can see: those of the table, or of the window (which begins and ends inside a tile, as the block's other rows have theirs) and the sinks.

@@ -140,7 +140,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
     float most = kUnseen;
 #pragma unroll
     for (int e = 0; e < 16; ++e) most = fmaxf(most, seen >> place(e) & 1 ? now[e] : kUnseen);
-    most *= scale;
+    most = most == kUnseen ? kUnseen : most * scale;                 // (a scale of 0 would make NaN of it)
     most = fmaxf(most, __shfl_xor(most, 32));
     if (most == kUnseen) most = kNoOrigin;
     const float to = fmaxf(origin, most);

@@ -176,6 +176,12 @@ def test_attention_refusals(lib):
     run(0, tokens=0)
 
 
+def test_attention_refuses_scales_that_leave_fp32_as_exponents_of_two(lib):
+    for scale, want in ((3e38, -3), (-2.4e38, -3), (2.3e38, 0), (0.0, 0)):
+        rc = lib.gptaq_attention(ONE, 256, 64, packed(seqs=0), 3, 4, 0, 0, scale, ONE, 256, 64, ONE, BIG, NULL)
+        assert rc == want, scale
+
+
 def test_attention_workspace(lib):
     size = lib.gptaq_attention_workspace_bytes
     for bad in ((0, 1, 4, 2, 64), (1, 0, 4, 2, 64), (1, 1, 4, 3, 64), (1, 1, 4, 2, 72), (-1, 1, 4, 2, 64), (1, 1, 0, 1, 64), ((1 << 24) + 1, 1, 1, 1, 64)):

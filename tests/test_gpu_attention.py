@@ -298,6 +298,22 @@ def test_large_scores():
 
 
 @pytest.mark.parametrize("pairs", [[(1, 300)], [(150, 150)]])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (33, 3)])
+def test_a_scale_of_zero_weighs_all_alike(pairs, window, sinks):
+    """Whatever the sums of products are (2^123 here, of either sign): each key that is seen has the same weight."""
+    c = Cache(pairs, 1, 64, 16, seed=11)
+    c.k[0][:] = np.where(np.arange(len(c.k[0])) % 3 == 0, 2.0 ** 62, -(2.0 ** 62))[:, None, None]
+    c.v[0] = 2.0 * c.r.integers(-8, 8, c.v[0].shape) + 1.0
+    q = bf16(np.full((c.tokens, 2, 64), 2.0 ** 55))
+    see = seen(c, 0, window, sinks).astype(np.float64)
+    want = see @ c.v[0][:, 0] / see.sum(1, keepdims=True)
+    for scale in (0.0, -0.0, 2.0 ** -149):               # (the last: exponents of 2^-26, weights within as much of 1, values up to 15)
+        got = f64(B.gptaq_attention(q, **c.device(), ws=workspace(c.tokens, 1, 2, 1, 64), window=window, sinks=sinks, scale=scale))
+        tol = np.abs(want) * (HALF + 4 * U) + 32 * 2.0 ** -26 * (scale != 0.0)
+        assert np.all(np.abs(got[:, 0] - want) <= tol) and np.array_equal(got[:, 0], got[:, 1]), scale
+
+
+@pytest.mark.parametrize("pairs", [[(1, 300)], [(150, 150)]])
 def test_scores_near_the_ends_of_fp32(pairs):
     """Scores of 1e33 and more, of either sign: one key that stands out has all the weight, and equal scores have equal weights."""
     c = Cache(pairs, 1, 64, 16, seed=10)
