@@ -93,7 +93,7 @@ __device__ __forceinline__ float at_origin(float m) { return m == -__builtin_inf
 __device__ __forceinline__ float at_factor(float was, float now) { return was == -__builtin_inff() ? 1.f : at_exp2(was - now); }
 
 // attention_many.hip: blocks of 32 kManyWaves rows, `blocks` of them (a.rows_bits is set).
-constexpr int kManyWaves = 8, kManyBits = 8;
+constexpr int kManyWaves = 4, kManyBits = 7;
 hipError_t launch_attention_many(const AttentionArgs& a, int64_t blocks, hipStream_t s);
 
 }  // namespace gptaq

@@ -256,20 +256,23 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
 constexpr int64_t kMostParts = 64, kFewBits = 4, kPartialRows = 65536;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
-// Rows of a sequence, on average, up to which blocks are of few: us a call of few / many, 32 heads over 2000 positions, 32 rows 13.6 / 21.8, 64 16.2 / 23.1, 128 22.1 /
-// 27.4, 512 50.8 / 47.2; 64 heads over 8, four sequences over 4000, 64 21.8 / 25.2, 128 31.8 / 30.2, 512 93 / 59; 32 over 8, sixteen over 2000, 64 29.3 / 37.5, 128 49.7 / 45.5, 512 162 / 79.
-constexpr int64_t kFewRows = 96;
+// Blocks of few rows read the keys once for 16 rows, and little else bounds them; blocks of many read them once for 128, and take longer to begin and end.  So calls are of
+// few as long as their blocks' tiles, with nine for what a block costs besides, are kFewWork at most, and where a sequence has 16 rows at most.  us a call of few / many, rows of a
+// sequence and key head: 32 heads behind 2000 positions (23k at 256 rows), 64 16.3 / 22.5, 256 26 / 35, 384 41 / 39, 1024 105 / 78; 64 heads over 8 behind 8000 (18k at 256), 256 28 / 35, 384 47 / 38;
+// four sequences of these behind 4000, 128 30.6 / 32.6 (19k), 192 38 / 36.5 (28k); sixteen, 32 heads over 8 behind 2000, 64 29 / 34 (22k), 96 45 / 39 (32k); 64 behind 500, 48 36 / 25 (28k);
+// 64 behind 8000, 64 heads over 8, 16 324 / 301, 32 408 / 319, 96 724 / 342; 32 heads with no positions before, 512 14 / 19, 768 23 / 34 (33k).
+constexpr int64_t kFewWork = 22000;
 struct Plan { int bits; int64_t parts; int min_tiles; };
-// Rows of a block, and parts of the keys.  Blocks of many rows: for a workgroup a CU, of 8 tiles at least.  Blocks of few rows: for two a CU, of 4 tiles at least, or, which
+// Rows of a block, and parts of the keys.  Blocks of many rows: for two workgroups a CU, of 8 tiles at least.  Blocks of few rows: for two a CU, of 4 tiles at least, or, which
 // evens sequences of different lengths out, for eight a CU of 32 tiles at least.  us a call, room for 512 / 1024 / 2048 workgroups of 4 tiles: 64 heads over 8 of 128, 64
 // sequences of up to 1000 positions 30.0 / 35.5 / 43.7 (those that find nothing to do take a microsecond, too), of up to 8191 245 / 241 / 234; 8 heads, 8 of up to 16000
 // 70.8 / 73.7 / 73.4.  Tiles at least, 2 / 4 / 9: 32 heads, one sequence of 200 8.1 / 5.8 / 7.5, a window of 1024 11.4 / 10.7 / 12.9; 64 over 8, 8000 18.4 / 16.0 / 15.4.
 static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t most_tiles) {
-  const int64_t group = heads / kv_heads;
-  const bool many = tokens * group > kFewRows * seqs;
+  const int64_t group = heads / kv_heads, sixteens = ((tokens * group - 1) >> kFewBits) + 1;
+  const bool many = tokens * group > 16 * seqs && (sixteens > seqs ? sixteens : seqs) * kv_heads * (most_tiles + 9) > kFewWork;
   const int bits = many ? kManyBits : kFewBits;
   const int64_t full = ((tokens * group - 1) >> bits) + 1, blocks = (full > seqs ? full : seqs) * kv_heads, min_tiles = many ? 8 : 4;
-  int64_t parts = (many ? 256 : 512) / blocks, even = 2048 / blocks;
+  int64_t parts = 512 / blocks, even = 2048 / blocks;
   if (parts > (most_tiles + min_tiles - 1) / min_tiles) parts = (most_tiles + min_tiles - 1) / min_tiles;
   if (even > most_tiles / 32) even = most_tiles / 32;
   if (!many && parts < even) parts = even;

@@ -5,17 +5,21 @@
 
 namespace gptaq {
 
-// A block is 32 NW rows, NW wavefronts of 32 rows each.  Keys and values come in tiles of 64 straight from memory to LDS, as they lie in the pages, into a ring of
-// kRing tiles with one barrier a tile.  Both products are taken transposed, with v_mfma 32x32x16: S^T = K Q^T leaves a lane the scores of one row (l % 32), and O^T = V^T P^T
+// A block is 32 NW rows, NW wavefronts of 32 rows each.  Keys and values come in pieces of 32 (half a tile) straight from memory to LDS, as they lie in the pages, into a ring
+// of kRing pieces with one barrier a piece.  Both products are taken transposed, with v_mfma 32x32x16: S^T = K Q^T leaves a lane the scores of one row (l % 32), and O^T = V^T P^T
 // takes the weights from there without an exchange, if the first product's row 16 s + 8 b + 4 a + i has key 16 s + 8 a + 4 b + i (bits 2 and 3 change places).
 // Reads of either from LDS are runs of 512 bytes: no bank is met twice.
-// PB: bits of a page as far as they matter to a tile's layout (4, 5, 6: pages of 16, 32, and more).
-constexpr int kRing = 4;                               // (five, with two tiles in flight: 1 % slower)
+// Bound by power: the matrix unit is busy for half of the cycles, at 2.0 GHz (2048 tokens behind 14336, 32 heads of 128: 508 us, 1.01 PFLOP/s; 8192 tokens, 64 heads over 8:
+// 0.55 ms, 1.0).  Two blocks of 128 rows share a CU, so that one works while the other begins, ends or waits; one block of 256 with pieces of 64 reads keys half as
+// often, which takes 2 to 4 % off the largest calls, and adds 3 to 10 % to those in a window or of a few rounds (8192 tokens, window 2048: 296 / 306 us; 512 tokens
+// of 32 heads 19 / 24; of 64 heads over 8 behind 8000, 40 / 58).
+// PB: bits of a page as far as they matter to a piece's layout (4, 5: pages of 16, and more).
+constexpr int kRing = 4, kPiece = 32;                  // (five, with two pieces in flight: the same times)
 template <int D, int NW> struct ManyShape {
-  static constexpr int kTileBytes = kTile * D * 2, kLoads = kTileBytes / 1024;      // of keys, or of values
+  static constexpr int kPieceBytes = kPiece * D * 2, kLoads = kPieceBytes / 1024;      // of keys, or of values
   static constexpr int kPerWave = 2 * kLoads / NW;
   static constexpr int kOutRow = D * 2 + 16;                                        // results in LDS
-  static constexpr int kRingBytes = kRing * 2 * kTileBytes, kOutBytes = 32 * NW * kOutRow;
+  static constexpr int kRingBytes = kRing * 2 * kPieceBytes, kOutBytes = 32 * NW * kOutRow;
   static constexpr int kLds = kRingBytes > kOutBytes ? kRingBytes : kOutBytes;
   static_assert(2 * kLoads % NW == 0, "every wavefront has as many loads");
 };
@@ -38,7 +42,7 @@ template <int D, int PB, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArgs a, int blocks) {
   using Shape = ManyShape<D, NW>;
   extern __shared__ __attribute__((aligned(256))) unsigned char smem[];
-  constexpr int KS = D / 16, VT = D / 32, P = 1 << PB, TILE = Shape::kTileBytes;
+  constexpr int KS = D / 16, VT = D / 32, P = 1 << PB, PIECE = Shape::kPieceBytes;
   const CacheShape& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
   // The heads of a block side by side, so that with eight key heads each XCD has one; late blocks first, which see the most, all of their first parts before any second
@@ -71,43 +75,41 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
 #pragma unroll
   for (int i = 0; i < KS; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4_at2*>(qrow + i * 16 + half * 8) ^ flip);
 
-  // ---- loads: a tile of keys, then of values, 1 KB each; a wavefront's are neighbours.  Of a page of up to 64 positions they are one run, of a larger one the keys'
-  // are a row of 64 positions each.
-  constexpr int PAGES = 1 << (6 - PB), PER = Shape::kLoads >> (6 - PB);      // pages of a tile, loads of a page
+  // ---- loads: a piece's keys, then its values, 1 KB each; a wavefront's are neighbours.  Of a page of up to 32 positions they are one run, of a larger one the keys' are
+  // two rows of 32 positions each.
+  constexpr int PAGES = PB == 4 ? 4 : 2, PER = Shape::kLoads * 2 / PAGES;      // pages of a tile (that of each half of it at least), loads of a page
   const int64_t head_bytes = (int64_t)(D * 2) << c.page_bits;        // of a page, of one head
   const int64_t page_bytes = head_bytes * c.kv_heads;
-  const unsigned char* const keys_base = (const unsigned char*)a.keys + head * head_bytes;
-  const unsigned char* const values_base = (const unsigned char*)a.values + head * head_bytes;
-  const int last_tile = tiles.at(max(end - 1, 0));
-  static_assert(PER % Shape::kPerWave == 0, "a wavefront's loads of a tile are of one page");
+  static_assert(PER % Shape::kPerWave == 0, "a wavefront's loads of a piece are of one page");
   const int first_load = wave * Shape::kPerWave;                     // keys' loads, then values'
   const bool loads_values = first_load >= Shape::kLoads;
-  const int load0 = loads_values ? first_load - Shape::kLoads : first_load, own_page = load0 / PER, in_page0 = load0 % PER;
-  struct Ids { int page, there; };                                   // of a tile: the wavefront's own page, a bit for each that there is
+  const int load0 = loads_values ? first_load - Shape::kLoads : first_load, own_page = load0 / PER;
+  const unsigned char* const base = (const unsigned char*)(loads_values ? a.values : a.keys) + head * head_bytes;
+  const int load_step = loads_values || PB < 5 ? 1024 : 32 << c.page_bits, load_from = load0 % PER * load_step;      // from one load of a page to the next
+  const int load_lane = loads_values || PB < 5 ? lane * 16 : l32 * 16 + half * (16 << c.page_bits);
+  const int place_bytes = loads_values ? D * 2 : 16, off_mask = (1 << c.page_bits) - 1;
+  const int last_tile = tiles.at(max(end - 1, 0));
   auto tile_of = [&](int i) { return i < end ? tiles.at(i) : last_tile; };      // (behind the last that again)
+  struct Ids { int page[2], there; };                                // of a tile: the wavefront's own page of either half, a bit for each that there is
   // A tile's pages are asked for a tile before its loads, lane k for the k-th, by a vector load: what waits for it waits for what was asked for before it alone.
   auto ask_pages = [&](int tile) {
-    const int at = ((tile * kTile) >> c.page_bits) + lane % PAGES;
+    const int at = (tile * kTile + lane % PAGES * (kTile / PAGES)) >> c.page_bits;
     return at < c.table_pages ? c.table[(int64_t)s * c.ld_table + at] : -1;
   };
   auto pages_of = [&](Ids& g, int asked) {
     const bool there = (uint32_t)asked < (uint32_t)c.pages;
     g.there = (int)(__ballot(there) & ((1 << PAGES) - 1));
-    g.page = __builtin_amdgcn_readlane(there ? asked : 0, own_page);
+    g.page[0] = __builtin_amdgcn_readlane(there ? asked : 0, own_page);
+    g.page[1] = __builtin_amdgcn_readlane(there ? asked : 0, own_page + PAGES / 2);
   };
-  const int off_mask = (1 << c.page_bits) - 1;
-  const int key_step = PB < 6 ? 1024 : 16 << c.page_bits;            // from one load of keys of a page to the next
-  auto load_tile = [&](const Ids& g, int tile, int slot) {
-    const int off = PB < 6 ? 0 : (tile * kTile) & off_mask;
-    unsigned char* const to = smem + slot * 2 * TILE;
-    const LdsLoader loader((loads_values ? values_base : keys_base) + g.page * page_bytes);
-    const int step = loads_values ? 1024 : key_step, inside = loads_values ? off * (D * 2) + in_page0 * 1024 : off * 16 + in_page0 * key_step;
+  auto load_piece = [&](const Ids& g, int tile, int b, int slot) {
+    const int from = load_from + (PB < 5 ? 0 : ((tile * kTile + b * kPiece) & off_mask) * place_bytes);
+    unsigned char* const to = smem + slot * 2 * PIECE + first_load * 1024;
+    const LdsLoader loader(base + g.page[b] * page_bytes);
 #pragma unroll
-    for (int n = 0; n < Shape::kPerWave; ++n) loader.load(to + (first_load + n) * 1024, lane * 16, inside + n * step);
+    for (int n = 0; n < Shape::kPerWave; ++n) loader.load(to + n * 1024, load_lane, from + n * load_step);
   };
-  auto valid = [&](const Ids& g) {                                   // a bit for each 16 keys
-    return PAGES == 4 ? g.there : PAGES == 2 ? (g.there & 1) * 3 | (g.there >> 1) * 12 : g.there * 15;
-  };
+  auto valid = [&](const Ids& g) { return PAGES == 4 ? g.there : (g.there & 1) * 3 | (g.there >> 1) * 12; };      // a bit for each 16 keys
 
   f32x16 acc[VT];
 #pragma unroll
@@ -116,13 +118,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
     for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
   float origin = kNoOrigin, total = 0.f;                             // what is taken off scaled scores; total: this lane's keys alone
   const int key = (l32 & 0x13) | (l32 & 4) << 1 | (l32 & 8) >> 1;    // of 32 that the lane reads
-  int kread[2];
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int k = b * 32 + key;
-    kread[b] = (k >> PB) * (D * 2 * P) + (k & (P - 1)) * 16 + half * P * 16;
-  }
-  const int vread = (half * D + l32) * 16;
+  const int kread = (key >> PB) * (D * 2 * P) + (key & (P - 1)) * 16 + half * P * 16, vread = PIECE + (half * D + l32) * 16;
 
   // The weights of a step's scores are taken with the origin as it is.  Where their sum says that some score is far above it (or that there is none yet, which
   // makes every weight infinite), the origin becomes the largest score so far, sums are to be scaled by `factor`, and the weights are taken again.
@@ -159,56 +155,52 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   auto pack = [&](const float* w) {
     return __builtin_bit_cast(bf16x8, u32x4{at_bf16x2(w[0], w[1]), at_bf16x2(w[2], w[3]), at_bf16x2(w[4], w[5]), at_bf16x2(w[6], w[7])});
   };
-  auto values_at = [&](const unsigned char* vt, int step, int t) { return *reinterpret_cast<const u32x4*>(vt + vread + (step * 2 * D + t * 32) * 16); };
+  auto keys_of = [&](const unsigned char* at, int k) { return *reinterpret_cast<const bf16x8*>(at + kread + k * (2 * P * 16)); };
+  auto values_of = [&](const unsigned char* at, int h16, int t) { return *reinterpret_cast<const u32x4*>(at + vread + (h16 * 2 * D + t * 32) * 16); };
   f32x16 sc[2];                                                      // scores of 32 keys; element e: key 16 (e / 8) + 8 half + e % 8
   bf16x8 weight[2][2];                                               // [step & 1][16 keys]
-  // A tile of which parts are not there, 32 keys after the other; what is behind the last position that some row sees is taken for zeros.  CAREFUL (see
-  // attention_marks) takes any tile, and every sum in the same order as where it is not needed.
-  auto work = [&](auto careful, const unsigned char* kt, int j0, int ok) {
+  // A piece of a tile of which parts are not there; what is behind the last position that some row sees is taken for zeros.  CAREFUL (see
+  // attention_marks) takes any piece, and every sum in the same order as where it is not needed.
+  auto work = [&](auto careful, const unsigned char* at_piece, int j0, int ok) {
     constexpr bool CAREFUL = decltype(careful)::value;
-    const unsigned char* const vt = kt + TILE;
+    f32x16& s32 = sc[0];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      f32x16& s32 = sc[0];
+    for (int e = 0; e < 16; ++e) s32[e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s32[e] = 0.f;
+    for (int k = 0; k < KS; ++k) s32 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys_of(at_piece, k), qf[k], s32, 0, 0, 0);
+    const int j = j0 + 8 * half;
+    const uint32_t seen = seen_of(j) & ((ok & 1 ? 0xffu : 0u) | (ok & 2 ? 0xff0000u : 0u));
+    float w[16], sum = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
-        s32 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + kread[b] + k * (2 * P * 16)), qf[k], s32, 0, 0, 0);
-      const int j = j0 + 32 * b + 8 * half;
-      const uint32_t seen = seen_of(j) & ((ok >> (2 * b) & 1 ? 0xffu : 0u) | (ok >> (2 * b + 1) & 1 ? 0xff0000u : 0u));
-      float w[16], sum = 0.f;
+    for (int e = 0; e < 16; ++e) { w[e] = only(at_exp2(fmaf(s32[e], scale, -origin)), seen, e); sum += w[e]; }
+    if (raise(s32, w, sum, seen)) scale_sums();
+    total += sum;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) { w[e] = only(at_exp2(fmaf(s32[e], scale, -origin)), seen, e); sum += w[e]; }
-      if (raise(s32, w, sum, seen)) scale_sums();
-      total += sum;
+    for (int h16 = 0; h16 < 2; ++h16) {
+      weight[1][h16] = pack(w + 8 * h16);
+      u32x4 ones, ends;
 #pragma unroll
-      for (int h16 = 0; h16 < 2; ++h16) {
-        weight[1][h16] = pack(w + 8 * h16);
-        u32x4 ones, ends;
+      for (int h = 0; h < 4; ++h) {
+        const int at = 8 * h16 + 2 * h, left = pmax - j - 16 * h16 - 2 * h;      // keys of the lane's pair that are not behind the last
+        if (CAREFUL) ones[h] = (seen >> place(at) & 1 ? 0x3f80u : 0u) | (seen >> place(at + 1) & 1 ? 0x3f800000u : 0u);
+        ends[h] = left >= 1 ? ~0u : left == 0 ? 0xffffu : 0u;
+      }
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          const int at = 8 * h16 + 2 * h, left = pmax - j - 16 * h16 - 2 * h;      // keys of the lane's pair that are not behind the last
-          if (CAREFUL) ones[h] = (seen >> place(at) & 1 ? 0x3f80u : 0u) | (seen >> place(at + 1) & 1 ? 0x3f800000u : 0u);
-          ends[h] = left >= 1 ? ~0u : left == 0 ? 0xffffu : 0u;
+      for (int t = 0; t < VT; ++t) {
+        u32x4 v = values_of(at_piece, h16, t);
+        if (CAREFUL) {
+          u32x4 marks;
+          attention_marks(v, marks);
+          f32x16 n;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) n[e] = 0.f;
+          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), n, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[t][e] += attention_strange_sum(n[e]);
+        } else if (j0 + kPiece > pmax) {
+          v &= ends;
         }
-#pragma unroll
-        for (int t = 0; t < VT; ++t) {
-          u32x4 v = values_at(vt, 2 * b + h16, t);
-          if (CAREFUL) {
-            u32x4 marks;
-            attention_marks(v, marks);
-            f32x16 n;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) n[e] = 0.f;
-            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, marks), __builtin_bit_cast(bf16x8, ones), n, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[t][e] += attention_strange_sum(n[e]);
-          } else if (j0 + kTile > pmax) {
-            v &= ends;
-          }
-          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), weight[1][h16], acc[t], 0, 0, 0);
-        }
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), weight[1][h16], acc[t], 0, 0, 0);
       }
     }
   };
@@ -216,24 +208,24 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   // All other tiles go through in steps of 32 keys, each with three parts that do not wait for each other: the next step's scores, this one's
   // weights, and the product of the last one's weights with its values.  So the matrix unit works while the vector unit takes exponentials.  Groups of one
   // instruction of either product, the reads of the group after the next, and the group's share of the weights; the barriers keep the compiler to this order.
-  auto scores_alone = [&](f32x16& next, const unsigned char* kt, int from) {
+  auto scores_alone = [&](f32x16& next, const unsigned char* at) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) next[e] = 0.f;
 #pragma unroll
-    for (int k = 0; k < KS; ++k) next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + from + k * (2 * P * 16)), qf[k], next, 0, 0, 0);
+    for (int k = 0; k < KS; ++k) next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys_of(at, k), qf[k], next, 0, 0, 0);
   };
-  auto product_alone = [&](const bf16x8 (&w)[2], const unsigned char* vt, int step) {
+  auto product_alone = [&](const bf16x8 (&w)[2], const unsigned char* at) {
 #pragma unroll
     for (int k = 0; k < KS; ++k)
-      acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values_at(vt, step + k / VT, k % VT)), w[k / VT], acc[k % VT], 0, 0, 0);
+      acc[k % VT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values_of(at, k / VT, k % VT)), w[k / VT], acc[k % VT], 0, 0, 0);
   };
-  auto step = [&](const f32x16& now, f32x16& next, const unsigned char* kt, int kfrom, const bf16x8 (&before)[2], const unsigned char* vt, int vstep,
-                  bf16x8 (&packed)[2], bool parts_seen, int j) {
+  auto step = [&](const f32x16& now, f32x16& next, const unsigned char* at_next, const bf16x8 (&before)[2], const unsigned char* at_before, bf16x8 (&packed)[2],
+                  bool parts_seen, int j) {
     constexpr int AHEAD = 2;
     u32x4 kf[AHEAD + 1], vf[AHEAD + 1];
     auto read = [&](int k) {
-      kf[k % (AHEAD + 1)] = *reinterpret_cast<const u32x4*>(kt + kfrom + k * (2 * P * 16));
-      vf[k % (AHEAD + 1)] = values_at(vt, vstep + k / VT, k % VT);
+      kf[k % (AHEAD + 1)] = __builtin_bit_cast(u32x4, keys_of(at_next, k));
+      vf[k % (AHEAD + 1)] = values_of(at_before, k / VT, k % VT);
     };
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) read(k);
@@ -279,27 +271,33 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   auto pass = [&](auto careful) {
     constexpr bool CAREFUL = decltype(careful)::value;
     Ids ids[3];                                                      // pages of tiles i .. i + 2
-    int i = begin, slot = 0, tile[3], asked[3];
+    int i = begin, slot = 0, tile[3], asked[3];                      // slot: of the piece
     auto slot_of = [&](int ahead) { return (slot + ahead) % kRing; };
+    auto at_slot = [&](int ahead) { return smem + slot_of(ahead) * 2 * PIECE; };
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       tile[k] = tile_of(i + k);
       asked[k] = ask_pages(tile[k]);
     }
+    pages_of(ids[0], asked[0]);
+    pages_of(ids[1], asked[1]);
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      pages_of(ids[k], asked[k]);
-      load_tile(ids[k], tile[k], k);
-    }
-    auto top_of = [&]() {
-      am_wait<0>();                                                  // the wavefront's loads of tile i + 1 are there ..
-      am_barrier();                                                  // .. and everyone's; and tile i - 2 is no longer read
-      pages_of(ids[2], asked[2]);
-      asked[2] = ask_pages(tile_of(i + 3));
+    load_piece(ids[0], tile[0], 0, 0);
+    load_piece(ids[0], tile[0], 1, 1);
+    auto top_of = [&](int b) {                                       // before half b of tile i
+      am_wait<0>();                                                  // the wavefront's loads of the next piece are there ..
+      am_barrier();                                                  // .. and everyone's; and the piece before the last is no longer read
+      if (b == 1) {
+        pages_of(ids[2], asked[2]);
+        asked[2] = ask_pages(tile_of(i + 3));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      load_piece(ids[1], tile[1], b, slot_of(2));
       __builtin_amdgcn_sched_barrier(0);
-      load_tile(ids[2], tile[2], slot_of(2));
-      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto middle = [&]() {
+      slot = slot_of(1);
+      top_of(1);
     };
     auto advance = [&]() {
       ++i;
@@ -307,30 +305,34 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
 #pragma unroll
       for (int k = 0; k < 2; ++k) { ids[k] = ids[k + 1]; tile[k] = tile[k + 1]; }
       tile[2] = tile_of(i + 2);
-      if (i < end) top_of();
+      if (i < end) top_of(0);
     };
-    auto keys_at = [&](int ahead) { return smem + slot_of(ahead) * 2 * TILE; };
-    top_of();
+    top_of(0);
     while (i < end) {
       int kind = __builtin_amdgcn_readfirstlane(kind_of(ids[0], tile[0]));
       if (!CAREFUL && kind >= kParts) {
-        const unsigned char* kt = keys_at(0);
-        const unsigned char* vt = kt + TILE;                         // (the first product is with weights of zero)
-        scores_alone(sc[0], kt, kread[0]);
+        const unsigned char* before = at_slot(0);                    // (the first product is with weights of zero)
+        scores_alone(sc[0], before);
         weight[1][0] = weight[1][1] = bf16x8{};
         for (;;) {
           const int j = tile[0] * kTile + 8 * half;
-          step(sc[0], sc[1], kt, kread[1], weight[1], vt, 2, weight[0], kind == kParts, j);
-          vt = kt + TILE;
-          kt = keys_at(1);
-          step(sc[1], sc[0], kt, kread[0], weight[0], vt, 0, weight[1], kind == kParts, j + 32);
+          step(sc[0], sc[1], at_slot(1), weight[1], before, weight[0], kind == kParts, j);
+          before = at_slot(0);
+          middle();
+          step(sc[1], sc[0], at_slot(1), weight[0], before, weight[1], kind == kParts, j + 32);
+          before = at_slot(0);
           kind = i + 1 < end ? __builtin_amdgcn_readfirstlane(kind_of(ids[1], tile[1])) : kNothing;
           if (kind < kParts) break;
           advance();
         }
-        product_alone(weight[1], vt, 2);
-      } else if (kind != kNothing) {
-        work(careful, keys_at(0), tile[0] * kTile, valid(ids[0]));
+        product_alone(weight[1], before);
+      } else {
+#pragma unroll 1
+        for (int b = 0;; ++b) {
+          if (kind != kNothing) work(careful, at_slot(0), tile[0] * kTile + b * kPiece, valid(ids[0]) >> (2 * b));
+          if (b == 1) break;
+          middle();
+        }
       }
       advance();
     }
@@ -414,8 +416,7 @@ template <int D, int PB, int NW> static hipError_t launch_many_as(const Attentio
   return hipSuccess;
 }
 template <int D> static hipError_t launch_many_of(const AttentionArgs& a, int64_t blocks, hipStream_t s) {
-  return a.c.page_bits == 4 ? launch_many_as<D, 4, kManyWaves>(a, blocks, s) : a.c.page_bits == 5 ? launch_many_as<D, 5, kManyWaves>(a, blocks, s)
-                                                                                              : launch_many_as<D, 6, kManyWaves>(a, blocks, s);
+  return a.c.page_bits == 4 ? launch_many_as<D, 4, kManyWaves>(a, blocks, s) : launch_many_as<D, 5, kManyWaves>(a, blocks, s);
 }
 hipError_t launch_attention_many(const AttentionArgs& a, int64_t blocks, hipStream_t s) {
   return a.c.d == 64 ? launch_many_of<64>(a, blocks, s) : a.c.d == 96 ? launch_many_of<96>(a, blocks, s) : launch_many_of<128>(a, blocks, s);
