@@ -254,7 +254,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 }
 
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
-constexpr int64_t kMostParts = 64, kFewBits = 4, kPartialRows = 65536;
+constexpr int64_t kMostParts = 64, kPartialRows = 65536;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
 // Blocks of few rows read the keys once for 16 rows, and little else bounds them; blocks of many read them once for 128, and take longer to begin and end.  So calls are of
 // few as long as their blocks' tiles, with nine for what a block costs besides, are kFewWork at most, and where a sequence has 16 rows at most.  us a call of few / many, rows of a
