@@ -45,13 +45,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   constexpr int KS = D / 16, VT = D / 32, P = 1 << PB, PIECE = Shape::kPieceBytes;
   const CacheShape& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
-  // The heads of a block side by side, so that with eight key heads each XCD has one; late blocks first, which see the most, all of their first parts before any second
-  // one: workgroups that find nothing to do come last (they go to the shader engines in turn, and between others they would leave CUs idle).
+  // The heads of a block side by side, so that with eight key heads each XCD has one; late blocks first, which see the most.
   const int head = (int)(blockIdx.x % (unsigned)c.kv_heads), rest = (int)(blockIdx.x / (unsigned)c.kv_heads);
-  const int part = rest / blocks;
-  const Dealt dealt = cache_deal(c, a.first_block + rest % blocks, a.rows_bits, true);
+  const Dealt dealt = cache_deal(c, rest, a.first_block, blocks, a.parts, a.rows_bits);
   if (dealt.block < 0) return;
-  const int s = dealt.sequence;
+  const int s = dealt.sequence, part = dealt.part;
   const Sequence seq = cache_sequence(c, s);
   const int rows = seq.count * c.group;
   if (((int64_t)dealt.block << a.rows_bits) >= rows) return;         // (starts that do not ascend)
