@@ -201,58 +201,86 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) 
   }
 }
 
-// The parts of a row, a wavefront a row.  Latency: 3.2 us behind one token's few blocks, 5.5 behind 64 sequences'.  (32 parts at a time instead of eight: the same.)
-template <int D>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, int64_t first_row) {
+// The parts of a row, L lanes a row; a wavefront has 64 / L heads of a token.  Bound by the instructions of a row, and by latency where rows are few.  us, 64 / 32 / 16 lanes: 16384 rows of two
+// parts 11.7 / 9.6 / 8.6, 32768 21.4 / 12.2 / 10.4; with the kernel before it, one token of 64 heads over 8 behind 8000 14.5 / 14.8 / 16.2, of 32 heads in a window of 1024 10.7 / 10.7 / 10.9.
+template <int D, int L>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, int64_t first, int64_t items) {
   const CacheShape& c = a.c;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = first_row + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (int64_t)c.tokens * c.heads;
-  if (row >= rows) return;
-  const int token = (int)(row / c.heads), h = (int)(row % c.heads);
-  const int s = cache_find(c, token, 1, 0, 0);
-  const Sequence seq = cache_sequence(c, s);
+  const int lane = threadIdx.x & 63, in_row = lane & (L - 1), groups = (c.heads + 64 / L - 1) / (64 / L);
+  const int64_t item = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rows = (int64_t)c.tokens * c.heads;
+  if (item >= items) return;
+  const int token = (int)((uint32_t)item / (uint32_t)groups), h = (int)((uint32_t)item % (uint32_t)groups) * (64 / L) + lane / L;      // (rows are 2^30 at most)
+  const Sequence seq = cache_sequence(c, cache_find(c, token, 1, 0, 0));
   const int in_seq = token - seq.first;
-  if (in_seq < 0 || in_seq >= seq.count) return;                     // (no sequence's)
+  if (in_seq < 0 || in_seq >= seq.count || h >= c.heads) return;     // (no sequence's)
   // as the block of this row dealt its tiles out
   const int rows_seq = seq.count * c.group, row0 = (in_seq * c.group + h % c.group) >> a.rows_bits << a.rows_bits;
   const int last = min(row0 + (1 << a.rows_bits) - 1, rows_seq - 1);
   const Parts parts = attention_parts(a, attention_tiles(a, seq.before + row0 / c.group, seq.before + last / c.group).count);
   if (parts.count <= 1) return;
-  // a lane has the statistics of a part (there are 64 at most), and all lanes a share of every part's sums, eight parts at a time
+  // a lane has the statistics of every L-th part (there are 64 at most), and a share of every part's sums
   typedef __attribute__((ext_vector_type(2))) float f32x2;
-  f32x2 st = {-__builtin_inff(), 0.f};
-  if (lane < parts.count) st = *reinterpret_cast<const f32x2*>(a.stats + (lane * rows + row) * 2);
-  float m = st[0];
+  const int64_t row = (int64_t)token * c.heads + h;
+  constexpr int S = 64 / L;
+  f32x2 st[S];
+  float m = -__builtin_inff(), sum = 0.f, mine[S];
 #pragma unroll
-  for (int k = 1; k < 64; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
-  const float mine = lane < parts.count ? at_factor(st[0], m) : 0.f;
-  float sum = mine * st[1];
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
-  constexpr int N = (D + 63) / 64;
-  float o[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) o[k] = 0.f;
-  const float* const from = a.partial + row * D + lane;
-  for (int i0 = 0; i0 < parts.count; i0 += 8) {
-    float v[8][N];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int k = 0; k < N; ++k) v[i][k] = i0 + i < parts.count && (D % 64 == 0 || k * 64 + lane < D) ? from[(i0 + i) * rows * D + k * 64] : 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float factor = __shfl(mine, i0 + i);
-#pragma unroll
-      for (int k = 0; k < N; ++k)
-        if (i0 + i < parts.count) o[k] += factor * v[i][k];
-    }
+  for (int k = 0; k < S; ++k) {
+    st[k] = f32x2{-__builtin_inff(), 0.f};
+    if (L * k + in_row < parts.count) st[k] = *reinterpret_cast<const f32x2*>(a.stats + ((L * k + in_row) * rows + row) * 2);
+    m = fmaxf(m, st[k][0]);
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint16_t* const to = a.out + (int64_t)token * a.ldo + (int64_t)h * a.ho;
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-    if (D % 64 == 0 || k * 64 + lane < D) to[k * 64 + lane] = __builtin_bit_cast(uint16_t, (__bf16)(o[k] * inv));
+  for (int k = 1; k < L; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
+#pragma unroll
+  for (int k = 0; k < S; ++k) {
+    mine[k] = L * k + in_row < parts.count ? at_factor(st[k][0], m) : 0.f;
+    sum += mine[k] * st[k][1];
+  }
+#pragma unroll
+  for (int k = 1; k < L; k *= 2) sum += __shfl_xor(sum, k);
+  constexpr int E = D / L % 4 == 0 ? 4 : D / L % 2 == 0 ? 2 : 1, N = D / L / E;
+  typedef __attribute__((ext_vector_type(E))) float Entries;
+  Entries o[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) o[k] = Entries(0.f);
+  const float* const from = a.partial + row * D + in_row * (D / L);
+  auto add = [&](int count) {
+    for (int i0 = 0; i0 < count; i0 += 8) {
+      Entries v[8][N];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          v[i][k] = i0 + i < count ? *reinterpret_cast<const Entries*>(from + (i0 + i) * rows * D + E * k) : Entries(0.f);
+      float factors = mine[0];
+#pragma unroll
+      for (int k = 1; k < S; ++k) factors = i0 >= L * k ? mine[k] : factors;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float factor = __shfl(factors, (lane & -L) + (i0 & (L - 1)) + i);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          if (i0 + i < count) o[k] += factor * v[i][k];
+      }
+    }
+  };
+  const int count = __builtin_amdgcn_readfirstlane(parts.count);      // (a token's heads mostly are of one block, or of blocks alike)
+  if (__ballot(parts.count != count)) add(parts.count);
+  else add(count);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t* const to = a.out + (int64_t)token * a.ldo + (int64_t)h * a.ho + in_row * (D / L);
+  typedef uint32_t __attribute__((aligned(2))) u32_at2;
+  float y[D / L];
+#pragma unroll
+  for (int k = 0; k < D / L; ++k) y[k] = ((const float*)o)[k] * inv;
+  if (D / L % 2 == 0) {
+#pragma unroll
+    for (int k = 0; k < D / L; k += 2) *reinterpret_cast<u32_at2*>(to + k) = at_bf16x2(y[k], y[k + 1]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < D / L; ++k) to[k] = __builtin_bit_cast(uint16_t, (__bf16)y[k]);
+  }
 }
 
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
@@ -270,10 +298,11 @@ struct Plan { int bits; int64_t parts; int min_tiles; };
 // sequences of up to 1000 positions 30.0 / 35.5 / 43.7 (those that find nothing to do take a microsecond, too), of up to 8191 245 / 241 / 234; 8 heads, 8 of up to 16000
 // 70.8 / 73.7 / 73.4.  Tiles at least, 2 / 4 / 9: 32 heads, one sequence of 200 8.1 / 5.8 / 7.5, a window of 1024 11.4 / 10.7 / 12.9; 64 over 8, 8000 18.4 / 16.0 / 15.4.
 static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t most_tiles) {
-  const int64_t group = heads / kv_heads, sixteens = ((tokens * group - 1) >> kFewBits) + 1;
-  const bool many = tokens * group > 16 * seqs && (sixteens > seqs ? sixteens : seqs) * kv_heads * (most_tiles + 9) > kFewWork;
+  const int64_t rows = (tokens * (heads / kv_heads) - 1) / seqs + 1;      // of a sequence and key head, on average
+  auto blocks_of = [&](int bits) { return (((rows - 1) >> bits) + 1) * seqs * kv_heads; };
+  const bool many = rows > 16 && blocks_of(kFewBits) * (most_tiles + 9) > kFewWork;
   const int bits = many ? kManyBits : kFewBits;
-  const int64_t full = ((tokens * group - 1) >> bits) + 1, blocks = (full > seqs ? full : seqs) * kv_heads, min_tiles = many ? 8 : 4;
+  const int64_t blocks = blocks_of(bits), min_tiles = many ? 8 : 4;
   int64_t parts = 512 / blocks, even = 2048 / blocks;
   if (parts > (most_tiles + min_tiles - 1) / min_tiles) parts = (most_tiles + min_tiles - 1) / min_tiles;
   if (even > most_tiles / 32) even = most_tiles / 32;
@@ -297,10 +326,11 @@ static hipError_t launch_attention(const AttentionArgs& all, hipStream_t s) {
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   if (a.parts == 1) return hipSuccess;
-  const int64_t rows = (int64_t)a.c.tokens * a.c.heads;
-  for (int64_t first = 0; first < rows; first += (int64_t)1 << 25) {
-    const int64_t n = rows - first < ((int64_t)1 << 25) ? rows - first : (int64_t)1 << 25;
-    hipLaunchKernelGGL(attention_join_kernel<D>, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, a, first);
+  constexpr int kLanes = 32;
+  const int64_t items = (int64_t)a.c.tokens * ((a.c.heads + 64 / kLanes - 1) / (64 / kLanes)), each_launch = (int64_t)1 << 25;
+  for (int64_t first = 0; first < items; first += each_launch) {
+    const int64_t n = items - first < each_launch ? items - first : each_launch;
+    hipLaunchKernelGGL((attention_join_kernel<D, kLanes>), dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, a, first, items);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   return hipSuccess;
