@@ -288,22 +288,35 @@ constexpr int64_t kMostParts = 64, kPartialRows = 65536;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
 // Blocks of few rows read the keys once for 16 rows, and little else bounds them; blocks of many read them once for 128, and take longer to begin and end.  So calls are of
 // few as long as their blocks' tiles, with nine for what a block costs besides, are kFewWork at most, and where a sequence has 16 rows at most.  us a call of few / many, rows of a
-// sequence and key head: 32 heads behind 2000 positions (23k at 256 rows), 64 16.3 / 22.5, 256 26 / 35, 384 41 / 39, 1024 105 / 78; 64 heads over 8 behind 8000 (18k at 256), 256 28 / 35, 384 47 / 38;
-// four sequences of these behind 4000, 128 30.6 / 32.6 (19k), 192 38 / 36.5 (28k); sixteen, 32 heads over 8 behind 2000, 64 29 / 34 (22k), 96 45 / 39 (32k); 64 behind 500, 48 36 / 25 (28k);
-// 64 behind 8000, 64 heads over 8, 16 324 / 301, 32 408 / 319, 96 724 / 342; 32 heads with no positions before, 512 14 / 19, 768 23 / 34 (33k).
+// sequence and key head (and that number): 32 heads behind 2000 positions 96 19.6 / 25.6 (8k), 256 25.8 / 32.5 (23k), 512 51 / 46 (50k); 64 heads over 8 behind 8000, 256 27.7 / 29.5 (17k), 384
+// 47 / 35 (26k); four sequences of these behind 4000, 128 30 / 31 (18k), 256 44 / 41 (37k); sixteen, 32 heads over 8 behind 2000, 64 29.5 / 33.5 (21k), 96 45 / 37 (31k); 64 behind 500, 32 26 / 22
+// (17k), 48 37 / 24 (26k); 32 heads with no positions before, 512 14.5 / 19 (17k), 768 23 / 24.5 (32k); 64 behind 8000, 64 heads over 8, 16 324 / 301, 32 408 / 319, 96 724 / 342.
 constexpr int64_t kFewWork = 22000;
 struct Plan { int bits; int64_t parts; int min_tiles; };
-// Rows of a block, and parts of the keys.  Blocks of many rows: for two workgroups a CU, of 8 tiles at least.  Blocks of few rows: for two a CU, of 4 tiles at least, or, which
+// Rows of a block, and parts of the keys.  Blocks of many rows: the parts, of 8 tiles at least, that take the least time by what calls were measured to take: a tile 1.6 us where no CU has two
+// blocks, 2.35 where all have; sums that are joined 3.5 us, and their rows' and bytes' time.  us a call, as many parts as make two blocks a CU / these: three sequences of 256 tokens behind 600, 32 heads
+// 37 (2) / 29 (1); sixteen of 64 behind 2000, 32 heads over 8 60 (2) / 55 (1); 1024 tokens of 32 heads 41 (2) / 30 (1); 96 of 64 heads over 8 behind 8000 47 / 47 (8).
+// Blocks of few rows: for two a CU, of 4 tiles at least, or, which
 // evens sequences of different lengths out, for eight a CU of 32 tiles at least.  us a call, room for 512 / 1024 / 2048 workgroups of 4 tiles: 64 heads over 8 of 128, 64
 // sequences of up to 1000 positions 30.0 / 35.5 / 43.7 (those that find nothing to do take a microsecond, too), of up to 8191 245 / 241 / 234; 8 heads, 8 of up to 16000
 // 70.8 / 73.7 / 73.4.  Tiles at least, 2 / 4 / 9: 32 heads, one sequence of 200 8.1 / 5.8 / 7.5, a window of 1024 11.4 / 10.7 / 12.9; 64 over 8, 8000 18.4 / 16.0 / 15.4.
-static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t most_tiles) {
+static int64_t many_parts(int64_t blocks, int64_t rows, int64_t tiles, int64_t d) {
+  int64_t best = 1;
+  double least = 1e30;
+  for (int64_t parts = 1; parts <= kMostParts && (parts == 1 || (parts * blocks <= 512 && tiles / parts >= 8)); ++parts) {
+    const double each = (double)((tiles + parts - 1) / parts), groups = (double)(parts * blocks);
+    const double us = (groups <= 256 ? 1.6 : groups <= 512 ? 2.35 : 2.35 * groups / 512) * each + (parts > 1 ? 3.5 + (double)rows * (2e-4 + (double)(parts * d) * 4 / 7.3e6) : 0);
+    if (us < least) { least = us; best = parts; }
+  }
+  return best;
+}
+static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t d, int64_t most_tiles) {
   const int64_t rows = (tokens * (heads / kv_heads) - 1) / seqs + 1;      // of a sequence and key head, on average
   auto blocks_of = [&](int bits) { return (((rows - 1) >> bits) + 1) * seqs * kv_heads; };
   const bool many = rows > 16 && blocks_of(kFewBits) * (most_tiles + 9) > kFewWork;
   const int bits = many ? kManyBits : kFewBits;
   const int64_t blocks = blocks_of(bits), min_tiles = many ? 8 : 4;
-  int64_t parts = 512 / blocks, even = 2048 / blocks;
+  int64_t parts = many ? many_parts(blocks, tokens * heads, most_tiles, d) : 512 / blocks, even = 2048 / blocks;
   if (parts > (most_tiles + min_tiles - 1) / min_tiles) parts = (most_tiles + min_tiles - 1) / min_tiles;
   if (even > most_tiles / 32) even = most_tiles / 32;
   if (!many && parts < even) parts = even;
@@ -373,7 +386,7 @@ extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const
   // Tiles that a row can see: those of the table, or of the window (which begins and ends inside a tile, as the block's other rows have theirs) and the sinks.
   int64_t most_tiles = (cache->table_pages * cache->page + kTile - 1) / kTile;
   if (a.window && a.window / kTile + a.sinks / kTile + 4 < most_tiles) most_tiles = a.window / kTile + a.sinks / kTile + 4;
-  const Plan plan = attention_plan(tokens, seqs, heads, kv_heads, most_tiles);
+  const Plan plan = attention_plan(tokens, seqs, heads, kv_heads, d, most_tiles);
   a.rows_bits = plan.bits;
   a.parts = (int32_t)plan.parts;
   a.min_tiles = plan.min_tiles;
