@@ -15,7 +15,8 @@ struct AttentionArgs {
   int32_t parts;                       // the keys of a block of rows in so many parts at most, each of min_tiles tiles at least
   int32_t min_tiles, rows_bits;        // rows of a block (log2)
   int64_t first_block;
-  float *partial, *stats;              // [part][row of the call][d], [part][row of the call][maximum, sum]
+  int32_t mixed;                       // sequences of kFewMixed rows and fewer are taken by blocks of few rows, one a sequence, the others by blocks of many
+  float *partial, *stats;              // [part][row of the call][d], [part][row of the call][maximum, sum]; mixed, of few rows: [part][sequence][key head][row of 16]..
 };
 
 constexpr int kTile = 64;              // keys to a tile: what is dealt out
@@ -48,7 +49,7 @@ __device__ __forceinline__ int at_token(int row, int group) { return __builtin_a
 // Tiles a part has, and how many parts there are.  Blocks of few rows have no more than 20 parts unless these have 20 tiles: joining more takes longer than they save.  us,
 // one token, 64 heads over 8, with no such bound / with it: 8000 positions 15.6 / 14.6, 16000 23.2 / 19.7, 32000 33.2 / 29.7, 130000 107 / 107.
 struct Parts { int32_t each, count; };
-constexpr int kFewBits = 4;            // blocks of few rows have 16
+constexpr int kFewBits = 4, kFewMixed = 16;      // blocks of few rows have 16
 __device__ __forceinline__ Parts attention_parts(const AttentionArgs& a, int tiles) {
   const int least = a.rows_bits == kFewBits ? max(a.min_tiles, min(tiles / 20, 20)) : a.min_tiles;
   const int each = max(least, (tiles + a.parts - 1) / a.parts);

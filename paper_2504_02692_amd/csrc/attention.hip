@@ -22,11 +22,11 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) 
   const int head = (int)(blockIdx.x % (unsigned)c.kv_heads), rest = (int)(blockIdx.x / (unsigned)c.kv_heads);
   const int part = rest % a.parts;
   const int64_t block = a.first_block + rest / a.parts;
-  const int s = cache_find(c, block, c.group, 4, 1);
+  const int s = a.mixed ? (int)block : cache_find(c, block, c.group, 4, 1);
   const Sequence seq = cache_sequence(c, s);
-  const int64_t in_seq = block - cache_block_of(c, s, c.group, 4, 1);
+  const int64_t in_seq = a.mixed ? 0 : block - cache_block_of(c, s, c.group, 4, 1);
   const int rows = seq.count * c.group;
-  if (in_seq < 0 || in_seq * 16 >= rows) return;
+  if (in_seq < 0 || in_seq * 16 >= rows || (a.mixed && rows > kFewMixed)) return;
   const int row0 = (int)in_seq * 16, last = min(row0 + 15, rows - 1);
   const int pmin = seq.before + at_token(row0, c.group), pmax = seq.before + at_token(last, c.group);
   const Tiles tiles = attention_tiles(a, pmin, pmax);
@@ -175,7 +175,8 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) 
   const int64_t call_row = (int64_t)(seq.first + tok) * c.heads + head * c.group + rr % c.group;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   uint16_t* const to = a.out + (int64_t)(seq.first + tok) * a.ldo + (int64_t)(head * c.group + rr % c.group) * a.ho;
-  float* const to_part = a.partial + ((int64_t)part * c.tokens * c.heads + call_row) * D;
+  const int64_t part_row = a.mixed ? (((int64_t)part * c.seqs + s) * c.kv_heads + head) * kFewMixed + r : (int64_t)part * c.tokens * c.heads + call_row;
+  float* const to_part = a.partial + part_row * D;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
     const int e = i * 32 + e0 * 2;
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) 
     }
   }
   if (parts.count > 1 && e0 == 0) {
-    float* st = a.stats + ((int64_t)part * c.tokens * c.heads + call_row) * 2;
+    float* st = a.stats + part_row * 2;
     st[0] = m;
     st[1] = sum;
   }
@@ -206,28 +207,48 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) 
 template <int D, int L>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, int64_t first, int64_t items) {
   const CacheShape& c = a.c;
-  const int lane = threadIdx.x & 63, in_row = lane & (L - 1), groups = (c.heads + 64 / L - 1) / (64 / L);
-  const int64_t item = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rows = (int64_t)c.tokens * c.heads;
+  const int lane = threadIdx.x & 63, in_row = lane & (L - 1);
+  const int64_t item = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (item >= items) return;
-  const int token = (int)((uint32_t)item / (uint32_t)groups), h = (int)((uint32_t)item % (uint32_t)groups) * (64 / L) + lane / L;      // (rows are 2^30 at most)
-  const Sequence seq = cache_sequence(c, cache_find(c, token, 1, 0, 0));
+  int s, token, h;
+  int64_t row, step;                                                 // in the partial sums; from a part to the next
+  if (a.mixed && a.rows_bits == kFewBits) {                          // 16 rows of each sequence and key head; rows are 2^30 at most
+    constexpr uint32_t kItems = kFewMixed * L / 64;
+    const uint32_t block = (uint32_t)item / kItems, head = block % (uint32_t)c.kv_heads;
+    const int at = (int)((uint32_t)item % kItems) * (64 / L) + lane / L;
+    s = (int)(block / (uint32_t)c.kv_heads);
+    token = at / c.group;
+    h = (int)head * c.group + at % c.group;
+    row = (int64_t)block * kFewMixed + at;
+    step = (int64_t)c.seqs * c.kv_heads * kFewMixed;
+  } else {                                                           // 64 / L heads of a token
+    const uint32_t groups = (c.heads + 64 / L - 1) / (64 / L);
+    token = (int)((uint32_t)item / groups);
+    h = (int)((uint32_t)item % groups) * (64 / L) + lane / L;
+    s = cache_find(c, token, 1, 0, 0);
+    row = (int64_t)token * c.heads + h;
+    step = (int64_t)c.tokens * c.heads;
+  }
+  const Sequence seq = cache_sequence(c, s);
+  const int rows_seq = seq.count * c.group;
+  if (a.mixed && a.rows_bits == kFewBits) token += seq.first;
   const int in_seq = token - seq.first;
   if (in_seq < 0 || in_seq >= seq.count || h >= c.heads) return;     // (no sequence's)
+  if (a.mixed && (rows_seq <= kFewMixed) != (a.rows_bits == kFewBits)) return;
   // as the block of this row dealt its tiles out
-  const int rows_seq = seq.count * c.group, row0 = (in_seq * c.group + h % c.group) >> a.rows_bits << a.rows_bits;
+  const int row0 = (in_seq * c.group + h % c.group) >> a.rows_bits << a.rows_bits;
   const int last = min(row0 + (1 << a.rows_bits) - 1, rows_seq - 1);
   const Parts parts = attention_parts(a, attention_tiles(a, seq.before + row0 / c.group, seq.before + last / c.group).count);
   if (parts.count <= 1) return;
   // a lane has the statistics of every L-th part (there are 64 at most), and a share of every part's sums
   typedef __attribute__((ext_vector_type(2))) float f32x2;
-  const int64_t row = (int64_t)token * c.heads + h;
   constexpr int S = 64 / L;
   f32x2 st[S];
   float m = -__builtin_inff(), sum = 0.f, mine[S];
 #pragma unroll
   for (int k = 0; k < S; ++k) {
     st[k] = f32x2{-__builtin_inff(), 0.f};
-    if (L * k + in_row < parts.count) st[k] = *reinterpret_cast<const f32x2*>(a.stats + ((L * k + in_row) * rows + row) * 2);
+    if (L * k + in_row < parts.count) st[k] = *reinterpret_cast<const f32x2*>(a.stats + ((L * k + in_row) * step + row) * 2);
     m = fmaxf(m, st[k][0]);
   }
 #pragma unroll
@@ -252,7 +273,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int k = 0; k < N; ++k)
-          v[i][k] = i0 + i < count ? *reinterpret_cast<const Entries*>(from + (i0 + i) * rows * D + E * k) : Entries(0.f);
+          v[i][k] = i0 + i < count ? *reinterpret_cast<const Entries*>(from + (i0 + i) * step * D + E * k) : Entries(0.f);
       float factors = mine[0];
 #pragma unroll
       for (int k = 1; k < S; ++k) factors = i0 >= L * k ? mine[k] : factors;
@@ -284,14 +305,17 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 }
 
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
-constexpr int64_t kMostParts = 64, kPartialRows = 65536;
+constexpr int64_t kMostParts = 64, kMostFewMixed = 32, kPartialRows = 65536;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
 // Blocks of few rows read the keys once for 16 rows, and little else bounds them; blocks of many read them once for 128, and take longer to begin and end.  So calls are of
-// few as long as their blocks' tiles, with nine for what a block costs besides, are kFewWork at most, and where a sequence has 16 rows at most.  us a call of few / many, rows of a
+// few as long as the tiles of their blocks, with nine for what a block costs besides, are kFewWork at most.  In other calls sequences of 16 rows at most (a step's tokens
+// beside a prompt) are blocks of few all the same where there may be more than kMixedTiles tiles, which a block of many takes one after the other: 64 heads over 8, 7 sequences' tokens behind 32000 and 512 of a
+// prompt 734 us in blocks of many, 203 this way (apart 175 and 20); 16 behind 8000 and 2048 behind 2048 393 / 331; 31 behind 4000 and 512 134 / 128; but 100 behind 1000 and 300 91 / 102, and
+// prompts alone take 3 to 5 us longer, for the launches that find nothing.  us a call of few / many, rows of a
 // sequence and key head (and that number): 32 heads behind 2000 positions 96 19.6 / 25.6 (8k), 256 25.8 / 32.5 (23k), 512 51 / 46 (50k); 64 heads over 8 behind 8000, 256 27.7 / 29.5 (17k), 384
 // 47 / 35 (26k); four sequences of these behind 4000, 128 30 / 31 (18k), 256 44 / 41 (37k); sixteen, 32 heads over 8 behind 2000, 64 29.5 / 33.5 (21k), 96 45 / 37 (31k); 64 behind 500, 32 26 / 22
 // (17k), 48 37 / 24 (26k); 32 heads with no positions before, 512 14.5 / 19 (17k), 768 23 / 24.5 (32k); 64 behind 8000, 64 heads over 8, 16 324 / 301, 32 408 / 319, 96 724 / 342.
-constexpr int64_t kFewWork = 22000;
+constexpr int64_t kFewWork = 22000, kMixedTiles = 64;
 struct Plan { int bits; int64_t parts; int min_tiles; };
 // Rows of a block, and parts of the keys.  Blocks of many rows: the parts, of 8 tiles at least, that take the least time by what calls were measured to take: a tile 1.6 us where no CU has two
 // blocks, 2.35 where all have; sums that are joined 3.5 us, and their rows' and bytes' time.  us a call, as many parts as make two blocks a CU / these: three sequences of 256 tokens behind 600, 32 heads
@@ -300,7 +324,7 @@ struct Plan { int bits; int64_t parts; int min_tiles; };
 // evens sequences of different lengths out, for eight a CU of 32 tiles at least.  us a call, room for 512 / 1024 / 2048 workgroups of 4 tiles: 64 heads over 8 of 128, 64
 // sequences of up to 1000 positions 30.0 / 35.5 / 43.7 (those that find nothing to do take a microsecond, too), of up to 8191 245 / 241 / 234; 8 heads, 8 of up to 16000
 // 70.8 / 73.7 / 73.4.  Tiles at least, 2 / 4 / 9: 32 heads, one sequence of 200 8.1 / 5.8 / 7.5, a window of 1024 11.4 / 10.7 / 12.9; 64 over 8, 8000 18.4 / 16.0 / 15.4.
-static int64_t many_parts(int64_t blocks, int64_t rows, int64_t tiles, int64_t d) {
+static Plan many_plan(int64_t blocks, int64_t rows, int64_t tiles, int64_t d) {
   int64_t best = 1;
   double least = 1e30;
   for (int64_t parts = 1; parts <= kMostParts && (parts == 1 || (parts * blocks <= 512 && tiles / parts >= 8)); ++parts) {
@@ -308,45 +332,54 @@ static int64_t many_parts(int64_t blocks, int64_t rows, int64_t tiles, int64_t d
     const double us = (groups <= 256 ? 1.6 : groups <= 512 ? 2.35 : 2.35 * groups / 512) * each + (parts > 1 ? 3.5 + (double)rows * (2e-4 + (double)(parts * d) * 4 / 7.3e6) : 0);
     if (us < least) { least = us; best = parts; }
   }
-  return best;
+  return Plan{kManyBits, best, 8};
 }
-static Plan attention_plan(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t d, int64_t most_tiles) {
-  const int64_t rows = (tokens * (heads / kv_heads) - 1) / seqs + 1;      // of a sequence and key head, on average
-  auto blocks_of = [&](int bits) { return (((rows - 1) >> bits) + 1) * seqs * kv_heads; };
-  const bool many = rows > 16 && blocks_of(kFewBits) * (most_tiles + 9) > kFewWork;
-  const int bits = many ? kManyBits : kFewBits;
-  const int64_t blocks = blocks_of(bits), min_tiles = many ? 8 : 4;
-  int64_t parts = many ? many_parts(blocks, tokens * heads, most_tiles, d) : 512 / blocks, even = 2048 / blocks;
-  if (parts > (most_tiles + min_tiles - 1) / min_tiles) parts = (most_tiles + min_tiles - 1) / min_tiles;
+static Plan few_plan(int64_t blocks, int64_t most_tiles) {
+  int64_t parts = 512 / blocks, even = 2048 / blocks;
+  if (parts > (most_tiles + 3) / 4) parts = (most_tiles + 3) / 4;
   if (even > most_tiles / 32) even = most_tiles / 32;
-  if (!many && parts < even) parts = even;
-  return Plan{bits, parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts, (int)min_tiles};
+  if (parts < even) parts = even;
+  return Plan{kFewBits, parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts, 4};
 }
-// Room for the parts' sums: parts times blocks times their rows is 65536 at most.  (More tokens never take less, so a workspace serves all smaller calls.)
-static int64_t partial_rows(int64_t tokens, int64_t heads) { return kMostParts * tokens * heads < kPartialRows ? kMostParts * tokens * heads : kPartialRows; }
+static int64_t attention_blocks_of(int64_t tokens, int64_t seqs, int64_t group, int bits) {      // of sequences of one length
+  const int64_t rows = (tokens * group - 1) / seqs + 1;
+  return (((rows - 1) >> bits) + 1) * seqs;
+}
+// Room for the parts' sums: parts times blocks times their rows is 65536 at most, and parts are kMostParts at most; in calls that mix blocks, behind these half as many for those of few rows.
+// (More tokens never take less, so a workspace serves all smaller calls.)
+static int64_t partial_rows(int64_t tokens, int64_t heads) {
+  const int64_t rows = tokens * heads, few = kMostFewMixed * rows < kPartialRows / 2 ? kMostFewMixed * rows : kPartialRows / 2;
+  return (kMostParts * rows < kPartialRows ? kMostParts * rows : kPartialRows) + few;
+}
 
 template <int D>
-static hipError_t launch_attention(const AttentionArgs& all, hipStream_t s) {
-  AttentionArgs a = all;
-  const int64_t blocks = attention_blocks(a.c.tokens, a.c.seqs, a.c.group, a.rows_bits), each = (int64_t)a.parts * a.c.kv_heads;
-  if (a.rows_bits == kManyBits)
-    if (const hipError_t e = launch_attention_many(a, blocks, s); e != hipSuccess) return e;
+static hipError_t launch_attention(const AttentionArgs& many, const AttentionArgs& few, hipStream_t s) {
+  const CacheShape& c = many.c;
+  const bool is_many = many.rows_bits == kManyBits, is_few = !is_many || many.mixed;
+  if (is_many)
+    if (const hipError_t e = launch_attention_many(many, attention_blocks(c.tokens, c.seqs, c.group, kManyBits), s); e != hipSuccess) return e;
+  AttentionArgs a = few;
+  const int64_t blocks = is_few ? a.mixed ? c.seqs : attention_blocks(c.tokens, c.seqs, c.group, kFewBits) : 0, each = (int64_t)a.parts * c.kv_heads;
   const int64_t most = ((int64_t)1 << 23) / each;                    // (a grid has less than 2^32 threads)
-  for (int64_t first = a.rows_bits == kManyBits ? blocks : 0; first < blocks; first += most) {
+  for (int64_t first = 0; first < blocks; first += most) {
     a.first_block = first;
     const int64_t n = blocks - first < most ? blocks - first : most;
     hipLaunchKernelGGL(attention_few_kernel<D>, dim3((unsigned)(n * each)), dim3(256), 0, s, a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  if (a.parts == 1) return hipSuccess;
   constexpr int kLanes = 32;
-  const int64_t items = (int64_t)a.c.tokens * ((a.c.heads + 64 / kLanes - 1) / (64 / kLanes)), each_launch = (int64_t)1 << 25;
-  for (int64_t first = 0; first < items; first += each_launch) {
-    const int64_t n = items - first < each_launch ? items - first : each_launch;
-    hipLaunchKernelGGL((attention_join_kernel<D, kLanes>), dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, a, first, items);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  auto join = [&](const AttentionArgs& of, int64_t items) -> hipError_t {
+    const int64_t each_launch = (int64_t)1 << 25;
+    for (int64_t first = 0; first < items; first += each_launch) {
+      const int64_t n = items - first < each_launch ? items - first : each_launch;
+      hipLaunchKernelGGL((attention_join_kernel<D, kLanes>), dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, of, first, items);
+      if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  };
+  if (many.mixed && few.parts > 1)
+    if (const hipError_t e = join(few, (int64_t)c.seqs * c.kv_heads * (kFewMixed * kLanes / 64)); e != hipSuccess) return e;
+  return many.parts > 1 ? join(many, (int64_t)c.tokens * ((c.heads + 64 / kLanes - 1) / (64 / kLanes))) : hipSuccess;
 }
 
 static bool attention_size(int64_t tokens, int64_t seqs, int64_t heads, int64_t kv_heads, int64_t d) {
@@ -386,15 +419,40 @@ extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const
   // Tiles that a row can see: those of the table, or of the window (which begins and ends inside a tile, as the block's other rows have theirs) and the sinks.
   int64_t most_tiles = (cache->table_pages * cache->page + kTile - 1) / kTile;
   if (a.window && a.window / kTile + a.sinks / kTile + 4 < most_tiles) most_tiles = a.window / kTile + a.sinks / kTile + 4;
-  const Plan plan = attention_plan(tokens, seqs, heads, kv_heads, d, most_tiles);
-  a.rows_bits = plan.bits;
-  a.parts = (int32_t)plan.parts;
-  a.min_tiles = plan.min_tiles;
-  a.partial = (float*)ws;
-  a.stats = a.partial + (int64_t)a.parts * tokens * heads * d;
   if (cache->pages == 0) a.c.table_pages = 0;                                // no key anywhere: zeros
-  const hipError_t e = d == 64 ? launch_attention<64>(a, (hipStream_t)stream) : d == 96 ? launch_attention<96>(a, (hipStream_t)stream)
-                                                                            : launch_attention<128>(a, (hipStream_t)stream);
+  // For all that is known here sequences may be of one length, or have a token each but for one.
+  const int64_t group = heads / kv_heads, longest = (tokens > seqs ? tokens - seqs + 1 : 1) * group;
+  int64_t blocks = longest > kFewMixed ? ((longest - 1) >> kFewBits) + 1 : 0;
+  if (tokens * group > kFewMixed * seqs) { const int64_t like = attention_blocks_of(tokens, seqs, group, kFewBits); blocks = blocks > like ? blocks : like; }
+  const bool many = blocks * kv_heads * (most_tiles + 9) > kFewWork;
+  AttentionArgs f = a;
+  auto take = [&](AttentionArgs& x, const Plan& plan, float* at, int64_t part_rows) {
+    x.rows_bits = plan.bits; x.parts = (int32_t)plan.parts; x.min_tiles = plan.min_tiles;
+    const int64_t sums = plan.parts > 1 ? plan.parts * part_rows : 0;
+    x.partial = at;
+    x.stats = at + sums * d;
+    return at + (sums * (d + 2) + 3) / 4 * 4;                         // (vectors of four; a full workspace's sums are a multiple of four)
+  };
+  float* const at = (float*)ws;
+  if (!many) {
+    take(a, few_plan(attention_blocks_of(tokens, seqs, group, kFewBits) * kv_heads, most_tiles), at, tokens * heads);
+    f = a;
+  } else {
+    a.mixed = f.mixed = seqs > 1 && most_tiles > kMixedTiles;
+    float* const next = take(a, many_plan(attention_blocks_of(tokens, seqs, group, kManyBits) * kv_heads, tokens * heads, most_tiles, d), at, tokens * heads);
+    if (a.mixed) {
+      Plan plan = few_plan(seqs * kv_heads, most_tiles);
+      const int64_t room = kMostFewMixed * tokens * group / (seqs * kFewMixed);
+      if (plan.parts > room) plan.parts = room;
+      if (plan.parts > kMostFewMixed) plan.parts = kMostFewMixed;
+      if (plan.parts < 1) plan.parts = 1;
+      take(f, plan, next, seqs * kv_heads * kFewMixed);
+    } else {
+      f = a;
+    }
+  }
+  const hipError_t e = d == 64 ? launch_attention<64>(a, f, (hipStream_t)stream) : d == 96 ? launch_attention<96>(a, f, (hipStream_t)stream)
+                                                                               : launch_attention<128>(a, f, (hipStream_t)stream);
   if (e != hipSuccess) { set_last_hip_error(e); return GPTAQ_ELAUNCH; }
   return GPTAQ_OK;
 }

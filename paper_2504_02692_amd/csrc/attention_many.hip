@@ -47,7 +47,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
   // The heads of a block side by side, so that with eight key heads each XCD has one; late blocks first, which see the most.
   const int head = (int)(blockIdx.x % (unsigned)c.kv_heads), rest = (int)(blockIdx.x / (unsigned)c.kv_heads);
-  const Dealt dealt = cache_deal(c, rest, a.first_block, blocks, a.parts, a.rows_bits);
+  const Dealt dealt = cache_deal(c, rest, a.first_block, blocks, a.parts, a.rows_bits, a.mixed ? kFewMixed : 0);
   if (dealt.block < 0) return;
   const int s = dealt.sequence, part = dealt.part;
   const Sequence seq = cache_sequence(c, s);

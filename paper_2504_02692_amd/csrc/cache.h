@@ -47,14 +47,15 @@ __device__ __forceinline__ int cache_find(const CacheShape& c, int64_t block, in
   }
   return __builtin_amdgcn_readfirstlane(lo);
 }
-// The same without gaps, for work that fills the GPU once or a few times: sequence s has ceil(rows / 2^bits) blocks of its count * group rows, and a block is found by
+// The same without gaps, for work that fills the GPU once or a few times: sequence s has ceil(rows / 2^bits) blocks of its count * group rows (none where these are not more than `more_than`), and a block is found by
 // sums over the lanes, each of which has a run of sequences; then over that lane's sequences.  Workgroup `at` of those that deal out blocks first .. first + n - 1, counted from the
 // last block on, and `parts` parts of each: first parts before second ones, and behind them all the workgroups that find nothing to do (block -1).  They go to the shader engines in turn,
 // and between others they would leave CUs idle: two sequences' 16 tokens behind 16000, 64 heads over 8, 52 us with two of four blocks empty in every part, 32 this way.
 struct Dealt { int32_t sequence, block, part; };
-__device__ __forceinline__ int64_t cache_blocks(const CacheShape& c, int s, int bits) {
+__device__ __forceinline__ int64_t cache_blocks(const CacheShape& c, int s, int bits, int more_than) {
   const int first = cache_clamp(c.starts[s], 0, c.tokens), count = cache_clamp(c.starts[s + 1], first, c.tokens) - first;
-  return ((int64_t)count * c.group + (1 << bits) - 1) >> bits;
+  const int64_t rows = (int64_t)count * c.group;
+  return rows > more_than ? (rows + (1 << bits) - 1) >> bits : 0;
 }
 __device__ __forceinline__ int cache_prefix(int v) {                 // sums over this lane and those below
   const int lane = threadIdx.x & 63;
@@ -65,10 +66,10 @@ __device__ __forceinline__ int cache_prefix(int v) {                 // sums ove
   }
   return v;
 }
-__device__ __forceinline__ Dealt cache_deal(const CacheShape& c, uint32_t at, int64_t first, int n, int parts, int bits) {
+__device__ __forceinline__ Dealt cache_deal(const CacheShape& c, uint32_t at, int64_t first, int n, int parts, int bits, int more_than) {
   const int lane = threadIdx.x & 63, per = (c.seqs + 63) >> 6, mine0 = lane * per, mine1 = mine0 + per < c.seqs ? mine0 + per : c.seqs;
   int mine = 0;                                                      // (blocks are 2^23 at most; starts that do not ascend could say more than 31 bits)
-  for (int s = mine0; s < mine1; ++s) mine = min(mine + (int)cache_blocks(c, s, bits), 1 << 24);
+  for (int s = mine0; s < mine1; ++s) mine = min(mine + (int)cache_blocks(c, s, bits, more_than), 1 << 24);
   int sums = cache_prefix(mine);
   const int all = __builtin_amdgcn_readlane(sums, 63);
   const int here_all = (int)(all - first < n ? all - first : n);
@@ -83,7 +84,7 @@ __device__ __forceinline__ Dealt cache_deal(const CacheShape& c, uint32_t at, in
   if (per > 1) {
     const int end = s0 + per < c.seqs ? s0 + per : c.seqs;
     for (;; s0 += 64) {                                              // (ends: the lane's sequences have the block among them)
-      mine = s0 + lane < end ? (int)cache_blocks(c, s0 + lane, bits) : 0;
+      mine = s0 + lane < end ? (int)cache_blocks(c, s0 + lane, bits, more_than) : 0;
       sums = cache_prefix(mine);
       const int here = __builtin_amdgcn_readlane(sums, 63);
       if (block < here || s0 + 64 >= end) break;

@@ -229,3 +229,56 @@ def test_shared_pages_and_offsets_past_32_bits():
     dev.update(keys=big_k, values=big_v, table=table)
     q = queries(c, heads, d)
     check(B.gptaq_attention(q, **dev, ws=workspace(c.tokens, 2, heads, kv, d)), c, q, heads, 0, 0)
+
+
+MIXED = [  # steps beside prompts: (new, before) of the sequences, heads, kv_heads, d, page, window, sinks
+    ([(1, 3000), (300, 0), (1, 40), (0, 9), (2, 500), (1, 0)], 32, 8, 128, 16, 0, 0), ([(500, 20), (1, 700), (1, 2000)], 40, 20, 64, 64, 0, 0),
+    ([(16, 50), (17, 50), (15, 3), (400, 10), (1, 1000)], 48, 48, 96, 32, 0, 0), ([(1, 5600), (1, 77), (400, 4300), (1, 900)], 32, 16, 128, 16, 4100, 70),
+    ([(1, 5000)] * 3 + [(150, 4000)], 24, 24, 64, 128, 0, 0), ([(1, 900), (600, 0), (1, 3)], 32, 1, 128, 16, 0, 0), ([(1, 60)] * 40 + [(700, 0)] + [(1, 300)] * 25, 32, 8, 64, 16, 0, 0),
+    ([(2, 4500), (3, 1500), (500, 0), (1, 4500)], 32, 4, 96, 16, 4097, 10),
+]
+
+
+@pytest.mark.parametrize("pairs,heads,kv,d,page,window,sinks", MIXED)
+def test_steps_beside_prompts(pairs, heads, kv, d, page, window, sinks):
+    """In tables with room for 6400 positions: steps are blocks of few rows, and prompts of many."""
+    tokens, width = sum(c for c, _ in pairs), max(-(-(c + b) // page) for c, b in pairs)
+    tiles = min(100, window // 64 + sinks // 64 + 4 if window else 100)
+    assert len(pairs) > 1 and tiles > 64 and -(-(tokens - len(pairs) + 1) * (heads // kv) // 16) * kv * (tiles + 9) > 22000
+    run(pairs, heads, kv, d, page, window, sinks, wider=6400 // page - width)
+
+
+def test_captured_steps_beside_prompts():
+    """The sequences that are steps and those that are prompts change places, and lengths grow, between replays of one graph; the workspace holds what other calls left."""
+    heads, kv, d, page = 32, 8, 64, 16
+    shapes = [[(1, 2000), (300, 0), (4, 900)], [(300, 33), (1, 7), (4, 1200)], [(4, 500), (1, 2222), (300, 1000)], [(100, 0), (100, 700), (105, 90)]]
+    assert all(sum(c for c, _ in p) == 305 for p in shapes)
+    caches = [Cache(p, kv, d, page, seed=k) for k, p in enumerate(shapes)]
+    width, pages = 400, max(c.pages for c in caches)                 # (6400 positions)
+    keys, values = torch.zeros((pages, kv, d // 8, page, 8), dtype=torch.bfloat16, device="cuda"), torch.zeros((pages, kv, page // 8, d, 8), dtype=torch.bfloat16, device="cuda")
+    table = torch.full((3, width), -1, dtype=torch.int32, device="cuda")
+    starts, lengths = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    q, out = (torch.zeros((305, heads, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ws = workspace(305, 3, heads, kv, d)
+
+    def put(c):
+        dev = c.device()
+        keys[:c.pages], values[:c.pages] = dev["keys"], dev["values"]
+        table.fill_(-1)
+        table[:, :c.table.shape[1]] = dev["table"]
+        starts.copy_(dev["starts"]); lengths.copy_(dev["lengths"]); q.copy_(queries(c, heads, d))
+
+    call = lambda ws, out: B.gptaq_attention(q, keys, values, table, starts, lengths, ws, out=out)
+    put(caches[0])
+    call(ws, out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(ws, out)
+    for c in [*caches, caches[0]]:
+        put(c)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(call(workspace(305, 3, heads, kv, d), torch.empty_like(out)), got)
+        check(got, c, q, heads, 0, 0)
