@@ -15,8 +15,9 @@ struct AttentionArgs {
   int32_t parts;                       // the keys of a block of rows in so many parts at most, each of min_tiles tiles at least
   int32_t min_tiles, rows_bits;        // rows of a block (log2)
   int64_t first_block;
-  int32_t mixed;                       // sequences of kFewMixed rows and fewer are taken by blocks of few rows, one a sequence, the others by blocks of many
-  float *partial, *stats;              // [part][row of the call][d], [part][row of the call][maximum, sum]; mixed, of few rows: [part][sequence][key head][row of 16]..
+  int32_t mixed;                       // sequences of kFewMixed rows and fewer are taken by blocks of few rows, one a sequence, the others by blocks of many;
+  int32_t target;                      // mixed, of few rows: so many blocks and parts together, where there are not more blocks
+  float *partial, *stats;              // [part][row of the call][d], [part][row of the call][maximum, sum]; mixed, of few rows: [part][block][key head][row of 16]..
 };
 
 constexpr int kTile = 64;              // keys to a tile: what is dealt out
@@ -50,9 +51,13 @@ __device__ __forceinline__ int at_token(int row, int group) { return __builtin_a
 // one token, 64 heads over 8, with no such bound / with it: 8000 positions 15.6 / 14.6, 16000 23.2 / 19.7, 32000 33.2 / 29.7, 130000 107 / 107.
 struct Parts { int32_t each, count; };
 constexpr int kFewBits = 4, kFewMixed = 16;      // blocks of few rows have 16
-__device__ __forceinline__ Parts attention_parts(const AttentionArgs& a, int tiles) {
+__device__ __forceinline__ Deal attention_deal(const AttentionArgs& a) {
+  const bool few = a.rows_bits == kFewBits;
+  return Deal{a.rows_bits, a.mixed && !few ? kFewMixed : 0, a.mixed && few ? kFewMixed : 0x7fffffff, a.parts, a.target};
+}
+__device__ __forceinline__ Parts attention_parts(const AttentionArgs& a, int tiles, int parts) {
   const int least = a.rows_bits == kFewBits ? max(a.min_tiles, min(tiles / 20, 20)) : a.min_tiles;
-  const int each = max(least, (tiles + a.parts - 1) / a.parts);
+  const int each = max(least, (tiles + parts - 1) / parts);
   return Parts{each, (tiles + each - 1) / each};
 }
 

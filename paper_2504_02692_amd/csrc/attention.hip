@@ -20,17 +20,25 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) 
   const CacheShape& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, quad = lane >> 4;
   const int head = (int)(blockIdx.x % (unsigned)c.kv_heads), rest = (int)(blockIdx.x / (unsigned)c.kv_heads);
-  const int part = rest % a.parts;
-  const int64_t block = a.first_block + rest / a.parts;
-  const int s = a.mixed ? (int)block : cache_find(c, block, c.group, 4, 1);
+  int part, s, parts_most = a.parts, index = 0, indexes = 0;
+  int64_t in_seq;
+  if (a.mixed) {
+    const Dealt dealt = cache_deal(c, (uint32_t)(a.first_block + rest), 0, 0x7fffffff, attention_deal(a));
+    if (dealt.block < 0) return;
+    part = dealt.part, s = dealt.sequence, in_seq = 0, parts_most = dealt.parts, index = dealt.index, indexes = dealt.all;
+  } else {
+    part = rest % a.parts;
+    const int64_t block = a.first_block + rest / a.parts;
+    s = cache_find(c, block, c.group, 4, 1);
+    in_seq = block - cache_block_of(c, s, c.group, 4, 1);
+  }
   const Sequence seq = cache_sequence(c, s);
-  const int64_t in_seq = a.mixed ? 0 : block - cache_block_of(c, s, c.group, 4, 1);
   const int rows = seq.count * c.group;
-  if (in_seq < 0 || in_seq * 16 >= rows || (a.mixed && rows > kFewMixed)) return;
+  if (in_seq < 0 || in_seq * 16 >= rows) return;
   const int row0 = (int)in_seq * 16, last = min(row0 + 15, rows - 1);
   const int pmin = seq.before + at_token(row0, c.group), pmax = seq.before + at_token(last, c.group);
   const Tiles tiles = attention_tiles(a, pmin, pmax);
-  const Parts parts = attention_parts(a, tiles.count);
+  const Parts parts = attention_parts(a, tiles.count, parts_most);
   if (part > 0 && part >= parts.count) return;                       // (part 0 writes the zeros of rows that see nothing)
   const int begin = part * parts.each, end = min(begin + parts.each, tiles.count);
 
@@ -175,7 +183,7 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) 
   const int64_t call_row = (int64_t)(seq.first + tok) * c.heads + head * c.group + rr % c.group;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   uint16_t* const to = a.out + (int64_t)(seq.first + tok) * a.ldo + (int64_t)(head * c.group + rr % c.group) * a.ho;
-  const int64_t part_row = a.mixed ? (((int64_t)part * c.seqs + s) * c.kv_heads + head) * kFewMixed + r : (int64_t)part * c.tokens * c.heads + call_row;
+  const int64_t part_row = a.mixed ? (((int64_t)part * indexes + index) * c.kv_heads + head) * kFewMixed + r : (int64_t)part * c.tokens * c.heads + call_row;
   float* const to_part = a.partial + part_row * D;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
@@ -210,17 +218,20 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
   const int lane = threadIdx.x & 63, in_row = lane & (L - 1);
   const int64_t item = first + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (item >= items) return;
-  int s, token, h;
+  int s, token, h, parts_most = a.parts;
   int64_t row, step;                                                 // in the partial sums; from a part to the next
   if (a.mixed && a.rows_bits == kFewBits) {                          // 16 rows of each sequence and key head; rows are 2^30 at most
     constexpr uint32_t kItems = kFewMixed * L / 64;
     const uint32_t block = (uint32_t)item / kItems, head = block % (uint32_t)c.kv_heads;
     const int at = (int)((uint32_t)item % kItems) * (64 / L) + lane / L;
-    s = (int)(block / (uint32_t)c.kv_heads);
+    const Deal deal = attention_deal(a);
+    const Dealt dealt = cache_deal(c, block / (uint32_t)c.kv_heads, 0, 0x7fffffff, Deal{deal.bits, deal.above, deal.most, 1, 0});
+    if (dealt.block < 0) return;
+    s = dealt.sequence, parts_most = cache_parts(deal, dealt.all);
     token = at / c.group;
     h = (int)head * c.group + at % c.group;
-    row = (int64_t)block * kFewMixed + at;
-    step = (int64_t)c.seqs * c.kv_heads * kFewMixed;
+    row = ((int64_t)dealt.index * c.kv_heads + head) * kFewMixed + at;
+    step = (int64_t)dealt.all * c.kv_heads * kFewMixed;
   } else {                                                           // 64 / L heads of a token
     const uint32_t groups = (c.heads + 64 / L - 1) / (64 / L);
     token = (int)((uint32_t)item / groups);
@@ -238,7 +249,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
   // as the block of this row dealt its tiles out
   const int row0 = (in_seq * c.group + h % c.group) >> a.rows_bits << a.rows_bits;
   const int last = min(row0 + (1 << a.rows_bits) - 1, rows_seq - 1);
-  const Parts parts = attention_parts(a, attention_tiles(a, seq.before + row0 / c.group, seq.before + last / c.group).count);
+  const Parts parts = attention_parts(a, attention_tiles(a, seq.before + row0 / c.group, seq.before + last / c.group).count, parts_most);
   if (parts.count <= 1) return;
   // a lane has the statistics of every L-th part (there are 64 at most), and a share of every part's sums
   typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -305,17 +316,18 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 }
 
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
-constexpr int64_t kMostParts = 64, kMostFewMixed = 32, kPartialRows = 65536;
+constexpr int64_t kMostParts = 64, kMostFewMixed = 32, kPartialRows = 65536, kFewMixedRows = 1024 * kFewMixed;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
 // Blocks of few rows read the keys once for 16 rows, and little else bounds them; blocks of many read them once for 128, and take longer to begin and end.  So calls are of
-// few as long as the tiles of their blocks, with nine for what a block costs besides, are kFewWork at most.  In other calls sequences of 16 rows at most (a step's tokens
-// beside a prompt) are blocks of few all the same where there may be more than kMixedTiles tiles, which a block of many takes one after the other: 64 heads over 8, 7 sequences' tokens behind 32000 and 512 of a
-// prompt 734 us in blocks of many, 203 this way (apart 175 and 20); 16 behind 8000 and 2048 behind 2048 393 / 331; 31 behind 4000 and 512 134 / 128; but 100 behind 1000 and 300 91 / 102, and
-// prompts alone take 3 to 5 us longer, for the launches that find nothing.  us a call of few / many, rows of a
+// few as long as the tiles of their blocks, with nine for what a block costs besides, are kFewWork at most.
+// In other calls sequences of 16 rows at most (a step's tokens beside a prompt) are blocks of few all the same, dealt out by themselves, where there may be more than kMixedTiles tiles, which a block
+// of many takes one after the other, and too few sequences to fill the chip that way.  64 heads over 8, all in blocks of many / this way: 7 sequences' tokens behind 32000 and 512 of a prompt 734 /
+// 197 us (apart 175 and 20); 16 behind 8000 and 2048 behind 2048 393 / 320 (102 and 214); but 31 behind 4000 and 512 134 / 128, 63 and 1000 222 / 227, 100
+// behind 1000 and 300 91 / 102, and prompts alone take 3 to 5 us longer, for launches that find nothing.  us a call of few / many, rows of a
 // sequence and key head (and that number): 32 heads behind 2000 positions 96 19.6 / 25.6 (8k), 256 25.8 / 32.5 (23k), 512 51 / 46 (50k); 64 heads over 8 behind 8000, 256 27.7 / 29.5 (17k), 384
 // 47 / 35 (26k); four sequences of these behind 4000, 128 30 / 31 (18k), 256 44 / 41 (37k); sixteen, 32 heads over 8 behind 2000, 64 29.5 / 33.5 (21k), 96 45 / 37 (31k); 64 behind 500, 32 26 / 22
 // (17k), 48 37 / 24 (26k); 32 heads with no positions before, 512 14.5 / 19 (17k), 768 23 / 24.5 (32k); 64 behind 8000, 64 heads over 8, 16 324 / 301, 32 408 / 319, 96 724 / 342.
-constexpr int64_t kFewWork = 22000, kMixedTiles = 64;
+constexpr int64_t kFewWork = 22000, kMixedTiles = 96, kMixedRows = 256;      // (kMixedRows: smaller calls need no room for both)
 struct Plan { int bits; int64_t parts; int min_tiles; };
 // Rows of a block, and parts of the keys.  Blocks of many rows: the parts, of 8 tiles at least, that take the least time by what calls were measured to take: a tile 1.6 us where no CU has two
 // blocks, 2.35 where all have; sums that are joined 3.5 us, and their rows' and bytes' time.  us a call, as many parts as make two blocks a CU / these: three sequences of 256 tokens behind 600, 32 heads
@@ -345,11 +357,10 @@ static int64_t attention_blocks_of(int64_t tokens, int64_t seqs, int64_t group, 
   const int64_t rows = (tokens * group - 1) / seqs + 1;
   return (((rows - 1) >> bits) + 1) * seqs;
 }
-// Room for the parts' sums: parts times blocks times their rows is 65536 at most, and parts are kMostParts at most; in calls that mix blocks, behind these half as many for those of few rows.
-// (More tokens never take less, so a workspace serves all smaller calls.)
+// Room for the parts' sums: parts times blocks times their rows is 65536 at most, and parts are kMostParts at most; in calls that mix blocks, behind these the sums of blocks of few rows,
+// of which there are 1024 at most where they have parts.  (More tokens never take less, so a workspace serves all smaller calls.)
 static int64_t partial_rows(int64_t tokens, int64_t heads) {
-  const int64_t rows = tokens * heads, few = kMostFewMixed * rows < kPartialRows / 2 ? kMostFewMixed * rows : kPartialRows / 2;
-  return (kMostParts * rows < kPartialRows ? kMostParts * rows : kPartialRows) + few;
+  return (kMostParts * tokens * heads < kPartialRows ? kMostParts * tokens * heads : kPartialRows) + (tokens * heads > kMixedRows ? kFewMixedRows : 0);
 }
 
 template <int D>
@@ -359,7 +370,9 @@ static hipError_t launch_attention(const AttentionArgs& many, const AttentionArg
   if (is_many)
     if (const hipError_t e = launch_attention_many(many, attention_blocks(c.tokens, c.seqs, c.group, kManyBits), s); e != hipSuccess) return e;
   AttentionArgs a = few;
-  const int64_t blocks = is_few ? a.mixed ? c.seqs : attention_blocks(c.tokens, c.seqs, c.group, kFewBits) : 0, each = (int64_t)a.parts * c.kv_heads;
+  // (mixed: of blocks and parts together)
+  const int64_t blocks = !is_few ? 0 : a.mixed ? (c.seqs > a.target ? c.seqs : a.target) : attention_blocks(c.tokens, c.seqs, c.group, kFewBits);
+  const int64_t each = (int64_t)(a.mixed ? 1 : a.parts) * c.kv_heads;
   const int64_t most = ((int64_t)1 << 23) / each;                    // (a grid has less than 2^32 threads)
   for (int64_t first = 0; first < blocks; first += most) {
     a.first_block = first;
@@ -438,15 +451,14 @@ extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const
     take(a, few_plan(attention_blocks_of(tokens, seqs, group, kFewBits) * kv_heads, most_tiles), at, tokens * heads);
     f = a;
   } else {
-    a.mixed = f.mixed = seqs > 1 && most_tiles > kMixedTiles;
+    a.mixed = f.mixed = seqs > 1 && most_tiles > kMixedTiles && most_tiles * 4 > seqs * kv_heads && tokens * heads > kMixedRows;
     float* const next = take(a, many_plan(attention_blocks_of(tokens, seqs, group, kManyBits) * kv_heads, tokens * heads, most_tiles, d), at, tokens * heads);
     if (a.mixed) {
-      Plan plan = few_plan(seqs * kv_heads, most_tiles);
-      const int64_t room = kMostFewMixed * tokens * group / (seqs * kFewMixed);
-      if (plan.parts > room) plan.parts = room;
-      if (plan.parts > kMostFewMixed) plan.parts = kMostFewMixed;
-      if (plan.parts < 1) plan.parts = 1;
-      take(f, plan, next, seqs * kv_heads * kFewMixed);
+      f.target = (int32_t)(kv_heads < 1024 ? 1024 / kv_heads : 1);   // four a CU: sequences' lengths differ
+      int64_t parts = (most_tiles + 3) / 4;
+      if (parts > kMostFewMixed) parts = kMostFewMixed;
+      take(f, Plan{kFewBits, parts < 1 ? 1 : parts, 4}, next, 0);
+      f.stats = f.partial + kFewMixedRows * d;
     } else {
       f = a;
     }

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, half = lane >> 5;
   // The heads of a block side by side, so that with eight key heads each XCD has one; late blocks first, which see the most.
   const int head = (int)(blockIdx.x % (unsigned)c.kv_heads), rest = (int)(blockIdx.x / (unsigned)c.kv_heads);
-  const Dealt dealt = cache_deal(c, rest, a.first_block, blocks, a.parts, a.rows_bits, a.mixed ? kFewMixed : 0);
+  const Dealt dealt = cache_deal(c, rest, a.first_block, blocks, attention_deal(a));
   if (dealt.block < 0) return;
   const int s = dealt.sequence, part = dealt.part;
   const Sequence seq = cache_sequence(c, s);
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attention_many_kernel(AttentionArg
   if (((int64_t)dealt.block << a.rows_bits) >= rows) return;         // (starts that do not ascend)
   const int row0 = dealt.block << a.rows_bits, last = min(row0 + 32 * NW - 1, rows - 1);
   const Tiles tiles = attention_tiles(a, seq.before + at_token(row0, c.group), seq.before + at_token(last, c.group));
-  const Parts parts = attention_parts(a, tiles.count);
+  const Parts parts = attention_parts(a, tiles.count, a.parts);
   if (part > 0 && part >= parts.count) return;                       // (part 0 writes the zeros of rows that see nothing)
   const int begin = part * parts.each, end = min(begin + parts.each, tiles.count);
 

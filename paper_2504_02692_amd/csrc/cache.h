@@ -47,15 +47,18 @@ __device__ __forceinline__ int cache_find(const CacheShape& c, int64_t block, in
   }
   return __builtin_amdgcn_readfirstlane(lo);
 }
-// The same without gaps, for work that fills the GPU once or a few times: sequence s has ceil(rows / 2^bits) blocks of its count * group rows (none where these are not more than `more_than`), and a block is found by
-// sums over the lanes, each of which has a run of sequences; then over that lane's sequences.  Workgroup `at` of those that deal out blocks first .. first + n - 1, counted from the
-// last block on, and `parts` parts of each: first parts before second ones, and behind them all the workgroups that find nothing to do (block -1).  They go to the shader engines in turn,
-// and between others they would leave CUs idle: two sequences' 16 tokens behind 16000, 64 heads over 8, 52 us with two of four blocks empty in every part, 32 this way.
-struct Dealt { int32_t sequence, block, part; };
-__device__ __forceinline__ int64_t cache_blocks(const CacheShape& c, int s, int bits, int more_than) {
+// The same without gaps, for work that fills the GPU once or a few times: sequence s has ceil(rows / 2^bits) blocks of its count * group rows where these are more than `above` and at
+// most `most`, and a block is found by sums over the lanes, each of which has a run of sequences; then over that lane's sequences.  Workgroup `at` of those that deal out blocks
+// first .. first + n - 1, counted from the last block on, and `parts` parts of each: first parts before second ones, or, with a `target`, a block's side by side, as many as make no more than that
+// together.  Behind them all come the workgroups that find nothing to do (block -1).  They go to the shader engines in turn, and between others they would leave CUs idle: two sequences' 16 tokens behind 16000, 64 heads over 8, 52 us with two of
+// four blocks empty in every part, 32 this way.
+struct Dealt { int32_t sequence, block, part, parts, index, all; };      // index: of all blocks
+struct Deal { int32_t bits, above, most, parts, target; };
+__device__ __forceinline__ int cache_parts(const Deal& d, int all) { return d.target ? max(1, min(d.parts, d.target / all)) : d.parts; }
+__device__ __forceinline__ int64_t cache_blocks(const CacheShape& c, int s, const Deal& d) {
   const int first = cache_clamp(c.starts[s], 0, c.tokens), count = cache_clamp(c.starts[s + 1], first, c.tokens) - first;
   const int64_t rows = (int64_t)count * c.group;
-  return rows > more_than ? (rows + (1 << bits) - 1) >> bits : 0;
+  return rows > d.above && rows <= d.most ? (rows + (1 << d.bits) - 1) >> d.bits : 0;
 }
 __device__ __forceinline__ int cache_prefix(int v) {                 // sums over this lane and those below
   const int lane = threadIdx.x & 63;
@@ -66,17 +69,20 @@ __device__ __forceinline__ int cache_prefix(int v) {                 // sums ove
   }
   return v;
 }
-__device__ __forceinline__ Dealt cache_deal(const CacheShape& c, uint32_t at, int64_t first, int n, int parts, int bits, int more_than) {
+__device__ __forceinline__ Dealt cache_deal(const CacheShape& c, uint32_t at, int64_t first, int n, const Deal& d) {
   const int lane = threadIdx.x & 63, per = (c.seqs + 63) >> 6, mine0 = lane * per, mine1 = mine0 + per < c.seqs ? mine0 + per : c.seqs;
   int mine = 0;                                                      // (blocks are 2^23 at most; starts that do not ascend could say more than 31 bits)
-  for (int s = mine0; s < mine1; ++s) mine = min(mine + (int)cache_blocks(c, s, bits, more_than), 1 << 24);
+  for (int s = mine0; s < mine1; ++s) mine = min(mine + (int)cache_blocks(c, s, d), 1 << 24);
   int sums = cache_prefix(mine);
   const int all = __builtin_amdgcn_readlane(sums, 63);
   const int here_all = (int)(all - first < n ? all - first : n);
-  if (here_all <= 0) return Dealt{0, -1, 0};
-  const int part = (int)(at / (uint32_t)here_all);
-  if (part >= parts) return Dealt{0, -1, 0};
-  int block = all - 1 - (int)(first + at % (uint32_t)here_all);
+  if (here_all <= 0) return Dealt{0, -1, 0, 0, 0, 0};
+  const int parts = cache_parts(d, all);
+  const uint32_t by = d.target ? (uint32_t)parts : (uint32_t)here_all, q = at / by, r = at - q * by;
+  const int part = (int)(d.target ? r : q), which = (int)(d.target ? q : r);
+  if (part >= parts || which >= here_all) return Dealt{0, -1, 0, 0, 0, 0};
+  const int index = all - 1 - (int)(first + which);
+  int block = index;
   uint64_t mask = __ballot(sums > block);
   int k = __builtin_ctzll(mask);
   block -= __builtin_amdgcn_readlane(sums, k) - __builtin_amdgcn_readlane(mine, k);
@@ -84,7 +90,7 @@ __device__ __forceinline__ Dealt cache_deal(const CacheShape& c, uint32_t at, in
   if (per > 1) {
     const int end = s0 + per < c.seqs ? s0 + per : c.seqs;
     for (;; s0 += 64) {                                              // (ends: the lane's sequences have the block among them)
-      mine = s0 + lane < end ? (int)cache_blocks(c, s0 + lane, bits, more_than) : 0;
+      mine = s0 + lane < end ? (int)cache_blocks(c, s0 + lane, d) : 0;
       sums = cache_prefix(mine);
       const int here = __builtin_amdgcn_readlane(sums, 63);
       if (block < here || s0 + 64 >= end) break;
@@ -95,7 +101,8 @@ __device__ __forceinline__ Dealt cache_deal(const CacheShape& c, uint32_t at, in
     block -= __builtin_amdgcn_readlane(sums, k) - __builtin_amdgcn_readlane(mine, k);
     s0 = s0 + k < end ? s0 + k : end - 1;
   }
-  return Dealt{__builtin_amdgcn_readfirstlane(s0), __builtin_amdgcn_readfirstlane(block), __builtin_amdgcn_readfirstlane(part)};
+  auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  return Dealt{same(s0), same(block), same(part), same(parts), same(index), same(all)};
 }
 // The page of a position, or -1.
 __device__ __forceinline__ int cache_page(const CacheShape& c, int s, int position) {

@@ -83,6 +83,10 @@ def test_arrays_that_make_no_sense_stay_inside(starts, lengths):
     q = bf16(np.ones((280, 4 * m, 64)))
     B.gptaq_attention(q, **dev, ws=workspace(280, 2, 4 * m, 2 * m, 64))
     torch.cuda.synchronize()
+    wide = torch.full((2, 800), -1, dtype=torch.int32, device="cuda")        # steps beside prompts
+    wide[:, :dev["table"].shape[1]] = dev["table"]
+    B.gptaq_attention(q[:, :16], **dict(dev, table=wide, keys=dev["keys"][:, :8].contiguous(), values=dev["values"][:, :8].contiguous()), ws=workspace(280, 2, 16, 8, 64))
+    torch.cuda.synchronize()
 
 
 def test_many_sequences():
@@ -233,19 +237,19 @@ def test_shared_pages_and_offsets_past_32_bits():
 
 MIXED = [  # steps beside prompts: (new, before) of the sequences, heads, kv_heads, d, page, window, sinks
     ([(1, 3000), (300, 0), (1, 40), (0, 9), (2, 500), (1, 0)], 32, 8, 128, 16, 0, 0), ([(500, 20), (1, 700), (1, 2000)], 40, 20, 64, 64, 0, 0),
-    ([(16, 50), (17, 50), (15, 3), (400, 10), (1, 1000)], 48, 48, 96, 32, 0, 0), ([(1, 5600), (1, 77), (400, 4300), (1, 900)], 32, 16, 128, 16, 4100, 70),
+    ([(16, 50), (17, 50), (15, 3), (400, 10), (1, 1000)], 48, 48, 96, 32, 0, 0), ([(1, 8600), (1, 77), (400, 6900), (1, 900)], 32, 16, 128, 16, 6100, 70),
     ([(1, 5000)] * 3 + [(150, 4000)], 24, 24, 64, 128, 0, 0), ([(1, 900), (600, 0), (1, 3)], 32, 1, 128, 16, 0, 0), ([(1, 60)] * 40 + [(700, 0)] + [(1, 300)] * 25, 32, 8, 64, 16, 0, 0),
-    ([(2, 4500), (3, 1500), (500, 0), (1, 4500)], 32, 4, 96, 16, 4097, 10),
+    ([(2, 7500), (3, 1500), (500, 0), (1, 6500)], 32, 4, 96, 16, 6097, 10),
 ]
 
 
 @pytest.mark.parametrize("pairs,heads,kv,d,page,window,sinks", MIXED)
 def test_steps_beside_prompts(pairs, heads, kv, d, page, window, sinks):
-    """In tables with room for 6400 positions: steps are blocks of few rows, and prompts of many."""
+    """In tables with room for 12800 positions: steps are blocks of few rows, and prompts of many."""
     tokens, width = sum(c for c, _ in pairs), max(-(-(c + b) // page) for c, b in pairs)
-    tiles = min(100, window // 64 + sinks // 64 + 4 if window else 100)
-    assert len(pairs) > 1 and tiles > 64 and -(-(tokens - len(pairs) + 1) * (heads // kv) // 16) * kv * (tiles + 9) > 22000
-    run(pairs, heads, kv, d, page, window, sinks, wider=6400 // page - width)
+    tiles = min(200, window // 64 + sinks // 64 + 4 if window else 200)
+    assert len(pairs) > 1 and tiles > 96 and tiles * 4 > len(pairs) * kv and -(-(tokens - len(pairs) + 1) * (heads // kv) // 16) * kv * (tiles + 9) > 22000
+    run(pairs, heads, kv, d, page, window, sinks, wider=12800 // page - width)
 
 
 def test_captured_steps_beside_prompts():
@@ -254,7 +258,7 @@ def test_captured_steps_beside_prompts():
     shapes = [[(1, 2000), (300, 0), (4, 900)], [(300, 33), (1, 7), (4, 1200)], [(4, 500), (1, 2222), (300, 1000)], [(100, 0), (100, 700), (105, 90)]]
     assert all(sum(c for c, _ in p) == 305 for p in shapes)
     caches = [Cache(p, kv, d, page, seed=k) for k, p in enumerate(shapes)]
-    width, pages = 400, max(c.pages for c in caches)                 # (6400 positions)
+    width, pages = 800, max(c.pages for c in caches)                 # (12800 positions)
     keys, values = torch.zeros((pages, kv, d // 8, page, 8), dtype=torch.bfloat16, device="cuda"), torch.zeros((pages, kv, page // 8, d, 8), dtype=torch.bfloat16, device="cuda")
     table = torch.full((3, width), -1, dtype=torch.int32, device="cuda")
     starts, lengths = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
