@@ -524,7 +524,9 @@ def gptaq_linear_workspace_bytes(tokens: int, m: int, n: int) -> int:
     return load().gptaq_linear_workspace_bytes(tokens, m, n)
 
 
-def _linear_out(X: torch.Tensor, tokens: int, n: int, w: _Weights, dtype, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
+def _linear_out(X: torch.Tensor, tokens: int, n: int, w: _Weights, kind: type, dtype, out: Optional[torch.Tensor], name: str) -> torch.Tensor:
+    if not isinstance(w, kind):                          # (the other kind's arguments are others, in another order)
+        raise GptaqError(f"{name}: weights: expected the {kind.__name__} that {kind._packs} returns, not {type(w).__name__}")
     if n != w.n:
         raise GptaqError(f"{name}: X has {n} columns, the weights {w.n}")
     if out is None:
@@ -543,7 +545,7 @@ def gptaq_linear(X: torch.Tensor, weights: LinearWeights, ws: torch.Tensor, out:
     _need(X, torch.bfloat16, "X")
     device = _here(X, out)
     tokens, n = X.shape
-    Y = _linear_out(X, tokens, n, weights, dtype, out, "gptaq_linear")
+    Y = _linear_out(X, tokens, n, weights, LinearWeights, dtype, out, "gptaq_linear")
     _check(load().gptaq_linear(X.data_ptr(), tokens, _ld(X, tokens, n), *weights._args(device), Y.data_ptr(), _ld(Y, tokens, weights.m),
                                Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear")
     return Y
@@ -557,7 +559,7 @@ def gptaq_linear_i8(codes: torch.Tensor, scales: torch.Tensor, weights: LinearWe
     if scales.numel() != tokens:
         raise GptaqError("gptaq_linear_i8: scales: expected one per token")
     device = _here(codes, scales, out)
-    Y = _linear_out(codes, tokens, n, weights, dtype, out, "gptaq_linear_i8")
+    Y = _linear_out(codes, tokens, n, weights, LinearWeights, dtype, out, "gptaq_linear_i8")
     _check(load().gptaq_linear_i8(codes.data_ptr(), scales.data_ptr(), tokens, _ld(codes, tokens, n), *weights._args(device), Y.data_ptr(),
                                   _ld(Y, tokens, weights.m), Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear_i8")
     return Y
@@ -622,7 +624,7 @@ def gptaq_linear8_i8(codes: torch.Tensor, scales: torch.Tensor, weights: Linear8
     if scales.numel() != tokens:
         raise GptaqError("gptaq_linear8_i8: scales: expected one per token")
     device = _here(codes, scales, out)
-    Y = _linear_out(codes, tokens, n, weights, dtype, out, "gptaq_linear8_i8")
+    Y = _linear_out(codes, tokens, n, weights, Linear8Weights, dtype, out, "gptaq_linear8_i8")
     _check(load().gptaq_linear8_i8(codes.data_ptr(), scales.data_ptr(), tokens, _ld(codes, tokens, n), *weights._args(device), Y.data_ptr(),
                                    _ld(Y, tokens, weights.m), Y.dtype is torch.float32, _ws(ws, device), ws.nbytes, _stream(device)), "gptaq_linear8_i8")
     return Y

@@ -265,3 +265,37 @@ def test_the_binding_looks_at_shapes(lib, monkeypatch):
         B.gptaq_attention(**rest, ws=ws)
     with pytest.raises(B.GptaqError, match="cpu"):
         B.gptaq_cache_append(**good)
+
+
+class Calls:
+    """In the library's place: what was called, and with how many arguments; every call succeeds."""
+
+    def __init__(self):
+        self.made = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.made.append((name, len(args))) or 0
+
+
+def test_products_tell_the_two_kinds_of_weights_apart(lib, monkeypatch):
+    """On host memory, with nothing behind the calls: weights of the other kind are refused before the library is reached, those of the own kind reach it."""
+    import torch
+    from paper_2504_02692_amd import binding as B
+    eight_bits = eight()
+    four = B.LinearWeights(torch.zeros(B.gptaq_linear_weights_bytes(48, 128, 0), dtype=torch.uint8), 48, 128, 0, None, torch.zeros(48), torch.zeros(1, dtype=torch.int32))
+    calls = Calls()
+    monkeypatch.setattr(B, "load", lambda: calls)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)                 # host memory's own number
+    monkeypatch.setattr(B, "_raw_stream", lambda device: 0)
+    for check in ("_need", "_need_vec"):
+        monkeypatch.setattr(B, check, lambda *args: None)
+    codes, scales, x, ws = torch.zeros(4, 128, dtype=torch.int8), torch.ones(4), torch.zeros(4, 128, dtype=torch.bfloat16), torch.zeros(256, dtype=torch.uint8)
+    for name, args, own, other in (("gptaq_linear8_i8", (codes, scales), eight_bits, four), ("gptaq_linear_i8", (codes, scales), four, eight_bits), ("gptaq_linear", (x,), four, eight_bits)):
+        with pytest.raises(B.GptaqError, match=f"{name}: weights: .*{type(own).__name__}"):
+            getattr(B, name)(*args, other, ws)
+        with pytest.raises(B.GptaqError, match=f"{name}: weights: "):
+            getattr(B, name)(*args, other.data, ws)
+        assert calls.made == []
+        getattr(B, name)(*args, own, ws)
+        assert calls.made == [(name, len(B._SIGS[name][1]))]
+        calls.made.clear()
