@@ -66,6 +66,8 @@ class QuantizedMLP(NamedTuple):
             both = product(codes, scales, self.gate_up, ws)
             codes, scales = B.gptaq_silu_mul_i8(both[:, :inner], both[:, inner:])
             return product(codes, scales, self.down, ws), total
+        if any(isinstance(w, B.Linear8Weights) for w in (self.gate_up, self.down)):
+            raise B.GptaqError("QuantizedMLP: layers of more than 4 bits take 8-bit activations")
         h, total = B.gptaq_rms_norm(x, self.norm, EPS, residual=residual)
         both = B.gptaq_linear(h, self.gate_up, ws)
         return B.gptaq_linear(B.gptaq_silu_mul(both[:, :inner], both[:, inner:]), self.down, ws), total

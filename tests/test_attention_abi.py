@@ -299,3 +299,18 @@ def test_products_tell_the_two_kinds_of_weights_apart(lib, monkeypatch):
         getattr(B, name)(*args, own, ws)
         assert calls.made == [(name, len(B._SIGS[name][1]))]
         calls.made.clear()
+
+
+def test_an_mlp_with_a_layer_of_more_than_4_bits_refuses_bf16_activations(lib, monkeypatch):
+    """Before anything runs, whichever of its layers it is."""
+    import torch
+    from paper_2504_02692_amd import binding as B
+    from paper_2504_02692_amd import quantized_mlp as M
+    calls = Calls()
+    four = lambda m, n: B.LinearWeights(torch.zeros(B.gptaq_linear_weights_bytes(m, n, 0), dtype=torch.uint8), m, n, 0, None, None, torch.zeros(1, dtype=torch.int32))
+    mlps = [M.QuantizedMLP(torch.ones(128), *layers) for layers in ((eight(96, 128), eight(128, 48)), (four(96, 128), eight(128, 48)), (eight(96, 128), four(128, 48)))]
+    monkeypatch.setattr(B, "load", lambda: calls)
+    for mlp in mlps:
+        with pytest.raises(B.GptaqError, match="8-bit activations"):
+            mlp(torch.zeros(4, 128), torch.zeros(4, 128), torch.zeros(256, dtype=torch.uint8), eight_bits=False)
+    assert calls.made == []
