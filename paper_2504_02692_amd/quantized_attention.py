@@ -35,18 +35,23 @@ class PagedCache:
         self.lengths = torch.zeros(seqs, dtype=torch.int32, device="cuda")
 
     def grow(self, counts) -> None:
-        """Makes room for counts[s] new tokens of each sequence, whose rows a pass takes one sequence after the other."""
+        """Makes room for counts[s] new tokens of each sequence, whose rows a pass takes one sequence after the other.  Where they do not fit, nothing changes."""
+        if len(counts) != len(self.counts) or min(counts, default=0) < 0:
+            raise ValueError(f"{len(self.counts)} sequences, each with a count of 0 or more, not {counts}")
+        lengths = [had + count for had, count in zip(self.counts, counts)]
+        missing = [max(0, -(-n // self.page) - len(table)) for n, table in zip(lengths, self.tables)]
+        if sum(missing) > len(self.free) or any(len(table) + more > self.table.shape[1] for table, more in zip(self.tables, missing)):
+            raise RuntimeError("the cache is full")
         starts = [0]
-        for s, count in enumerate(counts):
-            self.counts[s] += count
-            starts.append(starts[-1] + count)
-            while len(self.tables[s]) * self.page < self.counts[s]:
-                if not self.free or len(self.tables[s]) == self.table.shape[1]:
-                    raise RuntimeError("the cache is full")
-                self.table[s, len(self.tables[s])] = self.free[-1]
-                self.tables[s].append(self.free.pop())
+        for s, (table, more) in enumerate(zip(self.tables, missing)):
+            starts.append(starts[-1] + counts[s])
+            if more:                                     # (one copy a sequence)
+                had = len(table)
+                table += [self.free.pop() for _ in range(more)]
+                self.table[s, had:had + more] = torch.tensor(table[had:], dtype=torch.int32)
+        self.counts = lengths
         self.starts.copy_(torch.tensor(starts, dtype=torch.int32))
-        self.lengths.copy_(torch.tensor(self.counts, dtype=torch.int32))
+        self.lengths.copy_(torch.tensor(lengths, dtype=torch.int32))
 
 
 def frequencies(pairs: int) -> torch.Tensor:

@@ -314,3 +314,39 @@ def test_an_mlp_with_a_layer_of_more_than_4_bits_refuses_bf16_activations(lib, m
         with pytest.raises(B.GptaqError, match="8-bit activations"):
             mlp(torch.zeros(4, 128), torch.zeros(4, 128), torch.zeros(256, dtype=torch.uint8), eight_bits=False)
     assert calls.made == []
+
+
+def test_a_cache_that_is_full_stays_as_it_was(monkeypatch):
+    """The example's cache, in host memory: a call that does not fit changes nothing, so other sequences and fewer tokens still do."""
+    import torch
+    from paper_2504_02692_amd import quantized_attention as A
+    for name in ("zeros", "full"):
+        monkeypatch.setattr(torch, name, lambda *a, make=getattr(torch, name), device=None, **more: make(*a, **more))
+    cache = A.PagedCache(3, 6, 1, 64, 16, 64)                        # six pages, four a sequence at most
+
+    def state():
+        return [*cache.counts], [[*t] for t in cache.tables], [*cache.free], cache.table.tolist(), cache.starts.tolist(), cache.lengths.tolist()
+
+    def consistent(counts):
+        pages = [p for t in cache.tables for p in t] + cache.free
+        assert sorted(pages) == list(range(6))
+        for s, t in enumerate(cache.tables):
+            assert len(t) == -(-cache.counts[s] // 16) and cache.table[s].tolist() == t + [-1] * (4 - len(t))
+        assert cache.lengths.tolist() == cache.counts and cache.starts.tolist() == [0, counts[0], counts[0] + counts[1], sum(counts)]
+
+    cache.grow([33, 5, 0])
+    consistent([33, 5, 0])
+    for counts in ([1, 1, 49], [32, 0, 0], [0, 60, 0], [20, 20, 20]):  # too many pages in all, or of one sequence
+        before = state()
+        with pytest.raises(RuntimeError, match="full"):
+            cache.grow(counts)
+        assert state() == before
+    for counts in ([0, 0, 0], [15, 1, 0], [1, 26, 0], [15, 0, 0]):
+        cache.grow(counts)
+        consistent(counts)
+    assert cache.counts == [64, 32, 0] and not cache.free
+    for counts in ([0, 0], [0, 0, 0, 0], [0, -1, 0]):                # not a count for each sequence
+        before = state()
+        with pytest.raises(ValueError):
+            cache.grow(counts)
+        assert state() == before
