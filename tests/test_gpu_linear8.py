@@ -186,3 +186,91 @@ def test_codes_at_ties_and_ends():
     for wrong in (lambda: B.gptaq_quant_activations_i8(X, 0.0), lambda: B.gptaq_quant_activations_i8(X.float()), lambda: B.gptaq_quant_activations_i8(X.cpu())):
         with pytest.raises(B.GptaqError):
             wrong()
+
+
+# ---- many tokens: every tile of linear8_many_kernel, and the columns in parts
+
+def many_plan(tokens, m, n):
+    """(tile, parts) of a call, or None where it takes the kernel of few tokens: the rule as launch_linear8 and many8_plan have it."""
+    mt, kt, blocks = -(-m // 16), -(-n // 128), -(-tokens // 32)
+    if blocks == 1 or (blocks * mt <= 2048 and blocks * mt * kt <= 57344):
+        return None
+    tiles = [-(-tokens // t) * -(-m // r) for t, r in ((64, 128), (128, 128), (256, 256))]
+    t0, t1 = tiles[0] / 256, tiles[1] / 256
+    times = [kt * (max(0.5, 0.38 * t0) if t0 <= 2 else max(1.0, 0.37 * t0)), kt * (0.7 if t1 <= 1 else max(1.15, 0.69 * t1)),
+             kt * (1.6 if tiles[2] <= 128 else 1.9 * -(-tiles[2] // 256))]
+    read = m * kt * 128 / 5e6
+    best, least = (times.index(min(times)), 1), max(min(times), read)
+    for parts in range(2, min(kt // 4, 512 // tiles[0]) + 1):
+        us = max(read, kt / parts * max(0.5, 0.36 * t0 * parts)) + 4 + parts * tokens * m * 8 / 2.5e6
+        if us < least:
+            best, least = (0, parts), us
+    return best
+
+
+MANY = [  # tile and parts, tokens, m, n, what else of `case`
+    ((0, 1), 97, 8200, 130, dict(bias=True)), ((0, 1), 257, 4097, 128, dict(bias=True, perm=True)), ((0, 1), 1030, 1000, 100, dict(bits=5)),
+    ((0, 1), 257, 4097, 384, dict(sym=True, f32=True, bias=True, extra=3, shift=1)),
+    ((0, 2), 65, 8200, 5003, dict(bias=True)), ((0, 2), 3000, 260, 5003, dict(f32=True, perm=True)), ((0, 3), 33, 8200, 8192, dict(bias=True, bits=6)),
+    ((0, 3), 1500, 515, 5003, dict(bias=True, f32=True)), ((0, 4), 257, 2050, 8192, dict(perm=True, extra=16)), ((0, 5), 200, 2050, 8192, dict(bias=True, shift=5)),
+    ((0, 6), 700, 515, 11008, dict(sym=True)),
+    ((1, 1), 3000, 2050, 100, dict(bias=True)), ((1, 1), 1030, 6000, 130, dict(f32=True, bits=7)), ((1, 1), 3000, 2050, 384, dict(perm=True, bias=True, extra=7)),
+    ((1, 1), 1030, 6001, 640, dict(sym=True, f32=True, bias=True)),
+    ((2, 1), 1500, 8200, 100, dict(bias=True)), ((2, 1), 4097, 3001, 130, dict(f32=True, bias=True)), ((2, 1), 1500, 8200, 384, dict(perm=True, shift=1)),
+    ((2, 1), 2100, 6001, 640, dict(bits=5, bias=True, extra=16)),
+]
+
+
+@pytest.mark.parametrize("plan,tokens,m,n,form", MANY)
+def test_many_tokens_in_every_tile_and_in_parts(plan, tokens, m, n, form):
+    assert many_plan(tokens, m, n) == plan
+    case(tokens, m, n, **form)
+
+
+@pytest.mark.parametrize("tokens,m,n,plan", [(200, 260, 65536, (0, 30)), (3000, 2050, 384, (1, 1)), (1500, 8200, 384, (2, 1))])
+def test_many_tokens_hold_the_largest_sums(tokens, m, n, plan):
+    assert many_plan(tokens, m, n) == plan
+    case(tokens, m, n, extremes=True, f32=True)
+
+
+def test_parts_captured_and_replayed():
+    """Graphs of calls whose columns are in parts, and of others, that share a workspace, replayed in turn on new inputs, against eager calls."""
+    r = np.random.default_rng(16)
+    m, n = 2050, 8192
+    codes, scales, zeros = (dev(a) for a in layer(m, n, 8, False, r))
+    w = B.gptaq_linear8_pack(codes, scales, zeros)
+    tokens = (257, 9, 200)
+    assert [many_plan(t, m, n) for t in tokens] == [(0, 4), None, (0, 5)]
+    ws = B.workspace(B.gptaq_linear8_workspace_bytes(max(tokens), m, n))
+    inputs = [(torch.zeros((t, n), dtype=torch.int8, device="cuda"), torch.zeros(t, device="cuda"), torch.empty((t, m), device="cuda")) for t in tokens]
+    graphs = []
+    for x, xs, y in inputs:
+        B.gptaq_linear8_i8(x, xs, w, ws, out=y)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.gptaq_linear8_i8(x, xs, w, ws, out=y)
+        graphs.append(g)
+    for _ in range(3):
+        for (x, xs, y), g in zip(inputs, graphs):
+            x.copy_(dev(r.integers(-127, 128, x.shape).astype(np.int8)))
+            xs.copy_(dev(r.random(len(xs)).astype(np.float32)))
+            g.replay()
+        torch.cuda.synchronize()
+        for x, xs, y in inputs:
+            got = y.clone()
+            ws.fill_(255)
+            assert torch.equal(B.gptaq_linear8_i8(x, xs, w, ws, dtype=torch.float32), got)
+            want = torch.matmul(x.double(), (codes.double() - zeros).t().contiguous()) * xs.double()[:, None] * scales[:, 0].double()
+            assert torch.all((got.double() - want).abs() <= 4 * U * want.abs())
+
+
+@pytest.mark.parametrize("clip", [1.0, 0.5])
+def test_codes_of_rows_whose_scale_is_subnormal(clip):
+    """Scales that have few bits left, and no reciprocal in fp32: scale and codes are still those of the formula; so are rows of the smallest values there are."""
+    half = np.array([127.0, 0.5, 1.5, 2.5, -0.5, -1.5, 63.5, -62.5, 126.5, 0.0])
+    X = bf16(np.stack([half * 2.0 ** -k for k in (120, 126, 127, 129, 130, 132, 133)] + [np.r_[2.0 ** -133, -(2.0 ** -133), np.zeros(8)], np.full(10, -(2.0 ** -126))]))
+    codes, scales = B.gptaq_quant_activations_i8(X, clip)
+    want, scale = codes_of(X.float().cpu().numpy(), clip)
+    assert np.all(scale > 0) and np.any(scale < 2.0 ** -130)
+    assert np.array_equal(scales.cpu().numpy(), scale) and np.array_equal(codes.cpu().numpy(), want)
