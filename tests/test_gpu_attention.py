@@ -572,3 +572,17 @@ def test_the_same_bits_every_time():
             ws.fill_(255)
             assert torch.equal(B.gptaq_attention(q, **dev, ws=ws), first)
     assert B.gptaq_attention(q[:0], **dict(dev, starts=dev["starts"] * 0), ws=ws).shape == (0, heads, 128)
+
+
+def test_thousands_of_sequences():
+    """More than two searches of 64 find: most of them empty or of a token, in whatever order."""
+    r = np.random.default_rng(17)
+    for seqs, busy in ((4097, 60), (5000, 200), (10000, 90)):
+        pairs = [(0, 0)] * seqs
+        for s in {0, seqs - 1, *r.choice(seqs, busy, replace=False).tolist()}:
+            pairs[s] = (int(r.integers(0, 3)), int(r.integers(0, 70)))
+        pairs[seqs - 2] = (9, 40)
+        run(pairs, 2, 1, 64, 16)
+        append_case(pairs, 2, 1, 32, 16)
+    run([(1, int(b)) for b in r.integers(0, 20, 4500)], 2, 1, 64, 16)
+    append_case([(1, int(b)) for b in r.integers(0, 20, 4500)], 2, 1, 16, 16)

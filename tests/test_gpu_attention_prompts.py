@@ -286,3 +286,56 @@ def test_captured_steps_beside_prompts():
         got = out.clone()
         assert torch.equal(call(workspace(305, 3, heads, kv, d), torch.empty_like(out)), got)
         check(got, c, q, heads, 0, 0)
+
+
+def test_thousands_of_sequences():
+    """A lane's run of sequences is longer than a wavefront: prompts among empty sequences, alone and with steps beside them."""
+    r = np.random.default_rng(18)
+    for seqs in (4200, 10000):
+        pairs = [(0, 0)] * seqs
+        for s in (0, 63, 64, seqs // 64 + 1, seqs // 2, seqs - 1):
+            pairs[s] = (130, int(r.integers(0, 50)))
+        tokens = 6 * 130
+        for s in r.permutation(seqs).tolist():                       # (more tokens than sequences: as far as the host can tell one long prompt)
+            if tokens < seqs + 4500 and pairs[s][0] == 0:
+                pairs[s] = (int(r.integers(1, 100)), int(r.integers(0, 50)))
+                tokens += pairs[s][0]
+        width = max(-(-(c + b) // 16) for c, b in pairs) + 1
+        assert -(-(tokens - seqs + 1) // 16) * 8 * (-(-width * 16 // 64) + 9) > 22000
+        run(pairs, 8, 8, 64, 16)
+    pairs = [(0, 0)] * 4303
+    for s in r.choice(4303, 100, replace=False).tolist():
+        pairs[s] = (int(r.integers(1, 4)), int(r.integers(0, 900)))
+    pairs[0], pairs[70], pairs[2000], pairs[4302] = (1500, 0), (1, 2000), (1600, 100), (1500, 20)
+    width = max(-(-(c + b) // 64) for c, b in pairs)
+    assert 1300 * 4 > 4303 and -(-(sum(c for c, _ in pairs) - 4302) * 8 // 16) * 1309 > 22000
+    run(pairs, 8, 1, 64, 64, wider=1300 - width)
+
+
+def test_infinities_and_nan_in_steps_beside_prompts():
+    """Planted in a prompt's, a step's and two tokens' keys and values: those who see them have what the formula says, the others' outputs do not change."""
+    pairs, heads, kv = [(1, 500), (200, 37), (2, 90)], 64, 8
+    c = Cache(pairs, kv, 64, 16, seed=6, wider=800 - 32)             # (room for 12800 positions)
+    assert c.table.shape[1] == 800 and (203 - 3 + 1) * 8 // 16 * kv * 209 > 22000
+    q = queries(c, heads, 64, scale=0.5)
+    clean = c.device()
+    ws = workspace(c.tokens, 3, heads, kv, 64)
+    base = B.gptaq_attention(q, **clean, ws=ws)
+    check(base, c, q, heads, 0, 0)
+    for s, positions in ((0, (0, 250, 500)), (1, (3, 120, 236)), (2, (20, 90, 91))):
+        for j in positions:
+            for kind, bad in (("values", float("inf")), ("values", float("nan")), ("keys", float("nan"))):
+                dev = {k: v.clone() for k, v in clean.items()}
+                id, slot = int(c.table[s, j // 16]), j % 16
+                if kind == "values":
+                    dev["values"][id, 1, slot // 8, 5, slot % 8] = bad
+                else:
+                    dev["keys"][id, 1, 2, slot, 3] = bad
+                y = B.gptaq_attention(q, **dev, ws=ws)
+                assert torch.equal(y[:, :8], base[:, :8]) and torch.equal(y[:, 16:], base[:, 16:]), (s, j, kind, bad)
+                for h in (8, 15):
+                    want, got = plain_head(dev, c, q, h, 1, 0, 0), f64(y[:, h])
+                    odd = ~np.isfinite(want)
+                    assert odd.any() and np.array_equal(got[odd], want[odd], equal_nan=True), (s, j, kind, bad, h)
+                    same = torch.from_numpy(~odd).cuda()
+                    assert torch.equal(y[:, h][same], base[:, h][same]), (s, j, kind, bad, h)
