@@ -381,7 +381,7 @@ int gptaq_quant_activations_i8(const uint16_t* X, int64_t tokens, int64_t n, int
  *   up to d / 2.  out may be q itself (same strides); other overlaps are not allowed.  Queries of positions below 0 are not written.
  * gptaq_attention: out[i] = sum_j w_ij v_j / sum_j w_ij with w_ij = exp(scale q_i k_j) over the positions j that token i, at position p, sees: j <= p, and with
  *   window > 0 only j > p - window or j < sinks.  d is 64, 96 or 128; scale log2(e) is finite in fp32.  A token that sees nothing gives zeros.  What lies where no token sees it (other sequences'
- *   remains, infinities, NaN) changes nothing.
+ *   remains, infinities, NaN) changes nothing.  out may be q itself (same strides); it must not overlap q otherwise, nor the cache.
  *   ws     : >= gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d) bytes, 256-byte aligned; the size for more tokens serves fewer.
  * Scores, the softmax's maximum and sum, and the outputs' sums are fp32; weights w are rounded to bf16 for the product with the values.  The order of a sum depends on
  * the shapes and the lengths alone: no atomics, the same bits every time. */

@@ -798,7 +798,7 @@ def gptaq_attention_workspace_bytes(tokens: int, seqs: int, heads: int, kv_heads
 def gptaq_attention(q: torch.Tensor, keys: torch.Tensor, values: torch.Tensor, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor,
                     ws: torch.Tensor, window: int = 0, sinks: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Causal attention of new tokens' queries (tokens, heads, d) over the cache, which holds their own keys and values already.  window: positions a
-    token sees, itself among them (0: all); sinks: first positions that stay visible.  scale: 1 / sqrt(d) if not given."""
+    token sees, itself among them (0: all); sinks: first positions that stay visible.  scale: 1 / sqrt(d) if not given.  `out` may be q itself."""
     device = _here(q, keys, values, table, starts, lengths, out)
     shape = _heads_of(q, "gptaq_attention")
     tokens, heads, d = shape

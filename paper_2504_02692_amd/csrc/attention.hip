@@ -419,6 +419,7 @@ extern "C" int gptaq_attention(const uint16_t* q, int64_t ldq, int64_t hq, const
   if ((((uintptr_t)q | (uintptr_t)out) & 1) || ldq < 0 || hq < 0 || window < 0 || sinks < 0 ||
       !cache_rows_apart(tokens, ldo, heads, ho, d))
     return GPTAQ_EDIM;
+  if (out == q && tokens != 0 && ((tokens > 1 && ldo != ldq) || (heads > 1 && ho != hq))) return GPTAQ_EUNSUPPORTED;
   const float scale2 = scale * 1.4426950408889634f;
   if (!(fabsf(scale2) < __builtin_inff())) return GPTAQ_EUNSUPPORTED;
   if (tokens == 0 || seqs == 0) return GPTAQ_OK;

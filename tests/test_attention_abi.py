@@ -350,3 +350,11 @@ def test_a_cache_that_is_full_stays_as_it_was(monkeypatch):
         with pytest.raises(ValueError):
             cache.grow(counts)
         assert state() == before
+
+
+def test_attention_over_the_queries_memory_in_other_places_is_refused(lib):
+    own = -4                                              # (taken, as far as the workspace)
+    for tokens, heads, ldo, ho, want in ((3, 4, 512, 64, -3), (3, 4, 256, 80, -2), (3, 4, 768, 192, -3), (3, 4, 256, 64, own), (1, 4, 512, 64, own), (1, 4, 512, 72, -3),
+                                         (3, 2, 256, 64, own), (3, 2, 260, 64, -3)):
+        assert lib.gptaq_attention(ONE, 256, 64, packed(), tokens, heads, 0, 0, 0.125, ONE, ldo, ho, ONE, 0, NULL) == want, (tokens, heads, ldo, ho)
+    assert lib.gptaq_attention(ONE, 256, 64, packed(), 0, 4, 0, 0, 0.125, ONE, 512, 64, ONE, BIG, NULL) == 0

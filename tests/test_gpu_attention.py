@@ -586,3 +586,12 @@ def test_thousands_of_sequences():
         append_case(pairs, 2, 1, 32, 16)
     run([(1, int(b)) for b in r.integers(0, 20, 4500)], 2, 1, 64, 16)
     append_case([(1, int(b)) for b in r.integers(0, 20, 4500)], 2, 1, 16, 16)
+
+
+def test_the_output_may_be_the_queries_memory():
+    """With parts and a join, without, and in rows that are parts of longer ones."""
+    for pairs, heads, kv, extra in (([(1, 3000), (1, 5)], 8, 2, 0), ([(1, 30), (2, 20), (0, 3)], 8, 2, 6), ([(40, 100), (1, 7)], 6, 2, 0)):
+        c = Cache(pairs, kv, 64, 16)
+        q, dev, ws = queries(c, heads, 64, extra=extra), c.device(), workspace(c.tokens, len(pairs), heads, kv, 64)
+        want = B.gptaq_attention(q, **dev, ws=ws)
+        assert B.gptaq_attention(q, **dev, ws=ws, out=q) is q and torch.equal(q, want)

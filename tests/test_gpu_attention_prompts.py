@@ -339,3 +339,13 @@ def test_infinities_and_nan_in_steps_beside_prompts():
                     assert odd.any() and np.array_equal(got[odd], want[odd], equal_nan=True), (s, j, kind, bad, h)
                     same = torch.from_numpy(~odd).cuda()
                     assert torch.equal(y[:, h][same], base[:, h][same]), (s, j, kind, bad, h)
+
+
+def test_the_output_may_be_the_queries_memory():
+    """In blocks of many rows, with parts and without, and with steps beside prompts."""
+    for pairs, heads, kv, d, wider in (([(150, 60), (33, 0)], 4, 2, 64, 1), ([(100, 6000), (60, 100)], 24, 12, 128, 1), ([(1, 500), (200, 37), (2, 90)], 64, 8, 64, 766)):
+        m = times(pairs, heads, kv, 16, wider=wider)
+        c = Cache(pairs, kv * m, d, 16, wider=wider)
+        q, dev, ws = queries(c, heads * m, d), c.device(), workspace(c.tokens, len(pairs), heads * m, kv * m, d)
+        want = B.gptaq_attention(q, **dev, ws=ws)
+        assert B.gptaq_attention(q, **dev, ws=ws, out=q) is q and torch.equal(q, want)
