@@ -595,3 +595,35 @@ def test_the_output_may_be_the_queries_memory():
         q, dev, ws = queries(c, heads, 64, extra=extra), c.device(), workspace(c.tokens, len(pairs), heads, kv, 64)
         want = B.gptaq_attention(q, **dev, ws=ws)
         assert B.gptaq_attention(q, **dev, ws=ws, out=q) is q and torch.equal(q, want)
+
+
+@pytest.mark.parametrize("pairs", [[(1, 300), (3, 20)], [(150, 150)]])
+def test_scores_of_minus_infinity_weigh_nothing(pairs):
+    """Where a token sees no others, zeros, as for one that sees nothing.  One of infinity makes NaN."""
+    c = Cache(pairs, 2, 64, 16, seed=14)
+    for s in range(len(pairs)):
+        c.k[s][::3, 0, 7] = -np.inf
+        c.k[s][:, 1, 9] = -np.inf
+    q = queries(c, 4, 64)
+    q[..., 7] = q[..., 9] = 1.0
+    dev, ws = c.device(), workspace(c.tokens, len(pairs), 4, 2, 64)
+    y = B.gptaq_attention(q, **dev, ws=ws)
+    assert torch.all(y[:, 2:] == 0)
+    for s in range(len(pairs)):                                      # scores so low that they weigh nothing
+        c.k[s][::3, 0] = np.where(np.arange(64) == 7, -(2.0 ** 40), 0.0)
+        c.k[s][:, 1] = 0.0
+    see = f64(B.gptaq_attention(q, **c.device(), ws=ws))
+    assert np.array_equal(f64(y)[:, :2], see[:, :2])
+    c.k[0][0, 0, 7] = np.inf
+    y = B.gptaq_attention(q, **c.device(), ws=ws)
+    assert torch.all(torch.isnan(y[:c.pairs[0][0], :2])) and not torch.any(torch.isnan(y[c.pairs[0][0]:])) and not torch.any(torch.isnan(y[:, 2:]))
+
+
+@pytest.mark.parametrize("pairs", [[(1, 8000), (1, 30)], [(150, 300)]])
+def test_values_of_2_to_the_100(pairs):
+    """Sums of weights of up to 2^8 a key stay inside fp32 for them."""
+    c = Cache(pairs, 2, 64, 16, seed=15)
+    for s in range(len(pairs)):
+        c.v[s] = c.v[s] * 2.0 ** 100
+    q = queries(c, 4, 64, scale=8.0)
+    check(B.gptaq_attention(q, **c.device(), ws=workspace(c.tokens, len(pairs), 4, 2, 64)), c, q, 4, 0, 0)

@@ -349,3 +349,29 @@ def test_the_output_may_be_the_queries_memory():
         q, dev, ws = queries(c, heads * m, d), c.device(), workspace(c.tokens, len(pairs), heads * m, kv * m, d)
         want = B.gptaq_attention(q, **dev, ws=ws)
         assert B.gptaq_attention(q, **dev, ws=ws, out=q) is q and torch.equal(q, want)
+
+
+def test_scores_of_minus_infinity_weigh_nothing():
+    """Where a token sees no others, zeros, as for one that sees nothing."""
+    pairs = [(150, 150)]
+    m = times(pairs, 2, 1, 16)
+    c = Cache(pairs, m, 64, 16, seed=14)
+    c.k[0][::3, 0, 7] = -np.inf
+    c.k[0][:, 1, 9] = -np.inf
+    q = queries(c, 2 * m, 64)
+    q[..., 7] = q[..., 9] = 1.0
+    ws = workspace(c.tokens, 1, 2 * m, m, 64)
+    y = B.gptaq_attention(q, **c.device(), ws=ws)
+    assert torch.all(y[:, 2:4] == 0) and not torch.any(torch.isnan(y))
+    c.k[0][::3, 0] = np.where(np.arange(64) == 7, -(2.0 ** 40), 0.0)
+    assert torch.equal(y[:, :2], B.gptaq_attention(q, **c.device(), ws=ws)[:, :2])
+
+
+def test_values_of_2_to_the_100():
+    """Sums of weights of up to 2^8 a key stay inside fp32 for them."""
+    pairs = [(150, 3000)]
+    m = times(pairs, 2, 1, 16)
+    c = Cache(pairs, m, 64, 16, seed=15)
+    c.v[0] = c.v[0] * 2.0 ** 100
+    q = queries(c, 2 * m, 64, scale=8.0)
+    check(B.gptaq_attention(q, **c.device(), ws=workspace(c.tokens, 1, 2 * m, m, 64)), c, q, 2 * m, 0, 0)
