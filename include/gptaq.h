@@ -385,7 +385,7 @@ int gptaq_quant_activations_i8(const uint16_t* X, int64_t tokens, int64_t n, int
  *   ws     : >= gptaq_attention_workspace_bytes(tokens, seqs, heads, kv_heads, d) bytes, 256-byte aligned; the size for more tokens serves fewer.
  * Scores, the softmax's maximum and sum, and the outputs' sums are fp32; weights w are rounded to bf16 for the product with the values.  The order of a sum depends on
  * the shapes and the lengths alone: no atomics, the same bits every time.  A key whose score is minus infinity has no weight, and a token that sees no other gives zeros; one whose score is infinity
- * or NaN makes its tokens NaN.  The outputs' sums hold weights of up to 2^8 a key: outputs are infinite or NaN where the largest value, times the keys that a token sees, passes 2^119. */
+ * or NaN makes its tokens NaN.  The outputs' sums hold weights of up to 2^8 a key: outputs may be infinite or NaN where the largest value, times the keys that a token sees, passes 2^119. */
 typedef struct gptaq_cache {
   uint16_t *keys, *values;
   int64_t pages, kv_heads, page, d;

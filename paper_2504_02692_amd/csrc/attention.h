@@ -42,9 +42,6 @@ __device__ __forceinline__ Tiles attention_tiles(const AttentionArgs& a, int pmi
   if (t.first > end) t.count = min(t.sink_tiles, end);
   return t;
 }
-__device__ __forceinline__ bool attention_sees(const AttentionArgs& a, int p, int j) {
-  return j <= p && (a.window == 0 || j > p - a.window || j < a.sinks);
-}
 // The token of a row that is the same in all lanes (a division is vector work).
 __device__ __forceinline__ int at_token(int row, int group) { return __builtin_amdgcn_readfirstlane(row / group); }
 // Tiles a part has, and how many parts there are.  Blocks of few rows have no more than 20 parts unless these have 20 tiles: joining more takes longer than they save.  us,

@@ -15,14 +15,13 @@ struct CacheShape {
 };
 // A sequence's new tokens: rows first .. first + count - 1, positions before .. before + count - 1 (before may be negative where `lengths` says less than
 // `starts`; positions below 0 are no tokens).  Whatever the arrays hold, rows stay inside the tensors and positions inside 31 bits.
-struct Sequence { int32_t index, first, count, before; };
+struct Sequence { int32_t first, count, before; };
 // What one address serves all lanes is read through the scalar cache (nothing of it changes while a kernel runs), and waited for apart from loads to LDS.
 typedef const __attribute__((address_space(4))) int32_t* ConstantInts;
 __device__ __forceinline__ ConstantInts cache_constant(const int32_t* p) { return (ConstantInts)(uintptr_t)p; }
 __device__ __forceinline__ int cache_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 __device__ __forceinline__ Sequence cache_sequence(const CacheShape& c, int s) {
   Sequence q;
-  q.index = s;
   q.first = cache_clamp(cache_constant(c.starts)[s], 0, c.tokens);
   q.count = cache_clamp(cache_constant(c.starts)[s + 1], q.first, c.tokens) - q.first;
   q.before = cache_clamp(cache_constant(c.lengths)[s], 0, 1 << 30) - q.count;
