@@ -10,8 +10,8 @@ namespace gptaq {
 // row (l % 16), and O^T = V^T P^T takes them from there, with the keys in such an order that a lane's scores of 32 keys are what the second product wants of it: row
 // 4 a + i of the first product's tile T has key 8 a + 4 T + i.  The four wavefronts of a block take 32 keys each in turn and join through LDS.
 // Weights are rounded to bf16 for the second product (2^-9 each, as the output is once more); their sum is taken of the fp32 values.
-// 64 sequences of up to 8192 positions, 64 heads over 8 of 128: 207 us, 5.4 TB/s, with two loads of 16 KB in flight a wavefront and two blocks a CU.  One of 2000 in a window
-// of 1024: 6.3 us in 160 blocks, and the join.
+// 64 sequences of up to 8192 positions, 64 heads over 8 of 128: 212 to 217 us, 5.3 TB/s, with two loads of 16 KB in flight a wavefront and two blocks a CU.  One of 2000 in a
+// window of 1024: 7.6 to 8 us in 160 blocks, and 4.7 for the join.
 template <int D>
 __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionArgs a) {
   constexpr int KS = D / 32, VT = D / 16, PAD = D + 4;
@@ -318,24 +318,47 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, in
 // ---- how a call is dealt out.  The host knows neither the lengths nor the tokens of a sequence, so it plans with what it knows: tokens, sequences, heads.
 constexpr int64_t kMostParts = 64, kMostFewMixed = 32, kPartialRows = 65536, kFewMixedRows = 1024 * kFewMixed;
 static int64_t attention_blocks(int64_t tokens, int64_t seqs, int64_t group, int bits) { return ((tokens * group) >> bits) + seqs; }
-// Blocks of few rows read the keys once for 16 rows, and little else bounds them; blocks of many read them once for 128, and take longer to begin and end.  So calls are of
-// few as long as the tiles of their blocks, with nine for what a block costs besides, are kFewWork at most.
-// In other calls sequences of 16 rows at most (a step's tokens beside a prompt) are blocks of few all the same, dealt out by themselves, where there may be more than kMixedTiles tiles, which a block
-// of many takes one after the other, and too few sequences to fill the chip that way.  64 heads over 8, all in blocks of many / this way: 7 sequences' tokens behind 32000 and 512 of a prompt 734 /
-// 197 us (apart 175 and 20); 16 behind 8000 and 2048 behind 2048 393 / 320 (102 and 214); but 31 behind 4000 and 512 134 / 128, 63 and 1000 222 / 227, 100
-// behind 1000 and 300 91 / 102, and prompts alone take 3 to 5 us longer, for launches that find nothing.  us a call of few / many, rows of a
-// sequence and key head (and that number): 32 heads behind 2000 positions 96 19.6 / 25.6 (8k), 256 25.8 / 32.5 (23k), 512 51 / 46 (50k); 64 heads over 8 behind 8000, 256 27.7 / 29.5 (17k), 384
-// 47 / 35 (26k); four sequences of these behind 4000, 128 30 / 31 (18k), 256 44 / 41 (37k); sixteen, 32 heads over 8 behind 2000, 64 29.5 / 33.5 (21k), 96 45 / 37 (31k); 64 behind 500, 32 26 / 22
-// (17k), 48 37 / 24 (26k); 32 heads with no positions before, 512 14.5 / 19 (17k), 768 23 / 24.5 (32k); 64 behind 8000, 64 heads over 8, 16 324 / 301, 32 408 / 319, 96 724 / 342.
+// Blocks of few rows read the keys once for 16 rows, and little else bounds them; blocks of many read them once for 128, and take longer to begin and end.
+// So calls are of few as long as the tiles of their blocks, with nine for what a block costs besides, are kFewWork at most.
+//   us a call of few / many, by rows of a sequence and key head (in brackets the number that the rule goes by):
+//     32 heads behind 2000 positions           96 19.6 / 25.6 (8k)      256 25.8 / 32.5 (23k)    512 51 / 46 (50k)
+//     32 heads behind none                     512 14.5 / 19 (17k)      768 23 / 24.5 (32k)
+//     64 heads over 8 behind 8000              256 27.7 / 29.5 (17k)    384 47 / 35 (26k)
+//     four sequences of these behind 4000      128 30 / 31 (18k)        256 44 / 41 (37k)
+//     sixteen, 32 heads over 8 behind 2000     64 29.5 / 33.5 (21k)     96 45 / 37 (31k)
+//     64 behind 500                            32 26 / 22 (17k)         48 37 / 24 (26k)
+//     64 behind 8000, 64 heads over 8          16 324 / 301             32 408 / 319             96 724 / 342
+// Tiles are those of the table: one much wider than the sequences are long plans for the longest that it has room for.  us a call in a graph, in a table of
+// 512 positions (or 300) / of 128000: a prompt of 512, 32 heads 16.1 / 23.8; four of up to 300, 32 heads over 8 17.3 / 25.1.
+//
+// In calls of many, sequences of 16 rows at most (a step's tokens beside a prompt) are blocks of few all the same, dealt out by themselves, where there may be
+// more than kMixedTiles tiles, which a block of many takes one after the other, and too few sequences to fill the chip that way.
+//   us a call, 64 heads over 8, all in blocks of many / this way (steps and prompt in calls of their own):
+//     7 tokens behind 32000 and 512 of a prompt       734 / 197 (175 and 20)
+//     16 behind 8000 and 2048 behind 2048             393 / 320 (102 and 214)
+//     31 behind 4000 and 512                          134 / 128
+//     63 behind 4000 and 1000                         222 / 227
+//     100 behind 1000 and 300                         91 / 102
+//   Prompts alone take 3 to 5 us longer, for launches that find nothing.
 constexpr int64_t kFewWork = 22000, kMixedTiles = 96, kMixedRows = 256;      // (kMixedRows: smaller calls need no room for both)
 struct Plan { int bits; int64_t parts; int min_tiles; };
-// Rows of a block, and parts of the keys.  Blocks of many rows: the parts, of 8 tiles at least, that take the least time by what calls were measured to take: a tile 1.6 us where no CU has two
-// blocks, 2.35 where all have; sums that are joined 3.5 us, and their rows' and bytes' time.  us a call, as many parts as make two blocks a CU / these: three sequences of 256 tokens behind 600, 32 heads
-// 37 (2) / 29 (1); sixteen of 64 behind 2000, 32 heads over 8 60 (2) / 55 (1); 1024 tokens of 32 heads 41 (2) / 30 (1); 96 of 64 heads over 8 behind 8000 47 / 47 (8).
-// Blocks of few rows: for two a CU, of 4 tiles at least, or, which
-// evens sequences of different lengths out, for eight a CU of 32 tiles at least.  us a call, room for 512 / 1024 / 2048 workgroups of 4 tiles: 64 heads over 8 of 128, 64
-// sequences of up to 1000 positions 30.0 / 35.5 / 43.7 (those that find nothing to do take a microsecond, too), of up to 8191 245 / 241 / 234; 8 heads, 8 of up to 16000
-// 70.8 / 73.7 / 73.4.  Tiles at least, 2 / 4 / 9: 32 heads, one sequence of 200 8.1 / 5.8 / 7.5, a window of 1024 11.4 / 10.7 / 12.9; 64 over 8, 8000 18.4 / 16.0 / 15.4.
+// Rows of a block, and parts of the keys.
+// Blocks of many rows: the parts, of 8 tiles at least, that take the least time by what calls were measured to take: a tile 1.6 us where no CU has two blocks,
+// 2.35 where all have; sums that are joined 3.5 us, and their rows' and bytes' time.
+//   us a call, as many parts as make two blocks a CU / these:
+//     three sequences of 256 tokens behind 600, 32 heads       37 (2) / 29 (1)
+//     sixteen of 64 behind 2000, 32 heads over 8               60 (2) / 55 (1)
+//     1024 tokens of 32 heads                                  41 (2) / 30 (1)
+//     96 of 64 heads over 8 behind 8000                        47 / 47 (8)
+// Blocks of few rows: for two a CU, of 4 tiles at least, or, which evens sequences of different lengths out, for eight a CU of 32 tiles at least.
+//   us a call, room for 512 / 1024 / 2048 workgroups of 4 tiles:
+//     64 heads over 8 of 128, 64 sequences of up to 1000       30.0 / 35.5 / 43.7 (those that find nothing to do take a microsecond, too)
+//     64 of up to 8191                                         245 / 241 / 234
+//     8 heads, 8 of up to 16000                                70.8 / 73.7 / 73.4
+//   tiles at least, 2 / 4 / 9:
+//     32 heads, one sequence of 200                            8.1 / 5.8 / 7.5
+//     32 heads, a window of 1024                               11.4 / 10.7 / 12.9
+//     64 heads over 8, one of 8000                             18.4 / 16.0 / 15.4
 static Plan many_plan(int64_t blocks, int64_t rows, int64_t tiles, int64_t d) {
   int64_t best = 1;
   double least = 1e30;

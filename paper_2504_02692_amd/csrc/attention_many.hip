@@ -9,8 +9,10 @@ namespace gptaq {
 // of kRing pieces with one barrier a piece.  Both products are taken transposed, with v_mfma 32x32x16: S^T = K Q^T leaves a lane the scores of one row (l % 32), and O^T = V^T P^T
 // takes the weights from there without an exchange, if the first product's row 16 s + 8 b + 4 a + i has key 16 s + 8 a + 4 b + i (bits 2 and 3 change places).
 // Reads of either from LDS are runs of 512 bytes: no bank is met twice.
-// Bound by power: the matrix unit is busy for 49 % of the cycles, at 1.9 GHz (2048 tokens behind 14336, 32 heads of 128: 508 us, 1.01 PFLOP/s; 8192 tokens, 64 heads over 8:
-// 0.55 ms, 1.0).  Two blocks of 128 rows share a CU, so that one works while the other begins, ends or waits; one block of 256 with pieces of 64 reads keys half as
+// 2048 tokens behind 14336, 32 heads of 128: 528 us, 0.98 PFLOP/s; 8192 tokens, 64 heads over 8: 1.08 ms, 1.0; in a window of 2048, 32 heads: 314 to 323 us, of which a tenth is
+// masked.  No unit is busy throughout: the matrix unit for 51 % of the cycles (48 behind 14336, 41 in the window), vector instructions issue in 40 to 45 %, LDS is read
+// for a quarter, at a clock of 1.80 to 1.93 GHz.  Of a wavefront's time 46 % are its instructions, 27 to 30 % wait for a turn at a unit, and 23 to 28 % wait for loads, LDS or a
+// barrier: it is the steps' own chain, two wavefronts a SIMD, at the clock that there is.  Two blocks of 128 rows share a CU, so that one works while the other begins, ends or waits; one block of 256 with pieces of 64 reads keys half as
 // often, which takes 2 to 4 % off the largest calls, and adds 3 to 10 % to those in a window or of a few rounds (8192 tokens, window 2048: 296 / 306 us; 512 tokens
 // of 32 heads 19 / 24; of 64 heads over 8 behind 8000, 40 / 58).
 // PB: bits of a page as far as they matter to a piece's layout (4, 5: pages of 16, and more).

@@ -30,7 +30,7 @@ __device__ __forceinline__ void ca_unpack(u32x4 a, float (&v)[8]) {
 // written whole where all eight are new, and so many tokens share the cosines and sines.  grid.y shares out the block's pieces of 16 entries where there are few blocks.
 // (a, b) -> (a cos - b sin, b cos + a sin) in fp32, rounded once; the angle, position * frequency, is reduced to a fraction of a turn in fp64, as positions
 // times the largest frequency pass what fp32 resolves, and its sine and cosine are taken in fp32 from there (2^-24 of a turn, a 2^-13th of a bf16 rounding).
-// Bound by memory: five prompts of up to 4096 tokens, 32 heads of 128, 373 MB in 77 to 87 us (4.3 to 4.8 TB/s); 37 tokens by the launch and two trips to memory, 4.7 us.
+// Bound by memory: five prompts of up to 4096 tokens, 32 heads of 128, 373 MB in 87 to 89 us (4.2 to 4.3 TB/s); 37 tokens by the launch and two trips to memory, 4.3 us.
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs p) {
   __shared__ float turn[8 * 256];                                   // [position in the block][pair][cos, sin], 128 pairs at most
   const CacheShape& c = p.c;

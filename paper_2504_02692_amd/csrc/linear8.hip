@@ -19,7 +19,8 @@ __global__ __launch_bounds__(256) void linear8_invert_kernel(int32_t* inverse, i
   if (at < n && (uint32_t)perm[at] < (uint32_t)n) atomicMax(inverse + perm[at], at);
 }
 // R rows of a tile of 16 per workgroup, by way of LDS, where their bytes are picked out in the columns' order; a thread writes 16 columns of each.  (Picked from memory
-// they are a load of a byte each: 4096 x 11008 in act_order's order 377 us, this way 71.)
+// they are a load of a byte each: 4096 x 11008 in act_order's order 377 us, this way 72.)  Bound by those reads of LDS, one for every byte, in any order: 28672 x 8192 288 us,
+// three times what its bytes take.  It runs once a layer.
 constexpr int kPack8Lds = 65536;
 template <int R>
 __global__ __launch_bounds__(256) void linear8_pack_kernel(const uint8_t* codes, int64_t ldc, const float* scales, const float* zeros, int m, int n, int kt,
@@ -94,8 +95,8 @@ __device__ __forceinline__ i32x4 linear8_mfma(u32x4 a, u32x4 b, i32x4 c) {
 // among themselves.  Weights go straight from memory to the lanes that feed the matrix unit, two runs ahead; activations through LDS in runs of a token's 128
 // columns, to a place of the wavefront's own.  The activations' sum comes from one more matrix instruction, with ones.
 // The left operand is 16 tokens (lane l: token l % 16), the right 16 rows of W, the result has the row in l % 16 and tokens 4 (l / 16) .. + 3.
-// Bound by the weights' bytes, small layers by a launch and a trip to memory: 28672 x 8192, 17 tokens 53.6 us (4.4 TB/s); 4096 x 11008, 37 tokens 12.4 us (3.7 TB/s);
-// 4096 x 4096, one token 4.2 us.
+// Bound by the weights' bytes, small layers by a launch and a trip to memory: 28672 x 8192, 17 tokens 51 us (4.6 TB/s); 4096 x 11008, 37 tokens 12.7 us (3.7 TB/s);
+// 4096 x 4096, one token 5.2 to 5.7 us.
 constexpr int kFew8Waves = 16;
 template <int RT, int TT>
 __global__ __launch_bounds__(64 * kFew8Waves) void linear8_few_kernel(Linear8Args p) {

@@ -9,8 +9,9 @@ namespace gptaq {
 // read for half of the time that the matrix unit works.
 // The left operand is W, so that a lane has four rows of a token side by side.  The activations' sums (linear8.h) are taken by dot products of four of the fragments that
 // the wavefront has, each fragment by one of the wavefronts that share the tokens.
-// Bound by power: 8192 tokens, 28672 x 8192, tiles of 256 x 256 1.63 to 1.67 ms, 2.3 POP/s with the matrix unit busy for 60 % of the cycles at 1.87 GHz.  Small calls by
-// the latency of their stages: 257 tokens, 4096 x 1024, eight stages of 160 tiles, 9.2 us.
+// 8192 tokens, 28672 x 8192, tiles of 256 x 256: 1.65 ms, 2.3 POP/s, with the matrix unit busy for 60 % of the cycles at 1.74 to 1.81 GHz; of a wavefront's time 43 % waits
+// for its turn at the unit and 32 % for loads and barriers.  Small calls are bound by their stages, each of which waits for loads that were asked for two
+// stages before: 257 tokens, 4096 x 1024, eight stages of 160 tiles, 8.3 us.
 constexpr int kX8Ring = 4;
 template <int TT, int RT, int WT, int WR> struct Many8 {
   static constexpr int kTokens = 32 * TT * WT, kRows = 32 * RT * WR, kWaves = WT * WR;
